@@ -58,11 +58,11 @@ class flux_problem_t(C.Structure):
 
 
 class FluxError(RuntimeError):
-    def __init__(self, status: int, where: str):
+    def __init__(self, status: int, where: str, hip_error: int | None = None):
         self.status = status
         msg = lib().flux_status_string(status).decode()
         if status == FLUX_ERR_HIP:
-            msg += f" (hipError_t {lib().flux_last_hip_error()})"
+            msg += f" (hipError_t {lib().flux_last_hip_error() if hip_error is None else hip_error})"
         super().__init__(f"{where}: {msg} [status {status}]")
 
 

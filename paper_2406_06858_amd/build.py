@@ -1,4 +1,4 @@
-"""Builds libflux_mi355.so (gfx950) in-tree with hipcc.  Usage: python -m paper_2406_06858_amd.build"""
+"""Builds libflux_mi355.so and libflux_ffn_mi355.so (gfx950) in-tree with hipcc.  Usage: python -m paper_2406_06858_amd.build"""
 from __future__ import annotations
 
 import os
@@ -11,7 +11,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libflux_mi355.so")
+FFN_LIB = os.path.join(PKG, "libflux_ffn_mi355.so")
 N_CFGS = 10
+FFN_UNITS = ["flux_ffn_api", "flux_mx4"]      # sources of the second library
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -38,6 +40,8 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
         for nk in (0, 1):
             units.append((os.path.join(CSRC, "flux_gemm_inst.hip"), os.path.join(OBJ, f"flux_gemm_cfg{i}_nk{nk}.o"),
                           [f"-DFLUX_CFG_ID={i}", f"-DFLUX_B_NK={nk}"]))
+    ffn = [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), []) for name in FFN_UNITS]
+    units += ffn
     jobs = jobs or min(8, os.cpu_count() or 1, len(units))
 
     def compile_one(u):
@@ -49,7 +53,9 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
 
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(compile_one, units))
-    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
+    own = len(units) - len(ffn)
+    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs[:own]])
+    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", FFN_LIB, *objs[own:]])
     return LIB
 
 

@@ -1,0 +1,161 @@
+// Matrices to 4-bit blocks of 32 with one power of two each, and back (flux_mx4_quantize, flux_mx4_dequantize).
+//
+// For a block x with largest magnitude a:  e = max(floor(log2 a) - 2, -127),  code_i = E2M1(x_i / 2^e) rounded to nearest
+// even and held at 6.  floor(log2 a) is a's exponent field, so the largest magnitude is taken over the bit patterns, where
+// NaN and infinity come out on top and are told apart by being 0x7f800000 or more.
+//
+// What bounds both kernels is memory: 2 or 4 bytes read and 17/32 written a number, or the other way round.
+#include "flux_ffn_internal.h"
+
+namespace flux_ffn {
+
+constexpr int PER_LANE = 8;                      // numbers of a row that a lane takes: four lanes a block
+constexpr int PER_WAVE = 64 * PER_LANE;          // 16 blocks: the 16 bytes of scales that a wave writes are the padding's unit
+
+struct CastArgs {
+  const void* src;
+  void* dst;
+  uint8_t* q;
+  uint8_t* scales;
+  long long ld;                                  // of src or dst, in elements
+  int32_t rows, K, waves_per_row;
+  uint32_t row_bytes, scale_row_bytes;
+};
+
+__device__ __forceinline__ float from_bf16(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
+// The lane's numbers, zeros past the end of the row.  Rows need no alignment beyond their type's.
+template <class T>
+__device__ __forceinline__ void load8(const T* p, int left, float (&x)[PER_LANE]) {
+  T v[PER_LANE];
+  if (left >= PER_LANE) {
+    __builtin_memcpy(v, p, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) v[i] = i < left ? p[i] : T(0);
+  }
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    if constexpr (sizeof(T) == 2) x[i] = from_bf16(v[i]);
+    else x[i] = v[i];
+  }
+}
+
+// Code of the magnitude a (>= 0): how many of the midpoints between neighbouring values it has passed; a tie passes those
+// whose upper neighbour has the even code.
+__device__ __forceinline__ uint32_t code_of(float a) {
+  return (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) quantize_kernel(const CastArgs c) {
+  const int lane = threadIdx.x & 63;
+  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = (int)(w / c.waves_per_row), seg = (int)(w % c.waves_per_row);
+  if (row >= c.rows) return;
+  const int k = seg * PER_WAVE + lane * PER_LANE;
+  float x[PER_LANE];
+  load8(static_cast<const T*>(c.src) + (long long)row * c.ld + k, c.K - k, x);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  const bool finite = top < 0x7f800000u;
+  const int e = max((int)(top >> 23) - 2, 0);                    // the scale's byte
+  const float inverse = __uint_as_float((uint32_t)(254 - e) << 23);        // (e is 252 at most where the block is finite)
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i)
+    codes |= (code_of(fabsf(x[i]) * inverse) | (__float_as_uint(x[i]) >> 31) << 3) << (4 * i);
+  const int block = k / 32;
+  if (k < (c.K + 31) / 32 * 32) *reinterpret_cast<uint32_t*>(c.q + (long long)row * c.row_bytes + k / 2) = finite ? codes : 0u;
+  if (lane % 4 == 0) c.scales[(long long)row * c.scale_row_bytes + block] = (uint8_t)(finite ? e : 255);
+}
+
+__device__ __forceinline__ float value_of(uint32_t code, float scale) {
+  // exponent and mantissa of E2M1 onto those of fp32: 0 and 0.5 by a product, the rest by place
+  const uint32_t m = code & 7u;
+  const float a = m < 2u ? 0.5f * (float)m : __uint_as_float((126u << 23) + (m << 22));
+  return (code & 8u ? -a : a) * scale;
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) dequantize_kernel(const CastArgs c) {
+  const int lane = threadIdx.x & 63;
+  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = (int)(w / c.waves_per_row), seg = (int)(w % c.waves_per_row);
+  if (row >= c.rows) return;
+  const int k = seg * PER_WAVE + lane * PER_LANE;
+  if (k >= c.K) return;
+  const uint32_t codes = *reinterpret_cast<const uint32_t*>(c.q + (long long)row * c.row_bytes + k / 2);
+  const uint32_t e = c.scales[(long long)row * c.scale_row_bytes + k / 32];
+  const float scale = e == 255u ? __uint_as_float(0x7fc00000u) : e ? __uint_as_float(e << 23) : 0x1p-127f;
+  T v[PER_LANE];
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    const float y = value_of(codes >> (4 * i), scale);           // (three significant bits: exact in bf16)
+    if constexpr (sizeof(T) == 2) v[i] = (uint16_t)(__float_as_uint(y) >> 16);
+    else v[i] = y;
+  }
+  T* const p = static_cast<T*>(c.dst) + (long long)row * c.ld + k;
+  if (k + PER_LANE <= c.K) {
+    __builtin_memcpy(p, v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i)
+      if (k + i < c.K) p[i] = v[i];
+  }
+}
+
+static int cast_args(int32_t rows, int32_t K, int32_t dtype, const void* wide, int64_t ld, const void* q, const void* scales, CastArgs* c) {
+  if (wide == nullptr || q == nullptr || scales == nullptr || (dtype != FLUX_BF16 && dtype != FLUX_F32)) return FLUX_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(scales, 16) || !aligned(wide, dtype == FLUX_BF16 ? 2 : 4)) return FLUX_ERR_INVALID_ARG;
+  if (rows < 1 || K < 1) return FLUX_ERR_SHAPE;
+  const long long pitch = ld ? ld : K;
+  if (pitch < K || (long long)(rows - 1) * pitch + K >= (1ll << 31)) return FLUX_ERR_SHAPE;
+  c->q = static_cast<uint8_t*>(const_cast<void*>(q));
+  c->scales = static_cast<uint8_t*>(const_cast<void*>(scales));
+  c->ld = pitch;
+  c->rows = rows;
+  c->K = K;
+  c->waves_per_row = (K + PER_WAVE - 1) / PER_WAVE;
+  c->row_bytes = (uint32_t)row_bytes(K);
+  c->scale_row_bytes = (uint32_t)scale_row_bytes(K);
+  return FLUX_OK;
+}
+
+static dim3 cast_grid(const CastArgs& c) { return dim3((unsigned)(((long long)c.rows * c.waves_per_row + 3) / 4)); }
+
+}  // namespace flux_ffn
+
+using namespace flux_ffn;
+
+extern "C" {
+
+size_t flux_mx4_row_bytes(int32_t K) { return K < 1 ? 0 : (size_t)row_bytes(K); }
+size_t flux_mx4_scale_row_bytes(int32_t K) { return K < 1 ? 0 : (size_t)scale_row_bytes(K); }
+
+int flux_mx4_quantize(int32_t rows, int32_t K, int32_t src_dtype, const void* src, int64_t ld, void* q, void* scales, void* stream) {
+  CastArgs c = {};
+  const int st = cast_args(rows, K, src_dtype, src, ld, q, scales, &c);
+  if (st != FLUX_OK) return st;
+  c.src = src;
+  if (src_dtype == FLUX_BF16) hipLaunchKernelGGL(quantize_kernel<uint16_t>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
+  else hipLaunchKernelGGL(quantize_kernel<float>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
+  FFN_HIP(hipGetLastError());
+  return FLUX_OK;
+}
+
+int flux_mx4_dequantize(int32_t rows, int32_t K, const void* q, const void* scales, int32_t dst_dtype, void* dst, int64_t ld, void* stream) {
+  CastArgs c = {};
+  const int st = cast_args(rows, K, dst_dtype, dst, ld, q, scales, &c);
+  if (st != FLUX_OK) return st;
+  c.dst = dst;
+  if (dst_dtype == FLUX_BF16) hipLaunchKernelGGL(dequantize_kernel<uint16_t>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
+  else hipLaunchKernelGGL(dequantize_kernel<float>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
+  FFN_HIP(hipGetLastError());
+  return FLUX_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,171 @@
+"""CPU-only checks of the gated block's library and of its oracle: exports, struct layout, refusals before anything is
+enqueued, the oracle's slopes against differences, its 4-bit rounding against values worked out by hand."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from oracle import ffn_oracle as oo
+from paper_2406_06858_amd import binding as fb
+from paper_2406_06858_amd import ffn
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PTR = 4096            # never read: the calls below are refused before anything is enqueued
+
+
+def test_library_exports_what_the_header_declares():
+    header = open(os.path.join(ROOT, "include", "flux_ffn.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(r"\b(flux_[a-z0-9_]+)\s*\(", header))
+    assert declared == set(ffn.EXPORTS)
+    assert all(hasattr(ffn.lib(), name) for name in declared)
+
+
+def test_struct_layouts():
+    assert ctypes.sizeof(ffn.flux_glu_t) == 64 and ffn.flux_glu_t.ldx.offset == 32
+    assert ctypes.sizeof(ffn.flux_mx4_t) == 32 and ffn.flux_mx4_t.ldc.offset == 24
+
+
+def _glu(p, ptrs=None, ws=(PTR, 1 << 40), backward=False):
+    L = ffn.lib()
+    names = ["X", "Wg", "Wu", "G", "U", "dH", "dX", "dWg", "dWu"] if backward else ["X", "Wg", "Wu", "H", "G", "U"]
+    v = {n: PTR for n in names}
+    v.update(ptrs or {})
+    f = L.flux_glu_backward if backward else L.flux_glu
+    return f(None if p is None else ctypes.byref(p), *[v[n] for n in names], ws[0], ws[1], None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("bad,status", [
+    (dict(M=0), fb.FLUX_ERR_SHAPE), (dict(M=-1), fb.FLUX_ERR_SHAPE), (dict(N=0), fb.FLUX_ERR_SHAPE), (dict(K=0), fb.FLUX_ERR_SHAPE),
+    (dict(N=100), fb.FLUX_ERR_SHAPE), (dict(K=100), fb.FLUX_ERR_SHAPE),
+    (dict(ldx=248), fb.FLUX_ERR_SHAPE), (dict(ldx=260), fb.FLUX_ERR_SHAPE), (dict(ldw=120), fb.FLUX_ERR_SHAPE), (dict(ldh=120), fb.FLUX_ERR_SHAPE),
+    (dict(ldh=-128), fb.FLUX_ERR_INVALID_ARG), (dict(M=1 << 24, N=128), fb.FLUX_ERR_SHAPE), (dict(ldh=1 << 27), fb.FLUX_ERR_SHAPE),
+    (dict(act=3), fb.FLUX_ERR_INVALID_ARG), (dict(act=-1), fb.FLUX_ERR_INVALID_ARG), (dict(w_is_nk=2), fb.FLUX_ERR_INVALID_ARG),
+    (dict(out_dtype=2), fb.FLUX_ERR_INVALID_ARG), (dict(dw_dtype=-1), fb.FLUX_ERR_INVALID_ARG), (dict(dw_accumulate=2), fb.FLUX_ERR_INVALID_ARG),
+    (dict(reserved=1), fb.FLUX_ERR_INVALID_ARG),
+])
+def test_glu_refuses_problems(bad, status, backward):
+    p = ffn.glu_problem(64, 128, 256)
+    for k, v in bad.items():
+        setattr(p, k, v)
+    assert _glu(p, backward=backward) == status
+    assert ffn.flux_glu_workspace_bytes(int(backward), p) == 0
+
+
+@pytest.mark.parametrize("backward,ptrs", [
+    (False, {"X": 0}), (False, {"Wu": 0}), (False, {"H": 0}), (False, {"H": PTR + 8}), (False, {"G": 0}), (False, {"U": 0}), (False, {"U": PTR + 2}),
+    (True, {"X": 0}), (True, {"G": 0}), (True, {"dH": 0}), (True, {"dWg": 0}), (True, {"dWu": 0}), (True, {"dX": PTR + 8}),
+])
+def test_glu_refuses_pointers(backward, ptrs):
+    assert _glu(ffn.glu_problem(64, 128, 256), ptrs, backward=backward) == fb.FLUX_ERR_INVALID_ARG
+
+
+def test_null_problem_and_unknown_op():
+    assert _glu(None) == fb.FLUX_ERR_INVALID_ARG
+    assert ffn.flux_glu_workspace_bytes(2, ffn.glu_problem(64, 128, 256)) == 0
+    assert ffn.flux_mx4_workspace_bytes(2, ffn.mx4_problem(64, 128, 256)) == 0
+
+
+def test_backward_wants_its_workspace():
+    p = ffn.glu_problem(64, 128, 256)
+    need = ffn.flux_glu_workspace_bytes(ffn.FLUX_GLU_BACKWARD, p)
+    assert need > 0
+    for ws in ((0, 0), (PTR, need - 1), (PTR + 8, need)):
+        assert _glu(p, ws=ws, backward=True) == fb.FLUX_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(M=0), fb.FLUX_ERR_SHAPE), (dict(N=0), fb.FLUX_ERR_SHAPE), (dict(K=0), fb.FLUX_ERR_SHAPE), (dict(N=100), fb.FLUX_ERR_SHAPE),
+    (dict(ldc=120), fb.FLUX_ERR_SHAPE), (dict(ldc=130), fb.FLUX_ERR_SHAPE), (dict(ldc=-8), fb.FLUX_ERR_INVALID_ARG),
+    (dict(out_dtype=5), fb.FLUX_ERR_INVALID_ARG), (dict(reserved=1), fb.FLUX_ERR_INVALID_ARG),
+    (dict(M=1 << 24), fb.FLUX_ERR_SHAPE),
+])
+@pytest.mark.parametrize("glu", [False, True])
+def test_mx4_products_refuse(bad, status, glu):
+    L = ffn.lib()
+    p = ffn.mx4_problem(64, 128, 256)
+    for k, v in bad.items():
+        setattr(p, k, v)
+    f, n = (L.flux_mx4_glu, 7) if glu else (L.flux_mx4_gemm, 5)
+    assert f(ctypes.byref(p), *[PTR] * n, PTR, 1 << 40, None) == status
+
+
+def test_mx4_products_refuse_pointers_and_act():
+    L = ffn.lib()
+    p = ffn.mx4_problem(64, 128, 256)
+    for i in range(5):
+        for bad in (0, PTR + 8):
+            args = [PTR] * 5
+            args[i] = bad
+            assert L.flux_mx4_gemm(ctypes.byref(p), *args, PTR, 1 << 40, None) == fb.FLUX_ERR_INVALID_ARG
+    p.act = 9
+    assert L.flux_mx4_glu(ctypes.byref(p), *[PTR] * 7, PTR, 1 << 40, None) == fb.FLUX_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("args,status", [
+    ((0, 64, 0, PTR, 0, PTR, PTR), fb.FLUX_ERR_SHAPE), ((4, 0, 0, PTR, 0, PTR, PTR), fb.FLUX_ERR_SHAPE), ((4, 64, 0, PTR, 63, PTR, PTR), fb.FLUX_ERR_SHAPE),
+    ((4, 64, 2, PTR, 0, PTR, PTR), fb.FLUX_ERR_INVALID_ARG), ((4, 64, 0, 0, 0, PTR, PTR), fb.FLUX_ERR_INVALID_ARG),
+    ((4, 64, 0, PTR, 0, 0, PTR), fb.FLUX_ERR_INVALID_ARG), ((4, 64, 0, PTR, 0, PTR, 0), fb.FLUX_ERR_INVALID_ARG),
+    ((4, 64, 0, PTR + 1, 0, PTR, PTR), fb.FLUX_ERR_INVALID_ARG), ((4, 64, 1, PTR + 2, 0, PTR, PTR), fb.FLUX_ERR_INVALID_ARG),
+    ((4, 64, 0, PTR, 0, PTR + 4, PTR), fb.FLUX_ERR_INVALID_ARG), ((1 << 20, 1 << 12, 0, PTR, 0, PTR, PTR), fb.FLUX_ERR_SHAPE),
+])
+def test_casts_refuse(args, status):
+    rows, K, dtype, wide, ld, q, scales = args
+    L = ffn.lib()
+    assert L.flux_mx4_quantize(rows, K, dtype, wide, ld, q, scales, None) == status
+    assert L.flux_mx4_dequantize(rows, K, q, scales, dtype, wide, ld, None) == status
+
+
+def test_mx4_row_sizes():
+    for K, q, s in ((1, 16, 16), (32, 16, 16), (33, 32, 16), (512, 256, 16), (513, 272, 32), (8192, 4096, 256)):
+        assert (ffn.flux_mx4_row_bytes(K), ffn.flux_mx4_scale_row_bytes(K)) == (q, s)
+    assert ffn.flux_mx4_row_bytes(0) == 0 and ffn.flux_mx4_scale_row_bytes(-3) == 0
+
+
+# ---- the oracle ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh"])
+def test_oracle_slope_is_the_derivative(name):
+    g, h = np.linspace(-9, 9, 721), 1e-5
+    assert np.allclose(oo.slope(name, g), (oo.act(name, g + h) - oo.act(name, g - h)) / (2 * h), atol=1e-9)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh"])
+def test_oracle_gradients_against_differences(name):
+    rng = np.random.default_rng(7)
+    x, wg, wu, dh = rng.normal(size=(3, 5)), rng.normal(size=(5, 4)), rng.normal(size=(5, 4)), rng.normal(size=(3, 4))
+    _, g, u = oo.glu(name, x, wg, wu)
+    grads = oo.glu_backward(name, x, wg, wu, g, u, dh)[:3]
+    h = 1e-6
+    for i, t in enumerate((x, wg, wu)):
+        d = rng.normal(size=t.shape)
+        ins = [x, wg, wu]
+        ins[i] = t + h * d
+        up = (oo.glu(name, *ins)[0] * dh).sum()
+        ins[i] = t - h * d
+        assert np.isclose((up - (oo.glu(name, *ins)[0] * dh).sum()) / (2 * h), (grads[i] * d).sum(), rtol=1e-7, atol=1e-8)
+
+
+def test_oracle_rounding_by_hand():
+    # largest 7: floor(log2 7) = 2, scale 1; ties go to the even code; beyond 6 is 6
+    x = np.zeros((1, 32))
+    x[0, :12] = [7, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -5.1, 0.26, -0.25, 6.9]
+    codes, scales = oo.mx4_quantize(x)
+    assert scales[0, 0] == 127
+    assert list(oo.mx4_values(codes, scales)[0, :12]) == [6, 0, 1, 1, 2, 2, 4, 4, -6, 0.5, 0, 6]
+    assert np.signbit(oo.mx4_values(codes, scales)[0, 10])
+    for top, byte in ((2.0 ** -126, 0), (2.0 ** -124, 1), (2.0 ** -149, 0), (1.0, 125), (0.999, 124), (np.inf, 255), (np.nan, 255), (0.0, 0), (2.0 ** 127, 252)):
+        x[:] = 0
+        x[0, 3] = top
+        assert oo.mx4_quantize(x)[1][0, 0] == byte, top
+
+
+def test_oracle_packing_round_trip():
+    rng = np.random.default_rng(3)
+    codes, scales = rng.integers(0, 16, (3, 5, 32)).astype(np.uint8), rng.integers(0, 255, (3, 5)).astype(np.uint8)
+    q, s = oo.mx4_pack(codes, scales)
+    assert q.shape == (3, 80) and s.shape == (3, 16) and not s[:, 5:].any()
+    c2, s2 = oo.mx4_unpack(q, s)
+    assert (c2 == codes).all() and (s2 == scales).all()

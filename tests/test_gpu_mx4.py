@@ -1,0 +1,237 @@
+"""4-bit microscaled matrices on the GPU against their definition in 64 bits: the casts bit for bit, the products within
+the bounds of fp32 sums (K 2^-23 of the sum of magnitudes; see test_gpu_glu) and one rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ffn_oracle as oo
+from paper_2406_06858_amd import ffn
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+ROUND = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+SLOPE = 1.13
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _quantize(x):
+    """x on the GPU (any pitch): (q, scales), which held other bytes before."""
+    rows, K = x.shape
+    q = torch.full((rows, ffn.flux_mx4_row_bytes(K)), 0xA5, dtype=torch.uint8, device=DEV)
+    s = torch.full((rows, ffn.flux_mx4_scale_row_bytes(K)), 0xA5, dtype=torch.uint8, device=DEV)
+    ffn.flux_mx4_quantize(x, q, s)
+    torch.cuda.synchronize()
+    return q, s
+
+
+def _check_cast(x, pad=0):
+    rows, K = x.shape
+    q, s = _quantize(x)
+    wq, ws = oo.mx4_pack(*oo.mx4_quantize(_np(x)))
+    assert np.array_equal(s.cpu().numpy(), ws), "scales, zeros behind them included"
+    nan_block = np.repeat(ws[:, :q.shape[1] // 16] == 255, 16, axis=1)
+    assert np.array_equal(np.where(nan_block, 0, q.cpu().numpy()), np.where(nan_block, 0, wq))
+    for dtype in TORCH.values():
+        store = torch.full((rows, K + pad), 3.0, dtype=dtype, device=DEV)
+        ffn.flux_mx4_dequantize(q, s, store[:, :K])
+        torch.cuda.synchronize()
+        assert np.array_equal(_np(store[:, :K]), oo.mx4_values(*oo.mx4_unpack(wq, ws))[:, :K], equal_nan=True)
+        assert bool((store[:, K:] == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,K", [(1, 1), (1, 32), (3, 31), (2, 33), (5, 100), (7, 512), (4, 513), (3, 1000), (2, 2049), (130, 64), (1, 8192)])
+def test_casts(rows, K, dtype):
+    gen = torch.Generator().manual_seed(rows * 10007 + K)
+    x = torch.randn(rows, K, generator=gen) * torch.exp(2 * torch.randn(rows, 1, generator=gen))
+    _check_cast(x.to(TORCH[dtype]).to(DEV))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,pad", [(64, 8), (65, 3), (200, 1)])
+def test_casts_of_rows_in_a_wider_matrix(K, pad, dtype):
+    store = torch.full((9, K + pad + 1), float("nan"), dtype=TORCH[dtype], device=DEV)
+    store[:, 1:K + 1] = torch.randn(9, K, generator=torch.Generator().manual_seed(K)).to(DEV)
+    _check_cast(store[:, 1:K + 1], pad)
+
+
+def test_every_bf16_number():
+    """Each of the 65536 patterns in a block of its own sign and size, and next to a larger number."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    x = bits.view(torch.bfloat16)
+    alone = torch.zeros(65536, 2, dtype=torch.bfloat16)
+    alone[:, 0] = x
+    top = torch.abs(x)
+    alone[:, 1] = torch.where(torch.isfinite(top) & (top < 1e37), top * 4, top)
+    blocks = torch.zeros(65536, 32, dtype=torch.bfloat16)
+    blocks[:, 3:5] = alone
+    q, s = _quantize(blocks.to(DEV))
+    want_q, want_s = oo.mx4_pack(*oo.mx4_quantize(_np(blocks)))
+    assert np.array_equal(s.cpu().numpy(), want_s)
+    ok = want_s[:, 0] != 255
+    assert np.array_equal(q.cpu().numpy()[ok], want_q[ok])
+
+
+def test_ties_and_their_neighbours_in_32_bits():
+    """Midpoints between values, one ulp below and above them, at scales from the smallest to the largest."""
+    mids = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0], np.float32)
+    near = np.concatenate([np.nextafter(mids, np.float32(0)), mids, np.nextafter(mids, np.float32(9))])
+    rows = []
+    for e in (-126, -125, -100, -24, -3, 0, 1, 17, 90, 124):
+        for sign in (1, -1):
+            row = np.zeros(32, np.float32)
+            row[:27] = np.ldexp(near, e) * sign
+            row[30] = np.ldexp(np.float32(4.0), e)
+            rows.append(row)
+    _check_cast(torch.from_numpy(np.stack(rows)).to(DEV))
+
+
+def test_blocks_that_are_not_finite_or_empty():
+    x = torch.randn(4, 160, generator=torch.Generator().manual_seed(2))
+    x[0, 5], x[1, 40], x[2, 70], x[3, 159] = float("nan"), float("inf"), -float("inf"), float("nan")
+    x[:, 96:128] = 0
+    x[2, 100] = -0.0
+    for dtype in TORCH.values():
+        _check_cast(x.to(dtype).to(DEV))
+    _check_cast((x * 2.0 ** -140).to(DEV))          # subnormal
+
+
+# ---- products -----------------------------------------------------------------------------------------------------
+def _packed(rows, K, seed, scale=1.0):
+    """(q, scales) on the GPU and the values, every scale and code that a quantised matrix can hold among them."""
+    gen = torch.Generator().manual_seed(seed)
+    x = (torch.randn(rows, K, generator=gen) * scale * torch.exp(torch.randn(rows, 1, generator=gen))).to(torch.bfloat16)
+    codes, scales = oo.mx4_quantize(_np(x)) if rows * K <= 1 << 16 else oo.mx4_unpack(*(t.cpu().numpy() for t in _quantize(x.to(DEV))))
+    q, s = oo.mx4_pack(codes, scales)
+    return (torch.from_numpy(q).to(DEV), torch.from_numpy(s).to(DEV)), oo.mx4_values(codes, scales)
+
+
+def _workspace(op, p):
+    n = ffn.flux_mx4_workspace_bytes(op, p)
+    if n == 0:
+        return None
+    ws = torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+    ffn.flux_ffn_init(ws)
+    return ws
+
+
+def _gemm(a, b, M, N, K, out="bf16", pad=0):
+    p = ffn.mx4_problem(M, N, K, out_dtype=out, ldc=N + pad if pad else 0)
+    c = torch.full((M, N + pad), 7.0, dtype=TORCH[out], device=DEV)
+    ffn.flux_mx4_gemm(p, *a, *b, c, _workspace(ffn.FLUX_MX4_GEMM, p))
+    torch.cuda.synchronize()
+    assert bool((c[:, N:] == 7.0).all())
+    return c[:, :N]
+
+
+def _check_gemm(got, a, b, out):
+    ref, size = a @ b.T, np.abs(a) @ np.abs(b).T
+    err, e = np.abs(_np(got) - ref), a.shape[1] * 2.0 ** -23 * size
+    assert (err <= ROUND[out] * (np.abs(ref) + e) + e).all(), f"off by {np.max(err / (ROUND[out] * (np.abs(ref) + e) + e + 1e-300)):.3g} of the bound"
+
+
+PRODUCTS = [
+    (1, 8, 1), (1, 16, 32), (1, 136, 2080), (2, 264, 31), (7, 72, 100), (15, 128, 512), (16, 256, 1024), (17, 40, 544), (33, 200, 96), (48, 64, 4100), (64, 512, 1024),
+    (65, 136, 513), (100, 328, 777), (127, 64, 2048), (129, 256, 288), (256, 256, 256), (256, 512, 1024), (300, 520, 392), (255, 248, 5), (257, 8, 64), (200, 264, 4128),
+    (512, 128, 8192), (1000, 136, 72), (640, 1032, 520),
+]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_gemm(M, N, K, out):
+    (a, va), (b, vb) = _packed(M, K, 1), _packed(N, K, 2, 0.1)
+    _check_gemm(_gemm(a, b, M, N, K, out), va, vb, out)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 72, 100), (40, 264, 300), (300, 264, 300)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_gemm_pitch(M, N, K, out):
+    (a, va), (b, vb) = _packed(M, K, 3), _packed(N, K, 4)
+    _check_gemm(_gemm(a, b, M, N, K, out, pad=16), va, vb, out)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 64, 512), (64, 128, 1024), (300, 256, 768)])
+def test_gemm_any_code_and_scale(M, N, K):
+    """Random bytes: every code, scales over the range in which no sum overflows."""
+    rng = np.random.default_rng(M)
+    mats = []
+    for rows in (M, N):
+        codes, scales = rng.integers(0, 16, (rows, K // 32, 32)).astype(np.uint8), rng.integers(90, 160, (rows, K // 32)).astype(np.uint8)
+        q, s = oo.mx4_pack(codes, scales)
+        mats.append(((torch.from_numpy(q).to(DEV), torch.from_numpy(s).to(DEV)), oo.mx4_values(codes, scales)))
+    _check_gemm(_gemm(mats[0][0], mats[1][0], M, N, K, "f32"), mats[0][1], mats[1][1], "f32")
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 64, 200), (64, 136, 544), (300, 256, 520)])
+def test_gemm_nan_blocks_and_zeros(M, N, K):
+    """A NaN block spoils its row (of A) or column (of B) and nothing else; a row of zeros gives zeros."""
+    (a, va), (b, vb) = _packed(M, K, 5), _packed(N, K, 6)
+    a[0][0] = 0
+    va[0] = 0
+    a[1][M - 1, (K - 1) // 32] = 255
+    b[1][5, 1] = 255
+    got = _gemm(a, b, M, N, K, "f32")
+    assert bool(torch.isnan(got[M - 1]).all()) and bool(torch.isnan(got[:, 5]).all())
+    rows, cols = list(range(M - 1)), [j for j in range(N) if j != 5]
+    assert not got[0, cols].any()
+    _check_gemm(got[rows][:, cols], va[rows], vb[cols], "f32")
+
+
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_glu(M, N, K):
+    act = ("silu", "gelu", "gelu_tanh")[(M + N + K) % 3]
+    out = "f32" if M % 3 == 0 else "bf16"
+    (x, vx), (g, vg), (u, vu) = _packed(M, K, 7), _packed(N, K, 8, K ** -0.5), _packed(N, K, 9, K ** -0.5)
+    pad = 8 * (M % 2)
+    p = ffn.mx4_problem(M, N, K, out_dtype=out, act=act, ldc=N + pad if pad else 0)
+    h = torch.full((M, N + pad), 7.0, dtype=TORCH[out], device=DEV)
+    ffn.flux_mx4_glu(p, *x, *g, *u, h, _workspace(ffn.FLUX_MX4_GLU, p))
+    torch.cuda.synchronize()
+    assert bool((h[:, N:] == 7.0).all())
+    ref, gg, uu = oo.glu(act, vx, vg.T, vu.T)
+    eg, eu = (K * 2.0 ** -23 * (np.abs(vx) @ np.abs(w).T) for w in (vg, vu))
+    bound = (ROUND[out] + 2.0 ** -19) * np.abs(ref) + 1.01 * (SLOPE * eg * np.abs(uu) + np.abs(oo.act(act, gg)) * eu + SLOPE * eg * eu) + 1e-30
+    err = np.abs(_np(h[:, :N]) - ref)
+    assert (err <= bound).all(), f"off by {np.max(err / bound):.3g} of its bound"
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 512, 4096), (64, 512, 4096), (200, 256, 4096), (300, 512, 512)])
+def test_same_bits_again_on_another_stream_and_in_a_graph(M, N, K):
+    (a, _), (b, _), (u, _) = _packed(M, K, 10), _packed(N, K, 11, 0.02), _packed(N, K, 12, 0.02)
+    p = ffn.mx4_problem(M, N, K)
+    wg, wh = _workspace(ffn.FLUX_MX4_GEMM, p), _workspace(ffn.FLUX_MX4_GLU, p)
+    c, h = (torch.empty(M, N, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    q, s = torch.empty(M, ffn.flux_mx4_row_bytes(N), dtype=torch.uint8, device=DEV), torch.empty(M, ffn.flux_mx4_scale_row_bytes(N), dtype=torch.uint8, device=DEV)
+
+    def all_of_it(stream=None):
+        ffn.flux_mx4_gemm(p, *a, *b, c, wg, stream)
+        ffn.flux_mx4_glu(p, *a, *b, *u, h, wh, stream)
+        ffn.flux_mx4_quantize(h, q, s, stream)
+
+    outs = (c, h, q, s)
+    all_of_it()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        all_of_it()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_of_it(torch.cuda.current_stream())
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want))
+        all_of_it()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want))
