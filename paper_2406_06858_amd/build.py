@@ -13,7 +13,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libflux_mi355.so")
 FFN_LIB = os.path.join(PKG, "libflux_ffn_mi355.so")
 N_CFGS = 10
-FFN_UNITS = ["flux_ffn_api", "flux_mx4"]      # sources of the second library
+FFN_KINDS = 7      # products that the second library's tile kernel is built for
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -33,6 +33,13 @@ def _run(cmd):
     return err
 
 
+def ffn_units():
+    """(source, object, further flags) of the second library."""
+    units = [(os.path.join(CSRC, "flux_ffn_tile.hip"), os.path.join(OBJ, f"flux_ffn_tile{k}.o"), [f"-DFLUX_FFN_KIND={k}"])
+             for k in range(FFN_KINDS)]
+    return units + [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), []) for name in ("flux_ffn_api", "flux_mx4")]
+
+
 def build(verbose: bool = False, jobs: int | None = None) -> str:
     os.makedirs(OBJ, exist_ok=True)
     units = [(os.path.join(CSRC, "flux_api.hip"), os.path.join(OBJ, "flux_api.o"), [])]
@@ -40,7 +47,7 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
         for nk in (0, 1):
             units.append((os.path.join(CSRC, "flux_gemm_inst.hip"), os.path.join(OBJ, f"flux_gemm_cfg{i}_nk{nk}.o"),
                           [f"-DFLUX_CFG_ID={i}", f"-DFLUX_B_NK={nk}"]))
-    ffn = [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), []) for name in FFN_UNITS]
+    ffn = ffn_units()
     units += ffn
     jobs = jobs or min(8, os.cpu_count() or 1, len(units))
 

@@ -4,9 +4,6 @@
 
 namespace flux_ffn {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-
 static thread_local int g_last_hip_error = 0;
 int hip_failed(hipError_t e) {
   g_last_hip_error = (int)e;
@@ -14,88 +11,19 @@ int hip_failed(hipError_t e) {
 }
 
 // ---- kernels -------------------------------------------------------------------------------------------------
-// An operand of a product as a matrix of `rows` rows by k: element (r, k) of segment s at ptr[s][r * step_r + k * step_k], zero
-// outside rows x K.
-struct Operand {
-  const __bf16* ptr[2];
-  long long step_r, step_k;
-  int rows, K;
-  const uint8_t* scales[2];             // not null: ptr holds 4-bit blocks, rows of row_bytes and scale_row_bytes
-  long long row_bytes, scale_row_bytes;
-};
-
-__device__ __forceinline__ __bf16 element(const Operand& o, int seg, int r, int k) {
-  if (r >= o.rows || k >= o.K) return (__bf16)0.f;
-  if (o.scales[0] == nullptr) return o.ptr[seg][r * o.step_r + k * o.step_k];
-  const uint32_t byte = reinterpret_cast<const uint8_t*>(o.ptr[seg])[r * o.row_bytes + k / 2];
-  const uint32_t code = k & 1 ? byte >> 4 : byte & 15u, m = code & 7u, e = o.scales[seg][r * o.scale_row_bytes + k / 32];
-  const float a = m < 2u ? 0.5f * (float)m : __uint_as_float((126u << 23) + (m << 22));
-  const float scale = e == 255u ? __uint_as_float(0x7fc00000u) : e ? __uint_as_float(e << 23) : 0x1p-127f;
-  return (__bf16)((code & 8u ? -a : a) * scale);
-}
-
-struct Job {
-  Operand a, b;             // the result's rows and its columns
-  int32_t segs;             // segments of the contraction, or (gated) of b alone
-  int32_t gated;
-  int32_t act, out_f32, accumulate;
-  void* out;
-  __bf16 *g, *u;
-  long long ld;
-};
-
-__device__ __forceinline__ float act_of(int which, float g) {
-  return which == FLUX_ACT_SILU ? act<FLUX_ACT_SILU>(g) : which == FLUX_ACT_GELU ? act<FLUX_ACT_GELU>(g) : act<FLUX_ACT_GELU_TANH>(g);
-}
-
-// 64x64 of the result per workgroup, four waves of 32x32, slabs of 32 of k through LDS.
-__global__ void __launch_bounds__(256) simple_kernel(const Job j) {
-  __shared__ __bf16 la[64][40], lb[2][64][40];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  f32x4 acc[2][2][2] = {};
-  for (int seg = 0; seg < (j.gated ? 1 : j.segs); ++seg)
-    for (int k0 = 0; k0 < j.a.K; k0 += 32) {
-      for (int i = tid; i < 64 * 32; i += 256) {
-        const bool along_k = j.a.step_k == 1, b_along_k = j.b.step_k == 1;
-        const int ra = along_k ? i / 32 : i % 64, ka = along_k ? i % 32 : i / 64;
-        const int rb = b_along_k ? i / 32 : i % 64, kb = b_along_k ? i % 32 : i / 64;
-        la[ra][ka] = element(j.a, seg, m0 + ra, k0 + ka);
-        lb[0][rb][kb] = element(j.b, seg, n0 + rb, k0 + kb);
-        if (j.gated) lb[1][rb][kb] = element(j.b, 1, n0 + rb, k0 + kb);
-      }
-      __syncthreads();
-      for (int h = 0; h < (j.gated ? 2 : 1); ++h)
-        for (int mi = 0; mi < 2; ++mi)
-          for (int ni = 0; ni < 2; ++ni) {
-            bf16x8 x, y;
-            for (int e = 0; e < 8; ++e) {
-              x[e] = la[wm * 32 + mi * 16 + (lane & 15)][(lane >> 4) * 8 + e];
-              y[e] = lb[h][wn * 32 + ni * 16 + (lane & 15)][(lane >> 4) * 8 + e];
-            }
-            acc[h][mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc[h][mi][ni], 0, 0, 0);
-          }
-      __syncthreads();
-    }
-  for (int mi = 0; mi < 2; ++mi)
-    for (int ni = 0; ni < 2; ++ni)
-      for (int e = 0; e < 4; ++e) {
-        const int m = m0 + wm * 32 + mi * 16 + 4 * (lane >> 4) + e, n = n0 + wn * 32 + ni * 16 + (lane & 15);
-        if (m >= j.a.rows || n >= j.b.rows) continue;
-        float v = acc[0][mi][ni][e];
-        if (j.gated) {
-          const float u = acc[1][mi][ni][e];
-          if (j.g) { j.g[m * j.ld + n] = (__bf16)v; j.u[m * j.ld + n] = (__bf16)u; }
-          v = act_of(j.act, v) * u;
-        }
-        if (j.out_f32) {
-          float* p = static_cast<float*>(j.out) + m * j.ld + n;
-          *p = j.accumulate ? *p + v : v;
-        } else {
-          __bf16* p = static_cast<__bf16*>(j.out) + m * j.ld + n;
-          *p = (__bf16)(j.accumulate ? (float)*p + v : v);
-        }
-      }
+// The parts of a contraction that was cut over workgroups, added in ascending order, and the end of the product.
+template <int HALVES>
+__global__ void __launch_bounds__(256) join_kernel(const TileArgs t) {
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+  const int row = (int)(i / t.cols), col = (int)(i % t.cols);            // (cols % 8 == 0)
+  if (row >= t.rows) return;
+  const long long pitch = (long long)HALVES * t.cols, each = t.rows * pitch, at = row * pitch + col;
+  float v[8] = {}, u[8] = {};
+  for (int p = 0; p < t.parts; ++p) {
+    add8(t.partial, true, p * each + at, v);
+    if (HALVES == 2) add8(t.partial, true, p * each + at + t.cols, u);
+  }
+  finish8<HALVES>(t, 0, row, col, v, u);
 }
 
 // dG = dH U act'(G), dU = dH act(G), rounded to bf16 once: the operands of the three products.
@@ -126,7 +54,6 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs s) {
 }
 
 // ---- checks --------------------------------------------------------------------------------------------------
-constexpr size_t WS_HEADER = 0;
 constexpr long long LIMIT = 1ll << 31;
 
 static long long pitch_x(const flux_glu_t* p) { return p->ldx ? p->ldx : p->K; }
@@ -159,8 +86,63 @@ static int validate(int op, const flux_mx4_t* p) {
   return FLUX_OK;
 }
 
+// ---- how a product is run --------------------------------------------------------------------------------------
+struct Plan {
+  int shape = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0, jobs = 1;
+  bool edge = false;
+  size_t partial_bytes = 0;
+};
+
+static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
+static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// depth: pieces of two bytes of (a segment of) the contraction.
+static Plan plan_tiles(int kind, int rows, int cols, int depth) {
+  const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
+  const int slabs = segs * ceil_div(depth, 64);
+  Plan best;
+  double best_us = 0;
+  for (int i = 0; i < N_SHAPES; ++i) {
+    const Shape& sh = SHAPES[i];
+    const int sub = sh.bn / halves, tm = ceil_div(rows, sh.bm), tn = ceil_div(cols, sub);
+    const long long tiles = (long long)tm * tn * jobs, at_once = 256 * sh.per_unit;
+    for (int parts = 1; parts <= 16; ++parts) {
+      int each = ceil_div(slabs, parts);
+      if (kind >= MX_GEMM) each += each % 2;                    // (scales come for two slabs)
+      if (parts > 1 && (kind == DW || each < 4 || (long long)each * (parts - 1) >= slabs)) continue;
+      const double slab_us = i == 0 ? 1.4 : 1.0, ends_us = i == 0 ? 7.0 : 4.0;
+      double us = (double)ceil_div(tiles * parts, at_once) * (each * slab_us + ends_us);
+      if (parts > 1) us += 4.0 + 8.0 * parts * halves * (double)rows * cols / 4e6;
+      if (best.slabs == 0 || us < best_us) {
+        best_us = us;
+        best.shape = i;
+        best.parts = parts;
+        best.part_slabs = each;
+        best.slabs = slabs;
+        best.tiles_m = tm;
+        best.tiles_n = tn;
+        best.jobs = jobs;
+        best.edge = rows % sh.bm != 0 || cols % sub != 0 || depth % 64 != 0;
+        best.partial_bytes = parts > 1 ? (size_t)parts * halves * rows * cols * 4 : 0;
+      }
+    }
+  }
+  return best;
+}
+
+static Plan plan_glu(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N, p->K); }
+static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N); }
+static Plan plan_dw(const flux_glu_t* p) { return p->w_is_nk ? plan_tiles(DW, p->N, p->K, p->M) : plan_tiles(DW, p->K, p->N, p->M); }
+static Plan plan_mx4(int op, const flux_mx4_t* p) {
+  return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2));
+}
+
+// Rows of dG and of dU in the workspace start at multiples of 16 bytes (N % 8 == 0).
+static size_t slope_bytes(const flux_glu_t* p) { return 4ull * p->M * p->N; }
+
 static size_t glu_need(int op, const flux_glu_t* p) {
-  return op == FLUX_GLU_BACKWARD ? WS_HEADER + 4ull * p->M * p->N : 0;
+  if (op == FLUX_GLU_FORWARD) return plan_glu(p).partial_bytes;
+  return (slope_bytes(p) + 255) / 256 * 256 + plan_dx(p).partial_bytes;
 }
 
 static int workspace_ok(size_t need, const void* ws, size_t bytes) {
@@ -169,18 +151,29 @@ static int workspace_ok(size_t need, const void* ws, size_t bytes) {
 }
 
 // ---- dispatch ------------------------------------------------------------------------------------------------
-static int launch(const Job& j, hipStream_t s) {
-  hipLaunchKernelGGL(simple_kernel, dim3((j.b.rows + 63) / 64, (j.a.rows + 63) / 64), dim3(256), 0, s, j);
-  FFN_HIP(hipGetLastError());
-  return FLUX_OK;
-}
+static uint32_t extent(long long rows, long long pitch, long long row) { return (uint32_t)((rows - 1) * pitch + row); }
 
-static Operand plain(const void* p0, const void* p1, long long step_r, long long step_k, int rows, int K) {
-  return Operand{{static_cast<const __bf16*>(p0), static_cast<const __bf16*>(p1)}, step_r, step_k, rows, K, {nullptr, nullptr}, 0, 0};
-}
-static Operand blocks(const void* q0, const void* s0, const void* q1, const void* s1, int rows, int K) {
-  return Operand{{static_cast<const __bf16*>(q0), static_cast<const __bf16*>(q1)}, 0, 1, rows, K,
-                 {static_cast<const uint8_t*>(s0), static_cast<const uint8_t*>(s1)}, row_bytes(K), scale_row_bytes(K)};
+static int launch(int kind, const Plan& pl, TileArgs& t, void* partial, hipStream_t s) {
+  typedef hipError_t (*Launcher)(int, const TileArgs&, bool, int, hipStream_t);
+  static constexpr Launcher launchers[KINDS] = {launch_tile0, launch_tile1, launch_tile2, launch_tile3, launch_tile4, launch_tile5, launch_tile6};
+  t.slabs = pl.slabs;
+  t.seg_slabs = (t.depth + 63) / 64;
+  t.parts = pl.parts;
+  t.part_slabs = pl.part_slabs;
+  t.tiles_m = pl.tiles_m;
+  t.tiles_n = pl.tiles_n;
+  t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
+  t.partial = static_cast<float*>(partial);
+  const long long grid = (long long)pl.tiles_m * pl.tiles_n * pl.jobs * pl.parts;
+  if (grid >= (1ll << 31)) return FLUX_ERR_SHAPE;
+  FFN_HIP(launchers[kind](pl.shape, t, pl.edge, (int)grid, s));
+  if (pl.parts > 1) {
+    const dim3 join((unsigned)(((long long)t.rows * t.cols / 8 + 255) / 256));
+    if (halves_of(kind) == 2) hipLaunchKernelGGL(join_kernel<2>, join, dim3(256), 0, s, t);
+    else hipLaunchKernelGGL(join_kernel<1>, join, dim3(256), 0, s, t);
+    FFN_HIP(hipGetLastError());
+  }
+  return FLUX_OK;
 }
 
 static int mx4(int op, const flux_mx4_t* p, const void* Aq, const void* As, const void* B0, const void* S0, const void* B1, const void* S1,
@@ -191,16 +184,25 @@ static int mx4(int op, const flux_mx4_t* p, const void* Aq, const void* As, cons
     if (x == nullptr || !aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
   st = workspace_ok(flux_mx4_workspace_bytes(op, p), ws, bytes);
   if (st != FLUX_OK) return st;
-  Job j = {};
-  j.a = blocks(Aq, As, Aq, As, p->M, p->K);
-  j.b = blocks(B0, S0, B1, S1, p->N, p->K);
-  j.segs = 1;
-  j.gated = op == FLUX_MX4_GLU;
-  j.act = p->act;
-  j.out_f32 = p->out_dtype == FLUX_F32;
-  j.out = out;
-  j.ld = p->ldc ? p->ldc : p->N;
-  return launch(j, static_cast<hipStream_t>(stream));
+  TileArgs t = {};
+  t.a[0] = Aq;
+  t.b[0] = B0;
+  t.b[1] = B1;
+  t.sa = static_cast<const uint8_t*>(As);
+  t.sb[0] = static_cast<const uint8_t*>(S0);
+  t.sb[1] = static_cast<const uint8_t*>(S1);
+  t.pitch_a = t.pitch_b = (uint32_t)row_bytes(p->K);
+  t.pitch_s = (uint32_t)scale_row_bytes(p->K);
+  t.bytes_a = (uint32_t)p->M * t.pitch_a;
+  t.bytes_b = (uint32_t)p->N * t.pitch_b;
+  t.rows = p->M;
+  t.cols = p->N;
+  t.depth = (int)(t.pitch_a / 2);
+  t.act = p->act;
+  t.out_f32 = p->out_dtype == FLUX_F32;
+  t.ld = p->ldc ? p->ldc : p->N;
+  t.out[0] = out;
+  return launch(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, plan_mx4(op, p), t, ws, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace flux_ffn
@@ -213,10 +215,7 @@ int flux_ffn_last_hip_error(void) { return g_last_hip_error; }
 
 size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p) { return validate(op, p) == FLUX_OK ? glu_need(op, p) : 0; }
 
-size_t flux_mx4_workspace_bytes(int op, const flux_mx4_t* p) {
-  (void)op; (void)p;
-  return 0;
-}
+size_t flux_mx4_workspace_bytes(int op, const flux_mx4_t* p) { return validate(op, p) == FLUX_OK ? plan_mx4(op, p).partial_bytes : 0; }
 
 int flux_ffn_init(void* workspace, size_t workspace_bytes, void* stream) {
   if (workspace == nullptr && workspace_bytes != 0) return FLUX_ERR_INVALID_ARG;
@@ -233,18 +232,25 @@ int flux_glu(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu,
   if ((G == nullptr) != (U == nullptr) || !aligned(G, 16) || !aligned(U, 16)) return FLUX_ERR_INVALID_ARG;
   st = workspace_ok(glu_need(FLUX_GLU_FORWARD, p), workspace, workspace_bytes);
   if (st != FLUX_OK) return st;
-  Job j = {};
-  j.a = plain(X, X, pitch_x(p), 1, p->M, p->K);
-  j.b = p->w_is_nk ? plain(Wg, Wu, pitch_w(p), 1, p->N, p->K) : plain(Wg, Wu, 1, pitch_w(p), p->N, p->K);
-  j.segs = 1;
-  j.gated = 1;
-  j.act = p->act;
-  j.out_f32 = p->out_dtype == FLUX_F32;
-  j.out = H;
-  j.g = static_cast<__bf16*>(G);
-  j.u = static_cast<__bf16*>(U);
-  j.ld = pitch_h(p);
-  return launch(j, static_cast<hipStream_t>(stream));
+  TileArgs t = {};
+  t.a[0] = X;
+  t.b[0] = Wg;
+  t.b[1] = Wu;
+  const long long lx = pitch_x(p), lw = pitch_w(p);
+  t.pitch_a = (uint32_t)(lx * 2);
+  t.pitch_b = (uint32_t)(lw * 2);
+  t.bytes_a = extent(p->M, lx * 2, p->K * 2ll);
+  t.bytes_b = p->w_is_nk ? extent(p->N, lw * 2, p->K * 2ll) : extent(p->K, lw * 2, p->N * 2ll);
+  t.rows = p->M;
+  t.cols = p->N;
+  t.depth = p->K;
+  t.act = p->act;
+  t.out_f32 = p->out_dtype == FLUX_F32;
+  t.ld = pitch_h(p);
+  t.out[0] = H;
+  t.g = static_cast<__bf16*>(G);
+  t.u = static_cast<__bf16*>(U);
+  return launch(p->w_is_nk ? GLU_NK : GLU_KN, plan_glu(p), t, workspace, static_cast<hipStream_t>(stream));
 }
 
 int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu, const void* G, const void* U,
@@ -262,7 +268,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   d.G = static_cast<const __bf16*>(G);
   d.U = static_cast<const __bf16*>(U);
   d.dH = static_cast<const __bf16*>(dH);
-  d.dG = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + WS_HEADER);
+  d.dG = static_cast<__bf16*>(workspace);
   d.dU = d.dG + (long long)p->M * p->N;
   d.ldh = pitch_h(p);
   d.ldd = p->N;
@@ -273,29 +279,49 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   else if (p->act == FLUX_ACT_GELU) hipLaunchKernelGGL(slope_kernel<FLUX_ACT_GELU>, grid, dim3(256), 0, s, d);
   else hipLaunchKernelGGL(slope_kernel<FLUX_ACT_GELU_TANH>, grid, dim3(256), 0, s, d);
   FFN_HIP(hipGetLastError());
-  const long long lw = pitch_w(p), lx = pitch_x(p), n = p->N;
+  const long long lw = pitch_w(p), lx = pitch_x(p);
+  const uint32_t bytes_w = p->w_is_nk ? extent(p->N, lw * 2, p->K * 2ll) : extent(p->K, lw * 2, p->N * 2ll);
+  const uint32_t bytes_d = (uint32_t)((long long)p->M * p->N * 2), bytes_x = extent(p->M, lx * 2, p->K * 2ll);
   if (dX != nullptr) {
-    Job j = {};
-    j.a = plain(d.dG, d.dU, n, 1, p->M, p->N);
-    j.b = p->w_is_nk ? plain(Wg, Wu, 1, lw, p->K, p->N) : plain(Wg, Wu, lw, 1, p->K, p->N);
-    j.segs = 2;
-    j.out_f32 = p->out_dtype == FLUX_F32;
-    j.out = dX;
-    j.ld = lx;
-    st = launch(j, s);
+    TileArgs t = {};
+    t.a[0] = d.dG;
+    t.a[1] = d.dU;
+    t.b[0] = Wg;
+    t.b[1] = Wu;
+    t.pitch_a = (uint32_t)p->N * 2u;
+    t.pitch_b = (uint32_t)(lw * 2);
+    t.bytes_a = bytes_d;
+    t.bytes_b = bytes_w;
+    t.rows = p->M;
+    t.cols = p->K;
+    t.depth = p->N;
+    t.out_f32 = p->out_dtype == FLUX_F32;
+    t.ld = lx;
+    t.out[0] = dX;
+    st = launch(p->w_is_nk ? DX_KN : DX_NK, plan_dx(p), t, static_cast<char*>(workspace) + (slope_bytes(p) + 255) / 256 * 256, s);
     if (st != FLUX_OK) return st;
   }
-  for (int h = 0; h < 2 && dWg != nullptr; ++h) {
-    const Operand x = plain(X, X, 1, lx, p->K, p->M), y = plain(h ? d.dU : d.dG, d.dG, 1, n, p->N, p->M);
-    Job j = {};
-    j.a = p->w_is_nk ? y : x;
-    j.b = p->w_is_nk ? x : y;
-    j.segs = 1;
-    j.out_f32 = p->dw_dtype == FLUX_F32;
-    j.accumulate = p->dw_accumulate;
-    j.out = h ? dWu : dWg;
-    j.ld = lw;
-    st = launch(j, s);
+  if (dWg != nullptr) {
+    TileArgs t = {};
+    const void* const dgu[2] = {d.dG, d.dU};
+    for (int h = 0; h < 2; ++h) {
+      t.a[h] = p->w_is_nk ? dgu[h] : X;
+      t.b[h] = p->w_is_nk ? X : dgu[h];
+    }
+    const uint32_t pitch_d = (uint32_t)p->N * 2u, pitch = (uint32_t)(lx * 2);
+    t.pitch_a = p->w_is_nk ? pitch_d : pitch;
+    t.pitch_b = p->w_is_nk ? pitch : pitch_d;
+    t.bytes_a = p->w_is_nk ? bytes_d : bytes_x;
+    t.bytes_b = p->w_is_nk ? bytes_x : bytes_d;
+    t.rows = p->w_is_nk ? p->N : p->K;
+    t.cols = p->w_is_nk ? p->K : p->N;
+    t.depth = p->M;
+    t.out_f32 = p->dw_dtype == FLUX_F32;
+    t.accumulate = p->dw_accumulate;
+    t.ld = lw;
+    t.out[0] = dWg;
+    t.out[1] = dWu;
+    st = launch(DW, plan_dw(p), t, nullptr, s);
     if (st != FLUX_OK) return st;
   }
   return FLUX_OK;

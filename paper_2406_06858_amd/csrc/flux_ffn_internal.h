@@ -2,8 +2,24 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include "flux_ffn.h"
+#include "flux_ffn_tile.h"
 
 namespace flux_ffn {
+
+// Tiles of the tile kernel: rows, columns of products, workgroups per compute unit.
+struct Shape { int bm, bn, per_unit; };
+constexpr Shape SHAPES[] = {{256, 256, 1}, {128, 128, 2}};
+constexpr int N_SHAPES = 2;
+
+#define FFN_DECLARE(KIND) hipError_t launch_tile##KIND(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s);
+FFN_DECLARE(0)
+FFN_DECLARE(1)
+FFN_DECLARE(2)
+FFN_DECLARE(3)
+FFN_DECLARE(4)
+FFN_DECLARE(5)
+FFN_DECLARE(6)
+#undef FFN_DECLARE
 
 // Remembers a failed runtime call for flux_ffn_last_hip_error and returns the status for it.
 int hip_failed(hipError_t e);

@@ -1,0 +1,537 @@
+// The tile kernel of the gated block's products (gfx950): one main loop for bf16 operands in any order and for 4-bit
+// blocks.
+//
+// A tile is BM rows by BN columns of products, four waves of BM/2 x BN/2, a slab of contraction 128 bytes a row.  The
+// schedule is the one of the library's fused GEMMs (MmaPipe in flux_device.h): slabs go from memory into LDS directly,
+// fragments of the next k-step are read and loads of the slab after next are issued between the MFMAs of this one, and a
+// slab costs one barrier.  What differs by product:
+//
+//   gated    the columns of a wave are half gate, half up, of the SAME columns of the result: activation and product take
+//            both from the wave's own accumulators, and A is read once for two weights.
+//   dX       the contraction runs over dG Wg^T and then dU Wu^T: one accumulator, two segments of slabs.
+//   dW       both operands hold the contraction (tokens) along their rows' index: both tiles lie in LDS as they do in memory
+//            and both fragments are read transposing.  The gradients of both weights are one grid.
+//   4 bits   a slab's 128 bytes are 256 numbers, a k-step's MFMA is 16x16x128 with one scale per lane and operand: a lane
+//            holds one block of 32.  Same bytes, same fragment reads and same cycles per slab as bf16, four times the numbers.
+#pragma once
+#include "flux_device.h"
+#include "flux_ffn_act.h"
+
+namespace flux_ffn {
+
+using flux::bf16x8;
+using flux::f32x4;
+using flux::FragHalves;
+using flux::u32x2;
+using flux::u32x4;
+
+enum Kind : int { GLU_NK = 0, GLU_KN = 1, DX_NK = 2, DX_KN = 3, DW = 4, MX_GEMM = 5, MX_GLU = 6, KINDS = 7 };
+
+struct TileArgs {
+  const void* a[2];              // dX: by segment; dW: by weight; else [0]
+  const void* b[2];              // gated: gate, up; dX: by segment; dW: by weight; else [0]
+  const uint8_t* sa;             // 4 bits: scales of A; of B
+  const uint8_t* sb[2];
+  uint32_t pitch_a, pitch_b;     // bytes
+  uint32_t bytes_a, bytes_b;     // extents
+  uint32_t pitch_s;              // of a row of scales
+  int32_t rows, cols;            // of the result
+  int32_t depth;                 // of the contraction (of a segment of it), in pieces of two bytes
+  int32_t seg_slabs, slabs;      // slabs of a segment; of the whole contraction
+  int32_t parts, part_slabs;     // the contraction cut over workgroups: parts of part_slabs slabs each
+  int32_t tiles_m, tiles_n, band;
+  int32_t act, out_f32, accumulate;
+  int64_t ld;                    // pitch of the results, elements
+  void* out[2];                  // dW: by weight; else [0]
+  __bf16 *g, *u;                 // gated: kept for the backward pass, or null
+  float* partial;                // parts > 1: [parts][rows][halves * cols]
+};
+
+template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_>
+struct Cfg {
+  static constexpr int KIND = KIND_, BM = BM_, BN = BN_, NA = NA_, NB = NB_, OCC = OCC_;
+  static constexpr bool EDGE = EDGE_;                                        // the tile does not divide the product
+  static constexpr bool MX = KIND == MX_GEMM || KIND == MX_GLU, A_T = KIND == DW;
+  static constexpr bool B_NK = MX || KIND == GLU_NK || KIND == DX_NK;
+  static constexpr int HALVES = KIND == GLU_NK || KIND == GLU_KN || KIND == MX_GLU ? 2 : 1;
+  static constexpr int NT = 256, BK = 64;
+  static constexpr int WTM = BM / 2, WTN = BN / 2, MI = WTM / 16, NI = WTN / 16, NIH = NI / HALVES;
+  static constexpr int SUBN = BN / HALVES;                                   // columns of the result
+  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, SUB_BYTES = B_BYTES / HALVES;
+  static constexpr int RING_BYTES = NA * A_BYTES + NB * B_BYTES;
+  static constexpr int SC_BYTES = 256 * 16;                                  // scales of one operand, two slabs
+  static constexpr int EP_STRIDE = WTN + 8;
+  static constexpr int EP_BYTES = 4 * 32 * EP_STRIDE * 4;
+  static constexpr int LOOP_BYTES = RING_BYTES + (MX ? 4 * SC_BYTES : 0);
+  static constexpr int POOL_BYTES = LOOP_BYTES > EP_BYTES ? LOOP_BYTES : EP_BYTES;
+  static_assert(POOL_BYTES * OCC <= 160 * 1024, "LDS");
+  static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || (NA == 2 && NB == 2)), "rings");
+};
+
+// Which 16-byte slot of a row holds slot s: s ^ swizzle(row).  A fragment's lanes are rows 0..15 of slot q, the next sixteen
+// the same rows of the next slot that the k-step reads; an LDS read is answered in passes of sixteen lanes that hold every
+// row once, half of them of the one slot and half of the next (see swz_a).  bf16: the next slot is q + 1, and bits 0..2 of the
+// row serve.  4 bits: it is q + 2 (a lane reads blocks 2g and 2g + 1 of a slab, so that both their scales are two bytes side
+// by side), so bits 0 and 1 change places.
+template <bool MX>
+__device__ __forceinline__ int swizzle(int row) {
+  return MX ? (row & 4) | ((row & 1) << 1) | ((row >> 1) & 1) : row & 7;
+}
+
+// The scaled MFMA, accumulator in place; BYTE: which byte of the scale registers counts.
+template <int BYTE>
+__device__ __forceinline__ void mfma_scaled(f32x4& acc, const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb) {
+  if constexpr (BYTE == 0)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(acc) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  else
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(acc) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+
+// ---- operand loads ---------------------------------------------------------------------------------------------
+// One operand tile of R rows (or columns) of the result by 128 bytes of contraction, in LDS in one of two ways:
+//   along   rows of 128 bytes, one instruction 8 rows;
+//   across  (T) one row per step of the contraction, R values each, one instruction 512 / R of those.
+// (The same patterns as DmaLoader's.)  A lane outside the matrix loads from outside the buffer's records: zeros.
+template <int R, bool T, bool EDGE, bool MX>
+struct OperandLoader {
+  static constexpr int RPI = T ? 512 / R : 8;
+  static constexpr int INSTR = (T ? 64 : R) / RPI / 4;         // per wave
+  static constexpr int SLOTS = R / 8;
+  static constexpr uint32_t OUTSIDE = 0xfffffff0u;
+  static constexpr __device__ int wave_row(int wave) {
+    return RPI == 8 ? 8 * wave : RPI == 4 ? 8 * (wave & 1) + 4 * (wave >> 1) : 2 * (wave & 1) + 8 * (wave >> 1);
+  }
+  static constexpr __device__ int instr_row(int p) { return RPI == 8 ? p * 32 : RPI == 4 ? 16 * p : 4 * (p & 1) + 16 * (p >> 1); }
+  static_assert(RPI == 2 || RPI == 4 || RPI == 8, "the swizzle must not depend on the instruction");
+
+  uint32_t voff, pitch, lds_wave;
+  int lim, k_vec;                  // along: loads that have a row, the lane's place in the contraction; across: k_vec alone
+  __device__ __forceinline__ void init(uint32_t pitch_, int rows, int r0, int wave, int lane) {
+    pitch = pitch_;
+    lds_wave = (uint32_t)(wave_row(wave) * (1024 / RPI));
+    if constexpr (T) {
+      const int k = wave_row(wave) + lane / SLOTS, s = lane % SLOTS ^ flux::swz_b<SLOTS>(wave_row(wave) + lane / SLOTS);
+      voff = (uint32_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
+      if (EDGE) k_vec = r0 + s * 8 < rows ? k : 0x40000000;
+    } else {
+      const int row = 8 * wave + lane / 8, s = lane % 8 ^ swizzle<MX>(row);
+      voff = (uint32_t)(r0 + row) * pitch + (uint32_t)s * 16u;
+      if (EDGE) {
+        k_vec = s * 8;
+        lim = (rows - r0 - row + 31) / 32;
+      }
+    }
+  }
+  // the d-th of the wave's loads of the slab that starts at k (`depth` in all) into `tile`
+  __device__ __forceinline__ void load(int d, const __amdgpu_buffer_rsrc_t& rsrc, int k, int depth, unsigned char* tile) const {
+    const bool in = !EDGE || (T ? k_vec < depth - k - instr_row(d) : d < (k_vec < depth - k ? lim : 0));
+    const uint32_t from = T ? (uint32_t)(k + instr_row(d)) * pitch : (uint32_t)k * 2u + (uint32_t)instr_row(d) * pitch;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(tile + instr_row(d) * (1024 / RPI) + lds_wave), 16,
+                                             (int)(in ? voff : OUTSIDE), (int)from, 0, 0);
+  }
+};
+
+// A slab to ask for: where it lies, or nothing in the place of one past the end (its loads touch no memory).
+struct Slab {
+  __amdgpu_buffer_rsrc_t r0, r1;
+  int k;
+};
+
+template <class C>
+struct Pipe {
+  typedef OperandLoader<C::BM, C::A_T, C::EDGE, C::MX> LdA;
+  typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX> LdB;
+  static constexpr int NA = C::NA, NB = C::NB;
+  static constexpr bool A_LEADS = NA > NB;                               // by one slab
+  static constexpr int U = C::MX ? 4 : NA == NB ? NB : NA * NB;          // slabs after which all rings are where they were
+  static constexpr int KS = 2;
+  static constexpr int G = C::MI * C::NI;                                // MFMAs per k-step
+  static constexpr int NF = C::MI + C::NI, NS = C::MX ? NF : 0;          // fragments of a k-step; scales of a slab
+  static constexpr int LA = LdA::INSTR, LB = LdB::INSTR * C::HALVES, LS = C::MX ? 1 : 0, L = LA + LB + LS;
+  static constexpr int LX = A_LEADS ? LA : 0;
+  static constexpr int A_HI = (NA * C::A_BYTES + 65535) / 65536, B_HI = (NB * C::B_BYTES + 65535) / 65536;
+  static constexpr int NAV = C::A_T ? C::MI : KS, NBV = C::B_NK ? KS : C::NIH;
+  // Placement in MFMAs, as MmaPipe's: the barrier, the last fragment read of a k-step, the last load from the barrier on.
+  static constexpr int BAR_AT = G / 8, SPREAD = (G * 15 + 15) / 16, SPAN = G * (NA != NB ? 13 : 11) / 8;
+  static constexpr int load_slot(int d) { return BAR_AT + d * (SPAN - BAR_AT) / L; }
+  static constexpr int loads_before(int slot) { int n = 0; while (n < L && load_slot(n) < slot) ++n; return n; }
+  static constexpr int reads_before(int slot, int from, int all) { int n = 0; while (n < all && from + n * (SPREAD - from) / all < slot) ++n; return n; }
+  static constexpr int L0 = loads_before(G);
+
+  typedef std::conditional_t<C::MX, u32x4, bf16x8> Whole;
+  typedef std::conditional_t<C::A_T, FragHalves, Whole> FragA;
+  typedef std::conditional_t<C::B_NK, Whole, FragHalves> FragB;
+
+  unsigned char* pool;
+  LdA la;
+  LdB lb;
+  uint32_t voff_s[2];                // 4 bits: the lane's row of scales of A; of B
+  bool s_in[2];
+  int job, k0, KT, wave;             // first slab of this workgroup's, and how many
+  uint32_t a[A_HI][NAV], b[B_HI][NBV], sc[2];
+  FragA af[2][C::MI];
+  FragB bf[2][C::NI];
+  uint32_t fs[2][C::MX ? C::MI + C::NI : 1];
+
+  __device__ __forceinline__ unsigned char* slab_a(int i) const { return pool + i * C::A_BYTES; }
+  __device__ __forceinline__ unsigned char* slab_b(int i) const { return pool + NA * C::A_BYTES + i * C::B_BYTES; }
+  __device__ __forceinline__ unsigned char* scales(int operand, int pair) const { return pool + C::RING_BYTES + (operand * 2 + pair) * C::SC_BYTES; }
+
+  template <int R>
+  static __device__ __forceinline__ uint32_t across(uint32_t base, int r, int i, int g) {      // transposing read of rows r.. of the result
+    const int k = 8 * g + (i >> 2), n = r + 4 * (i & 3);
+    return base + k * (R * 2) + (((n >> 3) ^ flux::swz_b<R / 8>(k)) << 4) + ((n >> 2) & 1) * 8;
+  }
+  static __device__ __forceinline__ uint32_t along(uint32_t base, int row, int ks, int g) {
+    const int q = C::MX ? 2 * g + ks : ks * 4 + g;
+    return base + row * 128 + ((q ^ swizzle<C::MX>(row)) << 4);
+  }
+
+  __device__ __forceinline__ void init(const TileArgs& t, unsigned char* pool_, int m0, int n0, int wave_, int lane) {
+    pool = pool_;
+    wave = wave_;
+    la.init(t.pitch_a, t.rows, m0, wave, lane);
+    lb.init(t.pitch_b, t.cols, n0, wave, lane);
+    const uint32_t base_a = flux::lds_address(pool), base_b = base_a + NA * C::A_BYTES;
+    const int g = lane >> 4, i = lane & 15, wm = wave >> 1, wn = wave & 1, rb = wn * (C::SUBN / 2);
+#pragma unroll
+    for (int h = 0; h < A_HI; ++h)
+#pragma unroll
+      for (int v = 0; v < NAV; ++v) {
+        if constexpr (C::A_T) a[h][v] = across<C::BM>(base_a + h * 65536u, wm * C::WTM + v * 16, i, g);
+        else a[h][v] = along(base_a + h * 65536u, wm * C::WTM + i, v, g);
+      }
+#pragma unroll
+    for (int h = 0; h < B_HI; ++h)
+#pragma unroll
+      for (int v = 0; v < NBV; ++v) {
+        if constexpr (C::B_NK) b[h][v] = along(base_b + h * 65536u, rb + i, v, g);
+        else b[h][v] = across<C::SUBN>(base_b + h * 65536u, rb + v * 16, i, g);
+      }
+    if constexpr (C::MX) {
+      // wave w fetches 64 rows of each operand, 16 bytes (two slabs) a lane; of a gated B the lower half of the rows is gate's
+      const int row = 64 * wave + lane, half = row / C::SUBN, col = row - half * C::SUBN;
+      voff_s[0] = (uint32_t)(m0 + row) * t.pitch_s;
+      voff_s[1] = (uint32_t)(n0 + col) * t.pitch_s;
+      s_in[0] = row < C::BM && m0 + row < t.rows;
+      s_in[1] = row < C::BN && n0 + col < t.cols;
+      sc[0] = flux::lds_address(scales(0, 0)) + (wm * C::WTM + i) * 16 + 2 * g;
+      sc[1] = flux::lds_address(scales(1, 0)) + (rb + i) * 16 + 2 * g;
+    }
+  }
+
+  template <int OFF>
+  static __device__ __forceinline__ void read(u32x4& f, uint32_t base) { asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f) : "v"(base), "n"(OFF)); }
+  template <int OFF>
+  static __device__ __forceinline__ void read(bf16x8& f, uint32_t base) {
+    u32x4 v;
+    read<OFF>(v, base);
+    f = __builtin_bit_cast(bf16x8, v);
+  }
+  template <int OFF>
+  static __device__ __forceinline__ u32x2 read_tr(uint32_t base) {
+    u32x2 v;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(base), "n"(OFF));
+    return v;
+  }
+  template <int OFF, int ROW_BYTES, int HI, int NV>
+  static __device__ __forceinline__ void read_halves(FragHalves& f, const uint32_t (&base)[HI][NV], int v) {
+    constexpr int UP = OFF + 4 * ROW_BYTES;
+    f.lo = read_tr<OFF % 65536>(base[OFF / 65536][v]);
+    f.hi = read_tr<UP % 65536>(base[UP / 65536][v]);
+  }
+  // fragment R, in the order the MFMAs want them, of k-step K out of A's slab SA / B's slab SB in LDS
+  template <int SA, int SB, int K, int R>
+  __device__ __forceinline__ void fetch() {
+    constexpr bool IS_B = R >= 1 && R <= C::NI;
+    constexpr int I = R == 0 ? 0 : (IS_B ? R - 1 : R - C::NI);
+    if constexpr (!IS_B) {
+      if constexpr (C::A_T) {
+        read_halves<SA * C::A_BYTES + K * 32 * C::BM * 2, C::BM * 2>(af[K][I], a, I);
+      } else {
+        constexpr int OFF = SA * C::A_BYTES + I * 16 * 128;
+        read<OFF % 65536>(af[K][I], a[OFF / 65536][K]);
+      }
+    } else {
+      constexpr int BASE = SB * C::B_BYTES + I / C::NIH * C::SUB_BYTES;
+      if constexpr (C::B_NK) {
+        constexpr int OFF = BASE + I % C::NIH * 16 * 128;
+        read<OFF % 65536>(bf[K][I], b[OFF / 65536][K]);
+      } else {
+        read_halves<BASE + K * 32 * C::SUBN * 2, C::SUBN * 2>(bf[K][I], b, I % C::NIH);
+      }
+    }
+  }
+  // scales of fragment R for slab place S of the unrolled loop (both k-steps) into set S % 2
+  template <int S, int R>
+  __device__ __forceinline__ void fetch_scale() {
+    constexpr int PLACE = S / 2 % 2 * C::SC_BYTES + S % 2 * 8;
+    constexpr int OFF = R < C::MI ? R * 256 : ((R - C::MI) / C::NIH * C::SUBN + (R - C::MI) % C::NIH * 16) * 16;
+    asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(fs[S % 2][R]) : "v"(sc[R < C::MI ? 0 : 1]), "n"(PLACE + OFF));
+  }
+
+  __device__ __forceinline__ Slab slab(const TileArgs& t, bool is_b, int s) const {
+    const bool there = s < KT;
+    int k = k0 + s, seg = job;
+    if constexpr (C::KIND == DX_NK || C::KIND == DX_KN) {
+      seg = k >= t.seg_slabs ? 1 : 0;
+      k -= seg * t.seg_slabs;
+    }
+    const uint32_t bytes = there ? (is_b ? t.bytes_b : t.bytes_a) : 0u;
+    const auto rsrc = [&](const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000); };
+    if (!is_b) return Slab{rsrc(t.a[seg]), rsrc(t.a[seg]), k * C::BK};
+    if constexpr (C::HALVES == 2) return Slab{rsrc(t.b[0]), rsrc(t.b[1]), k * C::BK};
+    return Slab{rsrc(t.b[seg]), rsrc(t.b[seg]), k * C::BK};
+  }
+  __device__ __forceinline__ void load_b(const TileArgs& t, const Slab& w, int d, int place) const {
+    const int half = d / LdB::INSTR;
+    lb.load(d % LdB::INSTR, half ? w.r1 : w.r0, w.k, t.depth, slab_b(place) + half * C::SUB_BYTES);
+  }
+  // 4 bits: the scales of one operand, slabs 2 pair and 2 pair + 1
+  __device__ __forceinline__ void load_scales(const TileArgs& t, int operand, int pair) const {
+    const uint8_t* p = operand == 0 ? t.sa : t.sb[C::HALVES == 2 && 64 * wave >= C::SUBN ? 1 : 0];
+    const int rows = operand == 0 ? t.rows : t.cols;
+    const uint32_t at = (uint32_t)(k0 / 2 + pair) * 16u;
+    const bool there = 2 * pair < KT && at < t.pitch_s;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, there ? (int)((uint32_t)rows * t.pitch_s) : 0, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(scales(operand, pair % 2) + wave * 1024), 16,
+                                             (int)(s_in[operand] ? voff_s[operand] : LdA::OUTSIDE), (int)at, 0, 0);
+  }
+
+  // What step kt (place S of the unrolled loop; -1 ahead of the first) asks for from its barrier on: slab kt + NB, of A one
+  // further where it leads, first the operand that the next barrier needs; and with it scales: of A, for the next two slabs,
+  // beside an odd slab, of B beside an even one.
+  struct Window { Slab a, b; int kt; };
+  __device__ __forceinline__ Window window(const TileArgs& t, int kt) const { return Window{slab(t, false, kt + NA), slab(t, true, kt + NB), kt}; }
+  __device__ __forceinline__ void load(const TileArgs& t, const Window& w, int d, int S) const {
+    if (LS && d == L - 1) {
+      if ((S + NB) % 2 == 1) load_scales(t, 0, (w.kt + NB + 1) / 2);
+      else load_scales(t, 1, (w.kt + NB) / 2);
+      return;
+    }
+    const bool is_a = A_LEADS ? d >= LB : d < LA;
+    if (is_a) la.load(A_LEADS ? d - LB : d, w.a.r0, w.a.k, t.depth, slab_a((S + NA) % NA));
+    else load_b(t, w.b, A_LEADS ? d : d - LA, (S + NB) % NB);
+  }
+
+  __device__ __forceinline__ void start(const TileArgs& t) {
+    if (LS) load_scales(t, 0, 0);
+#pragma unroll
+    for (int j = 0; j < NB - 1; ++j) {
+      const Slab sa = slab(t, false, j), sb = slab(t, true, j);
+#pragma unroll
+      for (int d = 0; d < LA; ++d) la.load(d, sa.r0, sa.k, t.depth, slab_a(j));
+#pragma unroll
+      for (int d = 0; d < LB; ++d) load_b(t, sb, d, j);
+      if (LS) load_scales(t, 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (A_LEADS) {
+      const Slab sa = slab(t, false, NB - 1);
+#pragma unroll
+      for (int d = 0; d < LA; ++d) la.load(d, sa.r0, sa.k, t.depth, slab_a(NB - 1));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const Window w = window(t, -1);
+#pragma unroll
+    for (int d = 0; d < L0; ++d) load(t, w, d, U - 1);
+    flux::wait_vm_at_most<(NB - 2) * L + LX + L0>();
+    flux::barrier_keeping_loads_in_flight();
+    flux::static_for<NF>([&](auto r) { fetch<0, 0, 0, decltype(r)::value>(); });
+    flux::static_for<NS>([&](auto r) { fetch_scale<0, decltype(r)::value>(); });
+    settle_reads(0, 0);
+  }
+
+  static __device__ __forceinline__ void settle(u32x4& f) { asm volatile("" : "+v"(f)); }
+  static __device__ __forceinline__ void settle(bf16x8& f) { flux::frag_settle(f); }
+  static __device__ __forceinline__ void settle(FragHalves& f) { flux::frag_settle(f); }
+  __device__ __forceinline__ void settle_reads(int ks, int scale_set) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) settle(af[ks][i]);
+#pragma unroll
+    for (int i = 0; i < C::NI; ++i) settle(bf[ks][i]);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) asm volatile("" : "+v"(fs[scale_set][i]));
+  }
+
+  template <int S>
+  __device__ __forceinline__ void step(const TileArgs& t, int kt, f32x4 (&acc)[C::MI][C::NI]) {
+    kt = __builtin_amdgcn_readfirstlane(kt);
+    const Window rest = window(t, kt - 1), first = window(t, kt);
+    flux::static_for<KS>([&](auto ks_) {
+      constexpr int ks = decltype(ks_)::value;
+      constexpr bool LAST = ks == KS - 1;
+      flux::static_for<G>([&](auto g_) {
+        constexpr int g = decltype(g_)::value;
+        constexpr int mi = g / C::NI, ni = G < 64 || mi % 2 == 0 ? g % C::NI : C::NI - 1 - g % C::NI;
+        if constexpr (LAST && g == BAR_AT) {
+          // slab kt + 1 is there (this wave's part, then everyone's); this slab has been read by all
+          flux::wait_vm_at_most<(NB - 2) * L + LX>();
+          flux::barrier_keeping_loads_in_flight();
+        }
+        if constexpr (C::MX) mfma_scaled<ks>(acc[mi][ni], af[ks][mi], bf[ks][ni], fs[S % 2][mi], fs[S % 2][C::MI + ni]);
+        else flux::mfma_in_place(acc[mi][ni], flux::frag_value(af[ks][mi]), flux::frag_value(bf[ks][ni]));
+        constexpr int d0 = loads_before(LAST ? g : G + g), d1 = loads_before((LAST ? g : G + g) + 1);
+#pragma unroll
+        for (int d = d0; d < d1; ++d) {
+          if constexpr (LAST) load(t, first, d, S);
+          else load(t, rest, d, S + U - 1);
+        }
+        constexpr int ALL = NF + (LAST ? NS : 0);
+        constexpr int r0 = reads_before(g, LAST ? BAR_AT : 0, ALL), r1 = reads_before(g + 1, LAST ? BAR_AT : 0, ALL);
+        flux::static_for<r1 - r0>([&](auto r_) {
+          constexpr int r = r0 + decltype(r_)::value;
+          if constexpr (r >= NF) fetch_scale<(S + 1) % U, r - NF>();
+          else if constexpr (LAST) fetch<(S + 1) % NA, (S + 1) % NB, 0, r>();
+          else fetch<S % NA, S % NB, ks + 1, r>();
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      settle_reads(1 - ks, (S + 1) % 2);
+    });
+  }
+
+  __device__ __forceinline__ void run(const TileArgs& t, f32x4 (&acc)[C::MI][C::NI]) {
+    int kt = 0;
+    for (; kt + U <= KT; kt += U)
+      flux::static_for<U>([&](auto s_) { step<decltype(s_)::value>(t, kt + decltype(s_)::value, acc); });
+    flux::static_for<U - 1>([&](auto s_) {
+      constexpr int S = decltype(s_)::value;
+      if (kt + S < KT) step<S>(t, kt + S, acc);
+    });
+    flux::mfma_results_settle<C::MI, C::NI>(acc);
+  }
+};
+
+// ---- results ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void store8(void* p, bool f32, long long at, const float (&v)[8]) {
+  if (f32) {
+    float* const q = static_cast<float*>(p) + at;
+    flux::st_stream16(q, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+    flux::st_stream16(q + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+  } else {
+    flux::st_stream16(static_cast<__bf16*>(p) + at, make_uint4(flux::pack_bf16x2(v[0], v[1]), flux::pack_bf16x2(v[2], v[3]),
+                                                              flux::pack_bf16x2(v[4], v[5]), flux::pack_bf16x2(v[6], v[7])));
+  }
+}
+__device__ __forceinline__ void add8(const void* p, bool f32, long long at, float (&v)[8]) {
+  if (f32) {
+    const float* const q = static_cast<const float*>(p) + at;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += q[e];
+  } else {
+    const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p) + at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
+  }
+}
+// v = act(g) * u
+__device__ __forceinline__ void gate8(int which, const float (&g)[8], const float (&u)[8], float (&v)[8]) {
+  if (which == FLUX_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_SILU>(g[e]) * u[e];
+  } else if (which == FLUX_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_GELU>(g[e]) * u[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_GELU_TANH>(g[e]) * u[e];
+  }
+}
+// eight columns of one row of the result, from the sums of the products
+template <int HALVES>
+__device__ __forceinline__ void finish8(const TileArgs& t, int job, int row, int col, float (&v)[8], const float (&u)[8]) {
+  const long long at = row * t.ld + col;
+  if constexpr (HALVES == 2) {
+    if (t.g != nullptr) {
+      store8(t.g, false, at, v);
+      store8(t.u, false, at, u);
+    }
+    float h[8];
+    gate8(t.act, v, u, h);
+    store8(t.out[0], t.out_f32, at, h);
+  } else {
+    if (t.accumulate) add8(t.out[job], t.out_f32, at, v);
+    store8(t.out[job], t.out_f32, at, v);
+  }
+}
+
+// Workgroups are dealt round-robin to the eight dies: die d takes the d-th run of consecutive blocks, so that neighbouring tiles
+// share panels in one L2.
+__device__ __forceinline__ int by_die(int b, int n) {
+  const int die = b % 8, each = n / 8, more = n % 8;
+  return die * each + (die < more ? die : more) + b / 8;
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = t.tiles_m * t.tiles_n;
+  int b = by_die((int)blockIdx.x, (int)gridDim.x), job = 0;
+  if constexpr (C::KIND == DW) {
+    job = b >= tiles ? 1 : 0;
+    b -= job * tiles;
+  }
+  const int part = b / tiles;
+  b -= part * tiles;
+  const int band = b / (t.band * t.tiles_n), h = min(t.band, t.tiles_m - band * t.band);
+  const int r = b - band * t.band * t.tiles_n;
+  const int m0 = (band * t.band + r % h) * C::BM, n0 = r / h * C::SUBN;
+
+  Pipe<C> pipe;
+  pipe.job = job;
+  pipe.k0 = part * t.part_slabs;
+  pipe.KT = min(t.part_slabs, t.slabs - pipe.k0);
+  pipe.init(t, pool, m0, n0, wave, lane);
+  f32x4 acc[C::MI][C::NI];
+#pragma unroll
+  for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[mi][ni][e] = 0.f;
+  pipe.start(t);
+  pipe.run(t, acc);
+  flux::wait_vm0_and_barrier();          // the staging area lies over slabs that other waves may still be reading
+
+  // Through LDS, 32 rows at a time: a lane of a 16x16 block holds four rows of one column and gets eight columns of one row.
+  float* const ep = reinterpret_cast<float*>(pool) + wave * (32 * C::EP_STRIDE);
+  constexpr int CH = C::WTN / C::HALVES / 8, RPP = 64 / CH;
+  const int cc = lane % CH, rl = lane / CH;
+  const int row0 = m0 + (wave >> 1) * C::WTM, col = n0 + (wave & 1) * (C::SUBN / 2) + cc * 8;
+#pragma unroll
+  for (int mb = 0; mb < C::WTM / 32; ++mb) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ep[(16 * s + 4 * (lane >> 4) + e) * C::EP_STRIDE + ni * 16 + (lane & 15)] = acc[2 * mb + s][ni][e];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int it = 0; it < 32 / RPP; ++it) {
+      const int rr = it * RPP + rl, row = row0 + mb * 32 + rr;
+      if (C::EDGE && (row >= t.rows || col >= t.cols)) continue;
+      const float* const p = ep + rr * C::EP_STRIDE + cc * 8;
+      float v[8], u[8] = {};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = p[e];
+      if constexpr (C::HALVES == 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = p[C::WTN / 2 + e];
+      }
+      if (t.parts > 1) {
+        const long long at = ((long long)part * t.rows + row) * (C::HALVES * t.cols) + col;
+        store8(t.partial, true, at, v);
+        if constexpr (C::HALVES == 2) store8(t.partial, true, at + t.cols, u);
+      } else {
+        finish8<C::HALVES>(t, job, row, col, v, u);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+}  // namespace flux_ffn
