@@ -37,7 +37,7 @@ def ffn_units():
     """(source, object, further flags) of the second library."""
     units = [(os.path.join(CSRC, "flux_ffn_tile.hip"), os.path.join(OBJ, f"flux_ffn_tile{k}.o"), [f"-DFLUX_FFN_KIND={k}"])
              for k in range(FFN_KINDS)]
-    return units + [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), []) for name in ("flux_ffn_api", "flux_mx4")]
+    return units + [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), []) for name in ("flux_ffn_few", "flux_ffn_api", "flux_mx4")]
 
 
 def build(verbose: bool = False, jobs: int | None = None) -> str:

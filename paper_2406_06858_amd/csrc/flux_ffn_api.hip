@@ -89,7 +89,7 @@ static int validate(int op, const flux_mx4_t* p) {
 // ---- how a product is run --------------------------------------------------------------------------------------
 struct Plan {
   int shape = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0, jobs = 1;
-  bool edge = false;
+  bool edge = false, few = false;
   size_t partial_bytes = 0;
 };
 
@@ -101,6 +101,8 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth) {
   const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
+  best.few = rows <= FEW_ROWS && (kind == GLU_NK || kind >= MX_GEMM);
+  if (best.few) return best;
   double best_us = 0;
   for (int i = 0; i < N_SHAPES; ++i) {
     const Shape& sh = SHAPES[i];
@@ -156,6 +158,12 @@ static uint32_t extent(long long rows, long long pitch, long long row) { return 
 static int launch(int kind, const Plan& pl, TileArgs& t, void* partial, hipStream_t s) {
   typedef hipError_t (*Launcher)(int, const TileArgs&, bool, int, hipStream_t);
   static constexpr Launcher launchers[KINDS] = {launch_tile0, launch_tile1, launch_tile2, launch_tile3, launch_tile4, launch_tile5, launch_tile6};
+  if (pl.few) {
+    FewArgs f = {t.a[0], {t.b[0], t.b[1]}, t.sa, {t.sb[0], t.sb[1]}, t.pitch_a, t.pitch_b, t.bytes_a, t.bytes_b, t.pitch_s, t.rows, t.cols,
+                 t.depth / 8, t.act, t.out_f32, t.ld, t.out[0], t.g, t.u};
+    FFN_HIP(launch_few(kind, f, s));
+    return FLUX_OK;
+  }
   t.slabs = pl.slabs;
   t.seg_slabs = (t.depth + 63) / 64;
   t.parts = pl.parts;

@@ -1,0 +1,26 @@
+// Instantiates the kernel for few rows.
+#include "flux_ffn_internal.h"
+
+namespace flux_ffn {
+
+template <bool MX, int HALVES, int BLOCKS, int MB, int SLABS, int RING>
+static hipError_t go(const FewArgs& a, hipStream_t s) {
+  typedef FewCfg<MX, HALVES, BLOCKS, MB, SLABS, RING> C;
+  hipLaunchKernelGGL(few_kernel<C>, dim3((a.cols + C::COLS - 1) / C::COLS), dim3(C::NT), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool MX, int HALVES, int BLOCKS>
+static hipError_t by_rows(const FewArgs& a, hipStream_t s) {
+  if (a.rows <= 16) return go<MX, HALVES, BLOCKS, 1, 2, 3>(a, s);
+  if (a.rows <= 32) return go<MX, HALVES, BLOCKS, 2, 2, 2>(a, s);
+  return go<MX, HALVES, BLOCKS, 4, 1, MX ? 2 : 3>(a, s);
+}
+
+hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s) {
+  if (kind == MX_GEMM) return a.cols > 256 * 16 ? by_rows<true, 1, 2>(a, s) : by_rows<true, 1, 1>(a, s);
+  if (kind == MX_GLU) return by_rows<true, 2, 2>(a, s);
+  return by_rows<false, 2, 2>(a, s);
+}
+
+}  // namespace flux_ffn

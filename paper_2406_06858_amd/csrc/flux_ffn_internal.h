@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include "flux_ffn.h"
 #include "flux_ffn_tile.h"
+#include "flux_ffn_few.h"
 
 namespace flux_ffn {
 
@@ -20,6 +21,10 @@ FFN_DECLARE(4)
 FFN_DECLARE(5)
 FFN_DECLARE(6)
 #undef FFN_DECLARE
+
+// Products of at most this many rows whose weights lie along the contraction (GLU_NK and the 4-bit kinds).
+constexpr int FEW_ROWS = 64;
+hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s);
 
 // Remembers a failed runtime call for flux_ffn_last_hip_error and returns the status for it.
 int hip_failed(hipError_t e);

@@ -71,7 +71,12 @@ def lib():
 
 _DT = {"bf16": FLUX_BF16, "f32": FLUX_F32, torch.bfloat16: FLUX_BF16, torch.float32: FLUX_F32}
 _ACT = {"silu": FLUX_ACT_SILU, "gelu": FLUX_ACT_GELU, "gelu_tanh": FLUX_ACT_GELU_TANH}
-_ptr, _stream = binding._ptr, binding._stream
+_ptr = binding._ptr
+
+
+def _stream(s) -> int:
+    # (the current stream's handle without a torch.cuda.Stream around it: 0.1 us where that takes 2.9, as long as a launch)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if s is None else s.cuda_stream
 
 
 def _check(status: int, where: str):
