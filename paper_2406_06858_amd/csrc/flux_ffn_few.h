@@ -37,8 +37,10 @@ struct FewCfg {
   static constexpr int WAVES = 4, NT = 256, COLS = 16 * BLOCKS / HALVES;
   static constexpr int ROWS = 16 * (BLOCKS + MB);                          // of both operands: the columns' first
   static constexpr int SLAB_BYTES = ROWS * 128;
-  static constexpr int SC_LOADS = MX ? (ROWS + 63) / 64 : 0;
-  static constexpr int TURN_BYTES = SLABS * SLAB_BYTES + SC_LOADS * 1024;
+  // 4 bits: a row's scales for a turn are 8 bytes a slab, fetched in pieces of 4 (one slab) or 16 (two).
+  static constexpr int SC_ROW = 8 * SLABS, SC_PIECE = SLABS == 2 ? 16 : 4;
+  static constexpr int SC_LOADS = MX ? (ROWS * SC_ROW + 64 * SC_PIECE - 1) / (64 * SC_PIECE) : 0;
+  static constexpr int TURN_BYTES = SLABS * SLAB_BYTES + SC_LOADS * 64 * SC_PIECE;
   static constexpr int LOADS = SLABS * ROWS / 8 + SC_LOADS;                // of a wave and turn
   static constexpr int POOL_BYTES = WAVES * RING * TURN_BYTES;
   static_assert((RING - 1) * LOADS < 64 && POOL_BYTES <= 160 * 1024, "loads in flight, LDS");
@@ -82,19 +84,20 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
         }
       }
     }
-    // 4 bits: 16 bytes of scales a row, one row a lane: of the two slabs that this turn is (or is one of)
 #pragma unroll
     for (int l = 0; l < C::SC_LOADS; ++l) {
-      const int r = l * 64 + lane, row = r - 16 * C::BLOCKS;
+      const int piece = l * 64 + lane, r = piece / (C::SC_ROW / C::SC_PIECE), row = r - 16 * C::BLOCKS;
       const bool is_b = r < 16 * C::BLOCKS;
       const int half = C::HALVES == 2 ? r / 16 : 0, col = n0 + (C::HALVES == 2 ? r % 16 : r);
-      const uint32_t at = (uint32_t)(q * C::SLABS / 2) * 16u;
+      const uint32_t at = (uint32_t)(q * C::SC_ROW + piece % (C::SC_ROW / C::SC_PIECE) * C::SC_PIECE);
       const bool in = at < t.pitch_s && (is_b ? col < t.cols : row < t.rows && r < C::ROWS);
       const uint8_t* const base = is_b ? (half ? t.sb[1] : t.sb[0]) + (uint64_t)(uint32_t)col * t.pitch_s : t.sa + (uint64_t)(uint32_t)row * t.pitch_s;
       uint64_t p = reinterpret_cast<uint64_t>(base + at);
       if (!in) p = reinterpret_cast<uint64_t>(&flux::zero_vec);
       typedef const __attribute__((address_space(1))) void* global_ptr;
-      __builtin_amdgcn_global_load_lds((global_ptr)p, (flux::lds_void_t*)(mine + slot * C::TURN_BYTES + C::SLABS * C::SLAB_BYTES + l * 1024), 16, 0, 0);
+      flux::lds_void_t* const to = (flux::lds_void_t*)(mine + slot * C::TURN_BYTES + C::SLABS * C::SLAB_BYTES + l * 64 * C::SC_PIECE);
+      if constexpr (C::SC_PIECE == 16) __builtin_amdgcn_global_load_lds((global_ptr)p, to, 16, 0, 0);      // (a size has to be a literal)
+      else __builtin_amdgcn_global_load_lds((global_ptr)p, to, 4, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -107,20 +110,20 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
   uint32_t frag[2];
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) frag[ks] = flux::lds_address(mine) + i * 128 + (((C::MX ? 2 * g + ks : ks * 4 + g) ^ swizzle<C::MX>(i)) << 4);
-  const uint32_t scale = flux::lds_address(mine) + C::SLABS * C::SLAB_BYTES + i * 16 + 2 * g;
+  const uint32_t scale = flux::lds_address(mine) + C::SLABS * C::SLAB_BYTES + i * C::SC_ROW + 2 * g;
 
-  const auto multiply = [&](int slot, int q) {
+  const auto multiply = [&](int slot) {
     const uint32_t base = (uint32_t)(slot * C::TURN_BYTES);
     flux::static_for<C::SLABS>([&](auto s_) {
       constexpr int s = decltype(s_)::value;
       u32x4 f[2][C::BLOCKS + C::MB];
       uint32_t sc[C::MX ? C::BLOCKS + C::MB : 1];
-      const uint32_t f0 = frag[0] + base, f1 = frag[1] + base, odd = C::SLABS == 2 ? s * 8 : (q & 1) * 8, fs = scale + base + odd;
+      const uint32_t f0 = frag[0] + base, f1 = frag[1] + base, fs = scale + base + s * 8;
       flux::static_for<C::BLOCKS + C::MB>([&](auto b_) {
         constexpr int b = decltype(b_)::value, OFF = s * C::SLAB_BYTES + b * 2048;
         lds_read16<OFF>(f[0][b], f0);
         lds_read16<OFF>(f[1][b], f1);
-        if constexpr (C::MX) lds_read2<b * 256>(sc[b], fs);
+        if constexpr (C::MX) lds_read2<b * 16 * C::SC_ROW>(sc[b], fs);
       });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
@@ -155,7 +158,7 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
     ask(next, q + (C::RING - 1) * C::WAVES);            // (a turn past the end is asked for as zeros)
     flux::wait_vm_at_most<(C::RING - 1) * C::LOADS>();
     asm volatile("" ::: "memory");
-    multiply(slot, q);
+    multiply(slot);
     slot = slot + 1 == C::RING ? 0 : slot + 1;
     next = next + 1 == C::RING ? 0 : next + 1;
   }

@@ -12,9 +12,12 @@ static hipError_t go(const FewArgs& a, hipStream_t s) {
 
 template <bool MX, int HALVES, int BLOCKS>
 static hipError_t by_rows(const FewArgs& a, hipStream_t s) {
-  if (a.rows <= 16) return go<MX, HALVES, BLOCKS, 1, 2, 3>(a, s);
-  if (a.rows <= 32) return go<MX, HALVES, BLOCKS, 2, 2, 2>(a, s);
-  return go<MX, HALVES, BLOCKS, 4, 1, MX ? 2 : 3>(a, s);
+  // Rows of up to 1 KB are two turns of one slab a wave: nothing to look further ahead for, and with half of the LDS two
+  // workgroups share a unit.
+  const bool is_short = a.row_vecs <= 64;
+  if (a.rows <= 16) return is_short ? go<MX, HALVES, BLOCKS, 1, 1, 2>(a, s) : go<MX, HALVES, BLOCKS, 1, 2, 3>(a, s);
+  if (a.rows <= 32) return is_short ? go<MX, HALVES, BLOCKS, 2, 1, 2>(a, s) : go<MX, HALVES, BLOCKS, 2, 1, 4>(a, s);
+  return go<MX, HALVES, BLOCKS, 4, 1, 3>(a, s);
 }
 
 hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s) {
