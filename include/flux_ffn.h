@@ -48,7 +48,9 @@ typedef struct flux_glu {
   int32_t dw_dtype;         /* of dWg and dWu                                                   */
   int32_t dw_accumulate;    /* 1: dWg and dWu are added to what the buffers hold (micro-batches) */
   int64_t ldx, ldw, ldh;    /* pitches: X and dX; Wg, Wu, dWg and dWu; H, G, U and dH           */
-  int64_t reserved;         /* must be 0                                                        */
+  int32_t tile_config;      /* 0 = library picks; else an id from flux_ffn_tile_config_info     */
+  int32_t split_k;          /* 0 = library picks; else the parts a contraction is cut into (1..64; fewer
+                               where it is too short; the weights' gradients are never cut)     */
 } flux_glu_t;
 
 /* Bytes of workspace that `op` wants (0 for a problem that is refused).  The workspace has to be zero before its first call
@@ -102,6 +104,8 @@ typedef struct flux_mx4 {
   int32_t act;              /* flux_mx4_glu: flux_act_t                                         */
   int32_t reserved;         /* must be 0                                                        */
   int64_t ldc;              /* pitch of C and H: a multiple of 8, at least N; 0 = N             */
+  int32_t tile_config;      /* as in flux_glu_t                                                 */
+  int32_t split_k;
 } flux_mx4_t;
 
 /* As flux_glu_workspace_bytes; one workspace serves the operators of this header alike. */
@@ -113,6 +117,13 @@ int flux_mx4_gemm(const flux_mx4_t* p, const void* Aq, const void* As, const voi
 /* H = act(X Wg^T) * (X Wu^T). */
 int flux_mx4_glu(const flux_mx4_t* p, const void* Xq, const void* Xs, const void* Wgq, const void* Wgs, const void* Wuq,
                  const void* Wus, void* H, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Tile configurations, ids 1 .. count: rows by columns of products (of a gated product half are gate's and half up's), and one,
+ * 0 by 0, for products of at most 64 rows whose weights lie along the contraction (4 bits, or [N,K] in flux_glu): it
+ * reads the weights once and is what the library picks there.  FLUX_ERR_UNSUPPORTED where a problem asks for that one and is
+ * not of its kind. */
+int flux_ffn_tile_config_count(void);
+int flux_ffn_tile_config_info(int32_t id, int32_t* tile_m, int32_t* tile_n);
 
 /* hipError_t of the calling thread's last FLUX_ERR_HIP from this header's calls. */
 int flux_ffn_last_hip_error(void);

@@ -66,23 +66,30 @@ static bool pitch_ok(long long pitch, long long rows, long long cols) {
 static bool dtype_ok(int d) { return d == FLUX_BF16 || d == FLUX_F32; }
 static bool act_ok(int a) { return a >= FLUX_ACT_SILU && a <= FLUX_ACT_GELU_TANH; }
 
+constexpr int FEW_CONFIG = N_SHAPES + 1;        // id of the kernel for few rows
+static bool choice_ok(int config, int parts) { return config >= 0 && config <= FEW_CONFIG && parts >= 0 && parts <= 64; }
+static bool few_fits(int kind, int rows) { return rows <= FEW_ROWS && (kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU); }
+
 static int validate(int op, const flux_glu_t* p) {
   if (p == nullptr || (op != FLUX_GLU_FORWARD && op != FLUX_GLU_BACKWARD)) return FLUX_ERR_INVALID_ARG;
   if (!act_ok(p->act) || !dtype_ok(p->out_dtype) || !dtype_ok(p->dw_dtype)) return FLUX_ERR_INVALID_ARG;
-  if ((p->w_is_nk | 1) != 1 || (p->dw_accumulate | 1) != 1 || p->reserved != 0) return FLUX_ERR_INVALID_ARG;
+  if ((p->w_is_nk | 1) != 1 || (p->dw_accumulate | 1) != 1 || !choice_ok(p->tile_config, p->split_k)) return FLUX_ERR_INVALID_ARG;
   if (p->ldx < 0 || p->ldw < 0 || p->ldh < 0) return FLUX_ERR_INVALID_ARG;
   if (p->M < 1 || p->N < 1 || p->K < 1 || p->N % 8 != 0 || p->K % 8 != 0) return FLUX_ERR_SHAPE;
   const long long w_rows = p->w_is_nk ? p->N : p->K, w_cols = p->w_is_nk ? p->K : p->N;
   if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), w_rows, w_cols) || !pitch_ok(pitch_h(p), p->M, p->N)) return FLUX_ERR_SHAPE;
+  if (p->tile_config == FEW_CONFIG && (op != FLUX_GLU_FORWARD || !few_fits(p->w_is_nk ? GLU_NK : GLU_KN, p->M))) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
 
 static int validate(int op, const flux_mx4_t* p) {
   if (p == nullptr || (op != FLUX_MX4_GEMM && op != FLUX_MX4_GLU)) return FLUX_ERR_INVALID_ARG;
   if (!dtype_ok(p->out_dtype) || (op == FLUX_MX4_GLU && !act_ok(p->act)) || p->reserved != 0 || p->ldc < 0) return FLUX_ERR_INVALID_ARG;
+  if (!choice_ok(p->tile_config, p->split_k)) return FLUX_ERR_INVALID_ARG;
   if (p->M < 1 || p->N < 1 || p->K < 1 || p->N % 8 != 0) return FLUX_ERR_SHAPE;
   if (p->M * row_bytes(p->K) >= LIMIT || p->N * row_bytes(p->K) >= LIMIT) return FLUX_ERR_SHAPE;
   if (!pitch_ok(p->ldc ? p->ldc : p->N, p->M, p->N)) return FLUX_ERR_SHAPE;
+  if (p->tile_config == FEW_CONFIG && !few_fits(MX_GEMM, p->M)) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
 
@@ -96,47 +103,54 @@ struct Plan {
 static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// depth: pieces of two bytes of (a segment of) the contraction.
-static Plan plan_tiles(int kind, int rows, int cols, int depth) {
+// Estimated us of a product: rounds of workgroups, each its slabs and its ends, and what a cut contraction costs.
+static double tile_us(int kind, const Shape& sh, long long tiles, int parts, int slabs, double sums) {
+  const double us = (double)ceil_div(tiles * parts, 256 * sh.per_unit) * (slabs * sh.slab_us + sh.ends_us);
+  return parts > 1 ? us + 4.0 + 8.0 * parts * sums / 4e6 : us;
+}
+
+// depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
+static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int want_parts) {
   const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
-  best.few = rows <= FEW_ROWS && (kind == GLU_NK || kind >= MX_GEMM);
+  best.few = config == FEW_CONFIG || (config == 0 && want_parts == 0 && few_fits(kind, rows));
   if (best.few) return best;
   double best_us = 0;
-  for (int i = 0; i < N_SHAPES; ++i) {
+  for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
     const Shape& sh = SHAPES[i];
     const int sub = sh.bn / halves, tm = ceil_div(rows, sh.bm), tn = ceil_div(cols, sub);
-    const long long tiles = (long long)tm * tn * jobs, at_once = 256 * sh.per_unit;
-    for (int parts = 1; parts <= 16; ++parts) {
+    Plan pl;
+    double pl_us = 0;
+    for (int parts = 1; parts <= (want_parts ? want_parts : 16); ++parts) {
       int each = ceil_div(slabs, parts);
       if (kind >= MX_GEMM) each += each % 2;                    // (scales come for two slabs)
-      if (parts > 1 && (kind == DW || each < 4 || (long long)each * (parts - 1) >= slabs)) continue;
-      const double slab_us = i == 0 ? 1.4 : 1.0, ends_us = i == 0 ? 7.0 : 4.0;
-      double us = (double)ceil_div(tiles * parts, at_once) * (each * slab_us + ends_us);
-      if (parts > 1) us += 4.0 + 8.0 * parts * halves * (double)rows * cols / 4e6;
-      if (best.slabs == 0 || us < best_us) {
-        best_us = us;
-        best.shape = i;
-        best.parts = parts;
-        best.part_slabs = each;
-        best.slabs = slabs;
-        best.tiles_m = tm;
-        best.tiles_n = tn;
-        best.jobs = jobs;
-        best.edge = rows % sh.bm != 0 || cols % sub != 0 || depth % 64 != 0;
-        best.partial_bytes = parts > 1 ? (size_t)parts * halves * rows * cols * 4 : 0;
-      }
+      if (parts > 1 && (kind == DW || each < (want_parts ? 1 : 4) || (long long)each * (parts - 1) >= slabs)) continue;
+      const double us = tile_us(kind, sh, (long long)tm * tn * jobs, parts, each, (double)halves * rows * cols);
+      if (pl.slabs != 0 && !want_parts && us >= pl_us) continue;          // (asked for: the most that fit)
+      pl_us = us;
+      pl.shape = i;
+      pl.parts = parts;
+      pl.part_slabs = each;
+      pl.slabs = slabs;
+      pl.tiles_m = tm;
+      pl.tiles_n = tn;
+      pl.jobs = jobs;
+      pl.edge = rows % sh.bm != 0 || cols % sub != 0 || depth % 64 != 0;
+      pl.partial_bytes = parts > 1 ? (size_t)parts * halves * rows * cols * 4 : 0;
     }
+    if (best.slabs != 0 && pl_us >= best_us) continue;
+    best = pl;
+    best_us = pl_us;
   }
   return best;
 }
 
-static Plan plan_glu(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N, p->K); }
-static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N); }
-static Plan plan_dw(const flux_glu_t* p) { return p->w_is_nk ? plan_tiles(DW, p->N, p->K, p->M) : plan_tiles(DW, p->K, p->N, p->M); }
+static Plan plan_glu(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N, p->K, p->tile_config, p->split_k); }
+static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N, p->tile_config, p->split_k); }
+static Plan plan_dw(const flux_glu_t* p) { return plan_tiles(DW, p->w_is_nk ? p->N : p->K, p->w_is_nk ? p->K : p->N, p->M, p->tile_config, 1); }
 static Plan plan_mx4(int op, const flux_mx4_t* p) {
-  return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2));
+  return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2), p->tile_config, p->split_k);
 }
 
 // Rows of dG and of dU in the workspace start at multiples of 16 bytes (N % 8 == 0).
@@ -220,6 +234,15 @@ using namespace flux_ffn;
 extern "C" {
 
 int flux_ffn_last_hip_error(void) { return g_last_hip_error; }
+
+int flux_ffn_tile_config_count(void) { return FEW_CONFIG; }
+
+int flux_ffn_tile_config_info(int32_t id, int32_t* tile_m, int32_t* tile_n) {
+  if (id < 1 || id > FEW_CONFIG || tile_m == nullptr || tile_n == nullptr) return FLUX_ERR_INVALID_ARG;
+  *tile_m = id == FEW_CONFIG ? 0 : SHAPES[id - 1].bm;
+  *tile_n = id == FEW_CONFIG ? 0 : SHAPES[id - 1].bn;
+  return FLUX_OK;
+}
 
 size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p) { return validate(op, p) == FLUX_OK ? glu_need(op, p) : 0; }
 

@@ -7,10 +7,12 @@
 
 namespace flux_ffn {
 
-// Tiles of the tile kernel: rows, columns of products, workgroups per compute unit.
-struct Shape { int bm, bn, per_unit; };
-constexpr Shape SHAPES[] = {{256, 256, 1}, {128, 128, 2}};
-constexpr int N_SHAPES = 2;
+// Tiles of the tile kernel: rows, columns of products, workgroups per compute unit; what a round of them takes, us a slab and
+// for its two ends.
+struct Shape { int bm, bn, per_unit; double slab_us, ends_us; };
+constexpr Shape SHAPES[] = {{256, 256, 1, 1.4, 7.0}, {256, 128, 1, 0.8, 4.0}, {128, 128, 2, 1.0, 4.0},
+                            {128, 128, 1, 0.55, 4.0}, {64, 128, 2, 0.6, 4.0}, {64, 128, 1, 0.4, 4.0}};
+constexpr int N_SHAPES = 6;
 
 #define FFN_DECLARE(KIND) hipError_t launch_tile##KIND(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s);
 FFN_DECLARE(0)

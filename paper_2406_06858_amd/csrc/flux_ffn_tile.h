@@ -59,13 +59,16 @@ struct Cfg {
   static constexpr int SUBN = BN / HALVES;                                   // columns of the result
   static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, SUB_BYTES = B_BYTES / HALVES;
   static constexpr int RING_BYTES = NA * A_BYTES + NB * B_BYTES;
-  static constexpr int SC_BYTES = 256 * 16;                                  // scales of one operand, two slabs
+  // 4 bits: scales come for two slabs at a time, 16 bytes a row, into a ring of RS such pairs for either operand.  Those of A for a
+  // pair are asked for beside the slab ahead of it, those of B beside its first slab; RS is what that takes (see Pipe::load).
+  // The last KB takes what waves without a row write.
+  static constexpr int RS = (NB + 3) / 2, SC_A = BM * 16, SC_B = BN * 16, SC_BYTES = MX ? RS * (SC_A + SC_B) + 1024 : 0;
   static constexpr int EP_STRIDE = WTN + 8;
   static constexpr int EP_BYTES = 4 * 32 * EP_STRIDE * 4;
-  static constexpr int LOOP_BYTES = RING_BYTES + (MX ? 4 * SC_BYTES : 0);
+  static constexpr int LOOP_BYTES = RING_BYTES + SC_BYTES;
   static constexpr int POOL_BYTES = LOOP_BYTES > EP_BYTES ? LOOP_BYTES : EP_BYTES;
   static_assert(POOL_BYTES * OCC <= 160 * 1024, "LDS");
-  static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || (NA == 2 && NB == 2)), "rings");
+  static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || NA == NB), "rings");
 };
 
 // Which 16-byte slot of a row holds slot s: s ^ swizzle(row).  A fragment's lanes are rows 0..15 of slot q, the next sixteen
@@ -143,7 +146,7 @@ struct Pipe {
   typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX> LdB;
   static constexpr int NA = C::NA, NB = C::NB;
   static constexpr bool A_LEADS = NA > NB;                               // by one slab
-  static constexpr int U = C::MX ? 4 : NA == NB ? NB : NA * NB;          // slabs after which all rings are where they were
+  static constexpr int U = NA != NB ? NA * NB : C::MX && NB % 2 ? 2 * NB : NB;      // slabs after which the rings are where they were
   static constexpr int KS = 2;
   static constexpr int G = C::MI * C::NI;                                // MFMAs per k-step
   static constexpr int NF = C::MI + C::NI, NS = C::MX ? NF : 0;          // fragments of a k-step; scales of a slab
@@ -166,7 +169,6 @@ struct Pipe {
   LdA la;
   LdB lb;
   uint32_t voff_s[2];                // 4 bits: the lane's row of scales of A; of B
-  bool s_in[2];
   int job, k0, KT, wave;             // first slab of this workgroup's, and how many
   uint32_t a[A_HI][NAV], b[B_HI][NBV], sc[2];
   FragA af[2][C::MI];
@@ -175,7 +177,10 @@ struct Pipe {
 
   __device__ __forceinline__ unsigned char* slab_a(int i) const { return pool + i * C::A_BYTES; }
   __device__ __forceinline__ unsigned char* slab_b(int i) const { return pool + NA * C::A_BYTES + i * C::B_BYTES; }
-  __device__ __forceinline__ unsigned char* scales(int operand, int pair) const { return pool + C::RING_BYTES + (operand * 2 + pair) * C::SC_BYTES; }
+  // where the scales of a pair of slabs lie: place `at` of the ring
+  __device__ __forceinline__ unsigned char* scales(int operand, int at) const {
+    return pool + C::RING_BYTES + (operand ? C::RS * C::SC_A + at * C::SC_B : at * C::SC_A);
+  }
 
   template <int R>
   static __device__ __forceinline__ uint32_t across(uint32_t base, int r, int i, int g) {      // transposing read of rows r.. of the result
@@ -211,10 +216,8 @@ struct Pipe {
     if constexpr (C::MX) {
       // wave w fetches 64 rows of each operand, 16 bytes (two slabs) a lane; of a gated B the lower half of the rows is gate's
       const int row = 64 * wave + lane, half = row / C::SUBN, col = row - half * C::SUBN;
-      voff_s[0] = (uint32_t)(m0 + row) * t.pitch_s;
-      voff_s[1] = (uint32_t)(n0 + col) * t.pitch_s;
-      s_in[0] = row < C::BM && m0 + row < t.rows;
-      s_in[1] = row < C::BN && n0 + col < t.cols;
+      voff_s[0] = row < C::BM && m0 + row < t.rows ? (uint32_t)(m0 + row) * t.pitch_s : LdA::OUTSIDE;
+      voff_s[1] = row < C::BN && n0 + col < t.cols ? (uint32_t)(n0 + col) * t.pitch_s : LdA::OUTSIDE;
       sc[0] = flux::lds_address(scales(0, 0)) + (wm * C::WTM + i) * 16 + 2 * g;
       sc[1] = flux::lds_address(scales(1, 0)) + (rb + i) * 16 + 2 * g;
     }
@@ -262,12 +265,11 @@ struct Pipe {
       }
     }
   }
-  // scales of fragment R for slab place S of the unrolled loop (both k-steps) into set S % 2
+  // scales of fragment R (both k-steps) into set S % 2, S the slab's place in the unrolled loop; from_a, from_b: of its pair
   template <int S, int R>
-  __device__ __forceinline__ void fetch_scale() {
-    constexpr int PLACE = S / 2 % 2 * C::SC_BYTES + S % 2 * 8;
+  __device__ __forceinline__ void fetch_scale(uint32_t from_a, uint32_t from_b) {
     constexpr int OFF = R < C::MI ? R * 256 : ((R - C::MI) / C::NIH * C::SUBN + (R - C::MI) % C::NIH * 16) * 16;
-    asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(fs[S % 2][R]) : "v"(sc[R < C::MI ? 0 : 1]), "n"(PLACE + OFF));
+    asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(fs[S % 2][R]) : "v"(R < C::MI ? from_a : from_b), "n"(S % 2 * 8 + OFF));
   }
 
   __device__ __forceinline__ Slab slab(const TileArgs& t, bool is_b, int s) const {
@@ -294,8 +296,8 @@ struct Pipe {
     const uint32_t at = (uint32_t)(k0 / 2 + pair) * 16u;
     const bool there = 2 * pair < KT && at < t.pitch_s;
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, there ? (int)((uint32_t)rows * t.pitch_s) : 0, 0x00027000);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(scales(operand, pair % 2) + wave * 1024), 16,
-                                             (int)(s_in[operand] ? voff_s[operand] : LdA::OUTSIDE), (int)at, 0, 0);
+    unsigned char* const to = 64 * wave < (operand ? C::BN : C::BM) ? scales(operand, pair % C::RS) + wave * 1024 : pool + C::LOOP_BYTES - 1024;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)to, 16, (int)voff_s[operand], (int)at, 0, 0);
   }
 
   // What step kt (place S of the unrolled loop; -1 ahead of the first) asks for from its barrier on: slab kt + NB, of A one
@@ -323,7 +325,7 @@ struct Pipe {
       for (int d = 0; d < LA; ++d) la.load(d, sa.r0, sa.k, t.depth, slab_a(j));
 #pragma unroll
       for (int d = 0; d < LB; ++d) load_b(t, sb, d, j);
-      if (LS) load_scales(t, 1, 0);
+      if (LS) load_scales(t, (j + 1) % 2, (j + 1) / 2);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (A_LEADS) {
@@ -338,7 +340,7 @@ struct Pipe {
     flux::wait_vm_at_most<(NB - 2) * L + LX + L0>();
     flux::barrier_keeping_loads_in_flight();
     flux::static_for<NF>([&](auto r) { fetch<0, 0, 0, decltype(r)::value>(); });
-    flux::static_for<NS>([&](auto r) { fetch_scale<0, decltype(r)::value>(); });
+    flux::static_for<NS>([&](auto r) { fetch_scale<0, decltype(r)::value>(sc[0], sc[1]); });
     settle_reads(0, 0);
   }
 
@@ -359,6 +361,8 @@ struct Pipe {
   __device__ __forceinline__ void step(const TileArgs& t, int kt, f32x4 (&acc)[C::MI][C::NI]) {
     kt = __builtin_amdgcn_readfirstlane(kt);
     const Window rest = window(t, kt - 1), first = window(t, kt);
+    const uint32_t at = C::MX ? (uint32_t)((kt + 1) / 2 % C::RS) : 0u;                   // of the next slab's scales
+    const uint32_t from_a = C::MX ? sc[0] + at * C::SC_A : 0u, from_b = C::MX ? sc[1] + at * C::SC_B : 0u;
     flux::static_for<KS>([&](auto ks_) {
       constexpr int ks = decltype(ks_)::value;
       constexpr bool LAST = ks == KS - 1;
@@ -382,7 +386,7 @@ struct Pipe {
         constexpr int r0 = reads_before(g, LAST ? BAR_AT : 0, ALL), r1 = reads_before(g + 1, LAST ? BAR_AT : 0, ALL);
         flux::static_for<r1 - r0>([&](auto r_) {
           constexpr int r = r0 + decltype(r_)::value;
-          if constexpr (r >= NF) fetch_scale<(S + 1) % U, r - NF>();
+          if constexpr (r >= NF) fetch_scale<S + 1, r - NF>(from_a, from_b);
           else if constexpr (LAST) fetch<(S + 1) % NA, (S + 1) % NB, 0, r>();
           else fetch<S % NA, S % NB, ks + 1, r>();
         });

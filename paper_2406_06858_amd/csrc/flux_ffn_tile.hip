@@ -15,9 +15,15 @@ static hipError_t go(const TileArgs& a, bool edge, int grid, hipStream_t s) {
 #define FFN_CAT(a, b) FFN_CAT2(a, b)
 
 hipError_t FFN_CAT(launch_tile, FLUX_FFN_KIND)(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s) {
-  constexpr int NA = FLUX_FFN_KIND == MX_GEMM || FLUX_FFN_KIND == MX_GLU ? 2 : 3;
-  if (shape == 0) return go<256, 256, NA, 2, 1>(a, edge, grid, s);
-  return go<128, 128, 2, 2, 2>(a, edge, grid, s);
+  constexpr bool MX = FLUX_FFN_KIND == MX_GEMM || FLUX_FFN_KIND == MX_GLU;
+  switch (shape) {                     // (SHAPES)
+    case 0: return go<256, 256, MX ? 2 : 3, 2, 1>(a, edge, grid, s);
+    case 1: return go<256, 128, MX ? 2 : 3, MX ? 2 : 3, 1>(a, edge, grid, s);
+    case 2: return go<128, 128, 2, 2, 2>(a, edge, grid, s);
+    case 3: return go<128, 128, 4, 4, 1>(a, edge, grid, s);
+    case 4: return go<64, 128, MX ? 2 : 3, MX ? 2 : 3, 2>(a, edge, grid, s);
+    default: return go<64, 128, 6, 6, 1>(a, edge, grid, s);
+  }
 }
 
 }  // namespace flux_ffn

@@ -22,7 +22,7 @@ FLUX_MX4_GEMM, FLUX_MX4_GLU = 0, 1
 EXPORTS = [
     "flux_glu", "flux_glu_backward", "flux_glu_workspace_bytes", "flux_ffn_init", "flux_mx4_row_bytes",
     "flux_mx4_scale_row_bytes", "flux_mx4_quantize", "flux_mx4_dequantize", "flux_mx4_workspace_bytes", "flux_mx4_gemm",
-    "flux_mx4_glu", "flux_ffn_last_hip_error",
+    "flux_mx4_glu", "flux_ffn_tile_config_count", "flux_ffn_tile_config_info", "flux_ffn_last_hip_error",
 ]
 
 
@@ -31,7 +31,8 @@ class flux_glu_t(C.Structure):
         ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32),
         ("act", C.c_int32), ("w_is_nk", C.c_int32),
         ("out_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("dw_accumulate", C.c_int32),
-        ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64), ("reserved", C.c_int64),
+        ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64),
+        ("tile_config", C.c_int32), ("split_k", C.c_int32),
     ]
 
 
@@ -39,7 +40,7 @@ class flux_mx4_t(C.Structure):
     _fields_ = [
         ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32),
         ("out_dtype", C.c_int32), ("act", C.c_int32), ("reserved", C.c_int32),
-        ("ldc", C.c_int64),
+        ("ldc", C.c_int64), ("tile_config", C.c_int32), ("split_k", C.c_int32),
     ]
 
 
@@ -63,6 +64,7 @@ def lib():
         L.flux_mx4_dequantize.argtypes = [i32, i32, vp, vp, i32, vp, i64, vp]
         L.flux_mx4_gemm.argtypes = [pm, vp, vp, vp, vp, vp, vp, sz, vp]
         L.flux_mx4_glu.argtypes = [pm, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.flux_ffn_tile_config_info.argtypes = [i32, C.POINTER(i32), C.POINTER(i32)]
         for name in EXPORTS:
             getattr(L, name).restype = sz if name.endswith("_bytes") else C.c_int
         _lib = L
@@ -88,12 +90,14 @@ def _ws(workspace):
     return (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
-def glu_problem(M, N, K, act="silu", w_is_nk=0, out_dtype="bf16", dw_dtype="bf16", dw_accumulate=0, ldx=0, ldw=0, ldh=0) -> flux_glu_t:
-    return flux_glu_t(M, N, K, _ACT.get(act, act), w_is_nk, _DT[out_dtype], _DT[dw_dtype], dw_accumulate, ldx, ldw, ldh, 0)
+def glu_problem(M, N, K, act="silu", w_is_nk=0, out_dtype="bf16", dw_dtype="bf16", dw_accumulate=0, ldx=0, ldw=0, ldh=0,
+                tile_config=0, split_k=0) -> flux_glu_t:
+    return flux_glu_t(M, N, K, _ACT.get(act, act), w_is_nk, _DT[out_dtype], _DT[dw_dtype], dw_accumulate, ldx, ldw, ldh,
+                      tile_config, split_k)
 
 
-def mx4_problem(M, N, K, out_dtype="bf16", act="silu", ldc=0) -> flux_mx4_t:
-    return flux_mx4_t(M, N, K, _DT[out_dtype], _ACT.get(act, act), 0, ldc)
+def mx4_problem(M, N, K, out_dtype="bf16", act="silu", ldc=0, tile_config=0, split_k=0) -> flux_mx4_t:
+    return flux_mx4_t(M, N, K, _DT[out_dtype], _ACT.get(act, act), 0, ldc, tile_config, split_k)
 
 
 def flux_glu_workspace_bytes(op: int, p: flux_glu_t) -> int:
@@ -110,6 +114,16 @@ def flux_mx4_row_bytes(K: int) -> int:
 
 def flux_mx4_scale_row_bytes(K: int) -> int:
     return int(lib().flux_mx4_scale_row_bytes(K))
+
+
+def flux_ffn_tile_config_count() -> int:
+    return lib().flux_ffn_tile_config_count()
+
+
+def flux_ffn_tile_config_info(cfg_id: int):
+    v = [C.c_int32(0) for _ in range(2)]
+    _check(lib().flux_ffn_tile_config_info(cfg_id, *[C.byref(x) for x in v]), "flux_ffn_tile_config_info")
+    return tuple(x.value for x in v)
 
 
 def flux_ffn_init(workspace, stream=None):

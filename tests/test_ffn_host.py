@@ -25,7 +25,7 @@ def test_library_exports_what_the_header_declares():
 
 def test_struct_layouts():
     assert ctypes.sizeof(ffn.flux_glu_t) == 64 and ffn.flux_glu_t.ldx.offset == 32
-    assert ctypes.sizeof(ffn.flux_mx4_t) == 32 and ffn.flux_mx4_t.ldc.offset == 24
+    assert ctypes.sizeof(ffn.flux_mx4_t) == 40 and ffn.flux_mx4_t.ldc.offset == 24
 
 
 def _glu(p, ptrs=None, ws=(PTR, 1 << 40), backward=False):
@@ -45,7 +45,8 @@ def _glu(p, ptrs=None, ws=(PTR, 1 << 40), backward=False):
     (dict(ldh=-128), fb.FLUX_ERR_INVALID_ARG), (dict(M=1 << 24, N=128), fb.FLUX_ERR_SHAPE), (dict(ldh=1 << 27), fb.FLUX_ERR_SHAPE),
     (dict(act=3), fb.FLUX_ERR_INVALID_ARG), (dict(act=-1), fb.FLUX_ERR_INVALID_ARG), (dict(w_is_nk=2), fb.FLUX_ERR_INVALID_ARG),
     (dict(out_dtype=2), fb.FLUX_ERR_INVALID_ARG), (dict(dw_dtype=-1), fb.FLUX_ERR_INVALID_ARG), (dict(dw_accumulate=2), fb.FLUX_ERR_INVALID_ARG),
-    (dict(reserved=1), fb.FLUX_ERR_INVALID_ARG),
+    (dict(tile_config=-1), fb.FLUX_ERR_INVALID_ARG), (dict(tile_config=99), fb.FLUX_ERR_INVALID_ARG), (dict(split_k=65), fb.FLUX_ERR_INVALID_ARG),
+    (dict(split_k=-1), fb.FLUX_ERR_INVALID_ARG),
 ])
 def test_glu_refuses_problems(bad, status, backward):
     p = ffn.glu_problem(64, 128, 256)
@@ -81,7 +82,7 @@ def test_backward_wants_its_workspace():
     (dict(M=0), fb.FLUX_ERR_SHAPE), (dict(N=0), fb.FLUX_ERR_SHAPE), (dict(K=0), fb.FLUX_ERR_SHAPE), (dict(N=100), fb.FLUX_ERR_SHAPE),
     (dict(ldc=120), fb.FLUX_ERR_SHAPE), (dict(ldc=130), fb.FLUX_ERR_SHAPE), (dict(ldc=-8), fb.FLUX_ERR_INVALID_ARG),
     (dict(out_dtype=5), fb.FLUX_ERR_INVALID_ARG), (dict(reserved=1), fb.FLUX_ERR_INVALID_ARG),
-    (dict(M=1 << 24), fb.FLUX_ERR_SHAPE),
+    (dict(M=1 << 24), fb.FLUX_ERR_SHAPE), (dict(tile_config=99), fb.FLUX_ERR_INVALID_ARG), (dict(split_k=-1), fb.FLUX_ERR_INVALID_ARG),
 ])
 @pytest.mark.parametrize("glu", [False, True])
 def test_mx4_products_refuse(bad, status, glu):
@@ -117,6 +118,21 @@ def test_casts_refuse(args, status):
     L = ffn.lib()
     assert L.flux_mx4_quantize(rows, K, dtype, wide, ld, q, scales, None) == status
     assert L.flux_mx4_dequantize(rows, K, q, scales, dtype, wide, ld, None) == status
+
+
+def test_tile_configurations():
+    few = ffn.flux_ffn_tile_config_count()
+    shapes = [ffn.flux_ffn_tile_config_info(i) for i in range(1, few + 1)]
+    assert shapes[-1] == (0, 0) and all(m > 0 and n > 0 for m, n in shapes[:-1])
+    for bad in (0, few + 1):
+        with pytest.raises(fb.FluxError):
+            ffn.flux_ffn_tile_config_info(bad)
+    # the one for few rows: not for many, not for weights across the contraction, not for gradients
+    for p, backward in ((ffn.glu_problem(65, 128, 256, w_is_nk=1, tile_config=few), False), (ffn.glu_problem(8, 128, 256, tile_config=few), False),
+                        (ffn.glu_problem(8, 128, 256, w_is_nk=1, tile_config=few), True)):
+        assert _glu(p, backward=backward) == fb.FLUX_ERR_UNSUPPORTED
+    p = ffn.mx4_problem(65, 128, 256, tile_config=few)
+    assert ffn.lib().flux_mx4_gemm(ctypes.byref(p), *[PTR] * 5, PTR, 1 << 40, None) == fb.FLUX_ERR_UNSUPPORTED
 
 
 def test_mx4_row_sizes():

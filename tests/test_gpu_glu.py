@@ -42,14 +42,15 @@ def _workspace(op, p):
     return ws
 
 
-def _forward(M, N, K, act, nk, out="bf16", save=True, pad=0, seed=1, X=None, Wg=None, Wu=None, scale=None):
+def _forward(M, N, K, act, nk, out="bf16", save=True, pad=0, seed=1, X=None, Wg=None, Wu=None, scale=None,
+             tile_config=0, split_k=0):
     scale = K ** -0.5 if scale is None else scale
     X = _draw(seed, M, K) if X is None else X
     Wg = _draw(seed + 1, K, N, scale=2 * scale) if Wg is None else Wg
     Wu = _draw(seed + 2, K, N, scale=scale) if Wu is None else Wu
     w_cols = K if nk else N
     p = ffn.glu_problem(M, N, K, act=act, w_is_nk=nk, out_dtype=out, ldx=K + pad if pad else 0, ldw=w_cols + 2 * pad if pad else 0,
-                        ldh=N + 3 * pad if pad else 0)
+                        ldh=N + 3 * pad if pad else 0, tile_config=tile_config, split_k=split_k)
     nan = float("nan")
     w = [_pitched(t.t().contiguous() if nk else t, w_cols + 2 * pad, nan) for t in (Wg, Wu)]
     x = _pitched(X, K + pad, nan)
@@ -147,16 +148,28 @@ def test_forward_keeps_rows_apart(M, nk):
     _check_forward((X[keep], Wg, Wu), (H[keep], G[keep], U[keep]), "silu")
 
 
+TILES = list(range(1, ffn.flux_ffn_tile_config_count()))        # (the last one is for few rows)
+
+
+@pytest.mark.parametrize("nk", [0, 1])
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("cfg", TILES)
+def test_forward_of_every_tile(cfg, split, nk):
+    """Shapes that no tile divides and one that all do; K shorter than the ring of slabs and longer, cut and whole."""
+    for M, N, K in ((300, 200, 1480), (512, 256, 1024), (70, 72, 72)):
+        _check_forward(*_forward(M, N, K, "silu", nk, tile_config=cfg, split_k=split), "silu")
+
+
 # ---- backward -----------------------------------------------------------------------------------------------------
 def _backward(M, N, K, act, nk, out="bf16", dw="bf16", accumulate=0, pad=0, seed=3, X=None, Wg=None, Wu=None, G=None, U=None, dH=None,
-              want_x=True, want_w=True):
+              want_x=True, want_w=True, tile_config=0, split_k=0):
     X = _draw(seed, M, K) if X is None else X
     Wg, Wu = _draw(seed + 1, K, N, scale=K ** -0.5) if Wg is None else Wg, _draw(seed + 2, K, N, scale=K ** -0.5) if Wu is None else Wu
     G, U = _draw(seed + 3, M, N, scale=2.0) if G is None else G, _draw(seed + 4, M, N) if U is None else U
     dH = _draw(seed + 5, M, N) if dH is None else dH
     w_cols = K if nk else N
     p = ffn.glu_problem(M, N, K, act=act, w_is_nk=nk, out_dtype=out, dw_dtype=dw, dw_accumulate=accumulate, ldx=K + pad if pad else 0,
-                        ldw=w_cols + 2 * pad if pad else 0, ldh=N + 3 * pad if pad else 0)
+                        ldw=w_cols + 2 * pad if pad else 0, ldh=N + 3 * pad if pad else 0, tile_config=tile_config, split_k=split_k)
     nan = float("nan")
     w = [_pitched(t.t().contiguous() if nk else t, w_cols + 2 * pad, nan) for t in (Wg, Wu)]
     x = _pitched(X, K + pad, nan)
@@ -217,6 +230,14 @@ def test_backward_in_32_bits_and_accumulated(M, N, K, act, nk):
 def test_backward_pitches(M, N, K, nk):
     _check_backward(*_backward(M, N, K, "gelu_tanh", nk, pad=8, seed=51), "gelu_tanh")
     _check_backward(*_backward(M, N, K, "silu", nk, out="f32", dw="f32", pad=16, seed=52), "silu", "f32", "f32")
+
+
+@pytest.mark.parametrize("nk", [0, 1])
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("cfg", TILES)
+def test_backward_of_every_tile(cfg, split, nk):
+    for M, N, K in ((300, 712, 264), (256, 512, 256), (70, 72, 72)):
+        _check_backward(*_backward(M, N, K, "silu", nk, tile_config=cfg, split_k=split), "silu")
 
 
 @pytest.mark.parametrize("want_x,want_w", [(True, False), (False, True), (False, False)])

@@ -119,8 +119,8 @@ def _workspace(op, p):
     return ws
 
 
-def _gemm(a, b, M, N, K, out="bf16", pad=0):
-    p = ffn.mx4_problem(M, N, K, out_dtype=out, ldc=N + pad if pad else 0)
+def _gemm(a, b, M, N, K, out="bf16", pad=0, **choice):
+    p = ffn.mx4_problem(M, N, K, out_dtype=out, ldc=N + pad if pad else 0, **choice)
     c = torch.full((M, N + pad), 7.0, dtype=TORCH[out], device=DEV)
     ffn.flux_mx4_gemm(p, *a, *b, c, _workspace(ffn.FLUX_MX4_GEMM, p))
     torch.cuda.synchronize()
@@ -182,13 +182,30 @@ def test_gemm_nan_blocks_and_zeros(M, N, K):
     _check_gemm(got[rows][:, cols], va[rows], vb[cols], "f32")
 
 
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("cfg", range(1, ffn.flux_ffn_tile_config_count()))
+def test_gemm_of_every_tile(cfg, split):
+    for M, N, K in ((300, 200, 5900), (512, 256, 4096), (70, 72, 300)):
+        (a, va), (b, vb) = _packed(M, K, 13), _packed(N, K, 14)
+        _check_gemm(_gemm(a, b, M, N, K, "f32", tile_config=cfg, split_k=split), va, vb, "f32")
+
+
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("cfg", range(1, ffn.flux_ffn_tile_config_count()))
+def test_glu_of_every_tile(cfg, split):
+    for M, N, K in ((300, 200, 5900), (512, 256, 4096), (70, 72, 300)):
+        _check_glu(M, N, K, "silu", "f32", 0, tile_config=cfg, split_k=split)
+
+
 @pytest.mark.parametrize("M,N,K", PRODUCTS)
 def test_glu(M, N, K):
     act = ("silu", "gelu", "gelu_tanh")[(M + N + K) % 3]
-    out = "f32" if M % 3 == 0 else "bf16"
+    _check_glu(M, N, K, act, "f32" if M % 3 == 0 else "bf16", 8 * (M % 2))
+
+
+def _check_glu(M, N, K, act, out, pad, **choice):
     (x, vx), (g, vg), (u, vu) = _packed(M, K, 7), _packed(N, K, 8, K ** -0.5), _packed(N, K, 9, K ** -0.5)
-    pad = 8 * (M % 2)
-    p = ffn.mx4_problem(M, N, K, out_dtype=out, act=act, ldc=N + pad if pad else 0)
+    p = ffn.mx4_problem(M, N, K, out_dtype=out, act=act, ldc=N + pad if pad else 0, **choice)
     h = torch.full((M, N + pad), 7.0, dtype=TORCH[out], device=DEV)
     ffn.flux_mx4_glu(p, *x, *g, *u, h, _workspace(ffn.FLUX_MX4_GLU, p))
     torch.cuda.synchronize()
