@@ -49,16 +49,16 @@ typedef struct flux_glu {
   int32_t dw_accumulate;    /* 1: dWg and dWu are added to what the buffers hold (micro-batches) */
   int64_t ldx, ldw, ldh;    /* pitches: X and dX; Wg, Wu, dWg and dWu; H, G, U and dH           */
   int32_t tile_config;      /* 0 = library picks; else an id from flux_ffn_tile_config_info     */
-  int32_t split_k;          /* 0 = library picks; else the parts a contraction is cut into (1..64; fewer
-                               where it is too short; the weights' gradients are never cut)     */
+  int32_t split_k;          /* 0 = library picks; else the most parts (1..64) that the contraction of the tiles
+                               of a partly filled last round may be cut into; 1 = no cut        */
 } flux_glu_t;
 
-/* Bytes of workspace that `op` wants (0 for a problem that is refused).  The workspace has to be zero before its first call
- * (flux_ffn_init, or any other fill with zeros); a call leaves it fit for the next one, whatever its problem or op.  Calls that
- * share a workspace must not overlap in time. */
+/* Bytes of workspace that `op` wants (0 for a problem that is refused).  A workspace has to go through flux_ffn_init (or be
+ * filled with zeros) before its first call; a call leaves it fit for the next one, whatever its problem or op.  Calls
+ * that share a workspace must not overlap in time. */
 size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p);
 
-/* Fills a workspace with zeros. */
+/* Makes a workspace ready for its first call: clears what has to be zero in it. */
 int flux_ffn_init(void* workspace, size_t workspace_bytes, void* stream);
 
 /* H = act(X Wg) * (X Wu).  Products accumulate in fp32; activation and product are taken in fp32, rounded once.

@@ -1,4 +1,5 @@
 // The gated feed-forward block and the products of 4-bit matrices: checks of arguments, kernels, dispatch.
+#include <algorithm>
 #include "flux_ffn_internal.h"
 #include "flux_ffn_act.h"
 
@@ -11,19 +12,8 @@ int hip_failed(hipError_t e) {
 }
 
 // ---- kernels -------------------------------------------------------------------------------------------------
-// The parts of a contraction that was cut over workgroups, added in ascending order, and the end of the product.
-template <int HALVES>
-__global__ void __launch_bounds__(256) join_kernel(const TileArgs t) {
-  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
-  const int row = (int)(i / t.cols), col = (int)(i % t.cols);            // (cols % 8 == 0)
-  if (row >= t.rows) return;
-  const long long pitch = (long long)HALVES * t.cols, each = t.rows * pitch, at = row * pitch + col;
-  float v[8] = {}, u[8] = {};
-  for (int p = 0; p < t.parts; ++p) {
-    add8(t.partial, true, p * each + at, v);
-    if (HALVES == 2) add8(t.partial, true, p * each + at + t.cols, u);
-  }
-  finish8<HALVES>(t, 0, row, col, v, u);
+__global__ void __launch_bounds__(256) zero_kernel(uint4* p, long long n) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // dG = dH U act'(G), dU = dH act(G), rounded to bf16 once: the operands of the three products.
@@ -95,7 +85,7 @@ static int validate(int op, const flux_mx4_t* p) {
 
 // ---- how a product is run --------------------------------------------------------------------------------------
 struct Plan {
-  int shape = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0, jobs = 1;
+  int shape = 0, full = 0, cut = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0;
   bool edge = false, few = false;
   size_t partial_bytes = 0;
 };
@@ -103,10 +93,13 @@ struct Plan {
 static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Estimated us of a product: rounds of workgroups, each its slabs and its ends, and what a cut contraction costs.
-static double tile_us(int kind, const Shape& sh, long long tiles, int parts, int slabs, double sums) {
-  const double us = (double)ceil_div(tiles * parts, 256 * sh.per_unit) * (slabs * sh.slab_us + sh.ends_us);
-  return parts > 1 ? us + 4.0 + 8.0 * parts * sums / 4e6 : us;
+// Estimated us of a product: rounds of workgroups, each its slabs and its ends.
+static double tile_us(const Shape& sh, long long full, long long cut, int parts, int slabs, int part_slabs) {
+  const int at_once = 256 * sh.per_unit;
+  double us = (double)ceil_div(full, at_once) * (slabs * sh.slab_us + sh.ends_us);
+  if (cut > 0) us += part_slabs * (cut * parts <= 256 ? sh.alone_us : sh.slab_us) + sh.ends_us + sh.join_us;
+  else if (full <= 256) us = slabs * sh.alone_us + sh.ends_us;
+  return us;
 }
 
 // depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
@@ -120,24 +113,31 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
   for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
     const Shape& sh = SHAPES[i];
     const int sub = sh.bn / halves, tm = ceil_div(rows, sh.bm), tn = ceil_div(cols, sub);
+    const int at_once = 256 * sh.per_unit, tiles = tm * tn * jobs;
+    if ((long long)tm * tn * jobs >= (1ll << 30)) continue;
+    // Whole rounds of tiles are a workgroup each; what is left over may be cut along the contraction, over no more workgroups than
+    // run at once, since its parts wait for each other.
+    const int rest = tiles % at_once;
     Plan pl;
     double pl_us = 0;
-    for (int parts = 1; parts <= (want_parts ? want_parts : 16); ++parts) {
+    for (int parts = 1; parts <= (want_parts ? want_parts : MAX_PARTS); ++parts) {
       int each = ceil_div(slabs, parts);
       if (kind >= MX_GEMM) each += each % 2;                    // (scales come for two slabs)
-      if (parts > 1 && (kind == DW || each < (want_parts ? 1 : 4) || (long long)each * (parts - 1) >= slabs)) continue;
-      const double us = tile_us(kind, sh, (long long)tm * tn * jobs, parts, each, (double)halves * rows * cols);
+      if (parts > 1 && (rest == 0 || parts > MAX_PARTS || (long long)rest * parts > at_once || each < (want_parts ? 1 : 4) || (long long)each * (parts - 1) >= slabs)) continue;
+      const int cut = parts > 1 ? rest : 0;
+      const double us = tile_us(sh, tiles - cut, cut, parts, slabs, each);
       if (pl.slabs != 0 && !want_parts && us >= pl_us) continue;          // (asked for: the most that fit)
       pl_us = us;
       pl.shape = i;
+      pl.full = tiles - cut;
+      pl.cut = cut;
       pl.parts = parts;
       pl.part_slabs = each;
       pl.slabs = slabs;
       pl.tiles_m = tm;
       pl.tiles_n = tn;
-      pl.jobs = jobs;
       pl.edge = rows % sh.bm != 0 || cols % sub != 0 || depth % 64 != 0;
-      pl.partial_bytes = parts > 1 ? (size_t)parts * halves * rows * cols * 4 : 0;
+      pl.partial_bytes = (size_t)cut * parts * sh.bm * sh.bn * 4;
     }
     if (best.slabs != 0 && pl_us >= best_us) continue;
     best = pl;
@@ -148,7 +148,7 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
 
 static Plan plan_glu(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N, p->K, p->tile_config, p->split_k); }
 static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N, p->tile_config, p->split_k); }
-static Plan plan_dw(const flux_glu_t* p) { return plan_tiles(DW, p->w_is_nk ? p->N : p->K, p->w_is_nk ? p->K : p->N, p->M, p->tile_config, 1); }
+static Plan plan_dw(const flux_glu_t* p) { return plan_tiles(DW, p->w_is_nk ? p->N : p->K, p->w_is_nk ? p->K : p->N, p->M, p->tile_config, p->split_k); }
 static Plan plan_mx4(int op, const flux_mx4_t* p) {
   return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2), p->tile_config, p->split_k);
 }
@@ -156,9 +156,14 @@ static Plan plan_mx4(int op, const flux_mx4_t* p) {
 // Rows of dG and of dU in the workspace start at multiples of 16 bytes (N % 8 == 0).
 static size_t slope_bytes(const flux_glu_t* p) { return 4ull * p->M * p->N; }
 
+// The workspace: a word a cut tile, zero between calls; then dG and dU (backward); then the cut tiles' sums.
+constexpr size_t WS_HEADER = 512 * COUNTER_STRIDE * 4;
+static size_t after_slopes(const flux_glu_t* p) { return WS_HEADER + (slope_bytes(p) + 255) / 256 * 256; }
+static size_t need_of(const Plan& pl) { return pl.cut ? WS_HEADER + pl.partial_bytes : 0; }
+
 static size_t glu_need(int op, const flux_glu_t* p) {
-  if (op == FLUX_GLU_FORWARD) return plan_glu(p).partial_bytes;
-  return (slope_bytes(p) + 255) / 256 * 256 + plan_dx(p).partial_bytes;
+  if (op == FLUX_GLU_FORWARD) return need_of(plan_glu(p));
+  return after_slopes(p) + std::max(plan_dx(p).partial_bytes, plan_dw(p).partial_bytes);
 }
 
 static int workspace_ok(size_t need, const void* ws, size_t bytes) {
@@ -169,7 +174,7 @@ static int workspace_ok(size_t need, const void* ws, size_t bytes) {
 // ---- dispatch ------------------------------------------------------------------------------------------------
 static uint32_t extent(long long rows, long long pitch, long long row) { return (uint32_t)((rows - 1) * pitch + row); }
 
-static int launch(int kind, const Plan& pl, TileArgs& t, void* partial, hipStream_t s) {
+static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partial_at, hipStream_t s) {
   typedef hipError_t (*Launcher)(int, const TileArgs&, bool, int, hipStream_t);
   static constexpr Launcher launchers[KINDS] = {launch_tile0, launch_tile1, launch_tile2, launch_tile3, launch_tile4, launch_tile5, launch_tile6};
   if (pl.few) {
@@ -180,21 +185,16 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* partial, hipStrea
   }
   t.slabs = pl.slabs;
   t.seg_slabs = (t.depth + 63) / 64;
+  t.full_tiles = pl.full;
+  t.cut_tiles = pl.cut;
   t.parts = pl.parts;
   t.part_slabs = pl.part_slabs;
   t.tiles_m = pl.tiles_m;
   t.tiles_n = pl.tiles_n;
   t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
-  t.partial = static_cast<float*>(partial);
-  const long long grid = (long long)pl.tiles_m * pl.tiles_n * pl.jobs * pl.parts;
-  if (grid >= (1ll << 31)) return FLUX_ERR_SHAPE;
-  FFN_HIP(launchers[kind](pl.shape, t, pl.edge, (int)grid, s));
-  if (pl.parts > 1) {
-    const dim3 join((unsigned)(((long long)t.rows * t.cols / 8 + 255) / 256));
-    if (halves_of(kind) == 2) hipLaunchKernelGGL(join_kernel<2>, join, dim3(256), 0, s, t);
-    else hipLaunchKernelGGL(join_kernel<1>, join, dim3(256), 0, s, t);
-    FFN_HIP(hipGetLastError());
-  }
+  t.counters = static_cast<uint32_t*>(ws);
+  t.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_at);
+  FFN_HIP(launchers[kind](pl.shape, t, pl.edge, pl.full + pl.cut * pl.parts, s));
   return FLUX_OK;
 }
 
@@ -224,7 +224,7 @@ static int mx4(int op, const flux_mx4_t* p, const void* Aq, const void* As, cons
   t.out_f32 = p->out_dtype == FLUX_F32;
   t.ld = p->ldc ? p->ldc : p->N;
   t.out[0] = out;
-  return launch(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, plan_mx4(op, p), t, ws, static_cast<hipStream_t>(stream));
+  return launch(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, plan_mx4(op, p), t, ws, WS_HEADER, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace flux_ffn
@@ -246,11 +246,15 @@ int flux_ffn_tile_config_info(int32_t id, int32_t* tile_m, int32_t* tile_n) {
 
 size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p) { return validate(op, p) == FLUX_OK ? glu_need(op, p) : 0; }
 
-size_t flux_mx4_workspace_bytes(int op, const flux_mx4_t* p) { return validate(op, p) == FLUX_OK ? plan_mx4(op, p).partial_bytes : 0; }
+size_t flux_mx4_workspace_bytes(int op, const flux_mx4_t* p) { return validate(op, p) == FLUX_OK ? need_of(plan_mx4(op, p)) : 0; }
 
 int flux_ffn_init(void* workspace, size_t workspace_bytes, void* stream) {
   if (workspace == nullptr && workspace_bytes != 0) return FLUX_ERR_INVALID_ARG;
-  (void)stream;
+  if (!aligned(workspace, 16)) return FLUX_ERR_WORKSPACE;
+  const long long vecs = (long long)(std::min(workspace_bytes, WS_HEADER) / 16);           // (nothing else has to be zero)
+  if (vecs == 0) return FLUX_OK;
+  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<uint4*>(workspace), vecs);
+  FFN_HIP(hipGetLastError());
   return FLUX_OK;
 }
 
@@ -281,7 +285,7 @@ int flux_glu(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu,
   t.out[0] = H;
   t.g = static_cast<__bf16*>(G);
   t.u = static_cast<__bf16*>(U);
-  return launch(p->w_is_nk ? GLU_NK : GLU_KN, plan_glu(p), t, workspace, static_cast<hipStream_t>(stream));
+  return launch(p->w_is_nk ? GLU_NK : GLU_KN, plan_glu(p), t, workspace, WS_HEADER, static_cast<hipStream_t>(stream));
 }
 
 int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu, const void* G, const void* U,
@@ -299,7 +303,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   d.G = static_cast<const __bf16*>(G);
   d.U = static_cast<const __bf16*>(U);
   d.dH = static_cast<const __bf16*>(dH);
-  d.dG = static_cast<__bf16*>(workspace);
+  d.dG = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + WS_HEADER);
   d.dU = d.dG + (long long)p->M * p->N;
   d.ldh = pitch_h(p);
   d.ldd = p->N;
@@ -329,7 +333,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
     t.out_f32 = p->out_dtype == FLUX_F32;
     t.ld = lx;
     t.out[0] = dX;
-    st = launch(p->w_is_nk ? DX_KN : DX_NK, plan_dx(p), t, static_cast<char*>(workspace) + (slope_bytes(p) + 255) / 256 * 256, s);
+    st = launch(p->w_is_nk ? DX_KN : DX_NK, plan_dx(p), t, workspace, after_slopes(p), s);
     if (st != FLUX_OK) return st;
   }
   if (dWg != nullptr) {
@@ -352,7 +356,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
     t.ld = lw;
     t.out[0] = dWg;
     t.out[1] = dWu;
-    st = launch(DW, plan_dw(p), t, nullptr, s);
+    st = launch(DW, plan_dw(p), t, workspace, after_slopes(p), s);
     if (st != FLUX_OK) return st;
   }
   return FLUX_OK;

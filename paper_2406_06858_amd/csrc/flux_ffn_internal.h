@@ -7,11 +7,11 @@
 
 namespace flux_ffn {
 
-// Tiles of the tile kernel: rows, columns of products, workgroups per compute unit; what a round of them takes, us a slab and
-// for its two ends.
-struct Shape { int bm, bn, per_unit; double slab_us, ends_us; };
-constexpr Shape SHAPES[] = {{256, 256, 1, 1.4, 7.0}, {256, 128, 1, 0.8, 4.0}, {128, 128, 2, 1.0, 4.0},
-                            {128, 128, 1, 0.55, 4.0}, {64, 128, 2, 0.6, 4.0}, {64, 128, 1, 0.4, 4.0}};
+// Tiles of the tile kernel: rows, columns of products, workgroups per compute unit; and in us, what a slab takes where every unit
+// has that many, what it takes with one a unit, a workgroup's two ends, and what joining the parts of a cut tile adds.
+struct Shape { int bm, bn, per_unit; double slab_us, alone_us, ends_us, join_us; };
+constexpr Shape SHAPES[] = {{256, 256, 1, 1.35, 1.28, 8.0, 10.0}, {256, 128, 1, 0.8, 0.8, 5.0, 5.0}, {128, 128, 2, 1.05, 0.85, 5.0, 4.0},
+                            {128, 128, 1, 0.57, 0.55, 5.0, 3.0},  {64, 128, 2, 0.75, 0.48, 4.0, 3.0}, {64, 128, 1, 0.43, 0.43, 4.0, 2.0}};
 constexpr int N_SHAPES = 6;
 
 #define FFN_DECLARE(KIND) hipError_t launch_tile##KIND(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s);

@@ -38,13 +38,16 @@ struct TileArgs {
   int32_t rows, cols;            // of the result
   int32_t depth;                 // of the contraction (of a segment of it), in pieces of two bytes
   int32_t seg_slabs, slabs;      // slabs of a segment; of the whole contraction
-  int32_t parts, part_slabs;     // the contraction cut over workgroups: parts of part_slabs slabs each
+  // The first full_tiles tiles are a workgroup each; of the cut_tiles after them the contraction is cut over `parts` workgroups, each
+  // part_slabs slabs.
+  int32_t full_tiles, cut_tiles, parts, part_slabs;
   int32_t tiles_m, tiles_n, band;
   int32_t act, out_f32, accumulate;
   int64_t ld;                    // pitch of the results, elements
   void* out[2];                  // dW: by weight; else [0]
   __bf16 *g, *u;                 // gated: kept for the backward pass, or null
-  float* partial;                // parts > 1: [parts][rows][halves * cols]
+  float* partial;                // [cut_tiles][parts][BM * BN]
+  uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
 
 template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_>
@@ -67,7 +70,7 @@ struct Cfg {
   static constexpr int EP_BYTES = 4 * 32 * EP_STRIDE * 4;
   static constexpr int LOOP_BYTES = RING_BYTES + SC_BYTES;
   static constexpr int POOL_BYTES = LOOP_BYTES > EP_BYTES ? LOOP_BYTES : EP_BYTES;
-  static_assert(POOL_BYTES * OCC <= 160 * 1024, "LDS");
+  static_assert(POOL_BYTES * OCC <= 160 * 1024 && LOOP_BYTES >= EP_BYTES + 16, "LDS");
   static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || NA == NB), "rings");
 };
 
@@ -461,6 +464,125 @@ __device__ __forceinline__ void finish8(const TileArgs& t, int job, int row, int
   }
 }
 
+// ---- tiles whose contraction is cut ------------------------------------------------------------------------------
+// Every part leaves its sums in memory and counts itself in; when all have, each part adds up a share of the tile, 16-row blocks in
+// turn, in the parts' order whoever does it, and finishes those rows.  Nobody waits for long: a part that has waited 100 us for
+// the others (they may not have been given a compute unit yet) leaves its share to whoever comes last.  The tile's word holds, in
+// this order, how many have arrived, how many are done with the word, and a bit for every part that has left.  Arriving
+// and leaving are one atomic addition each, so that the last to arrive either finds the bit, or the leaver finds that all have arrived.
+//
+// Sums are stored and read past this die's L2 (SC1): "my stores are acknowledged" before counting in is all that the others need.
+//
+// us, joined by a kernel of its own / here: see the plan's table.
+constexpr int MAX_PARTS = 16, COUNTER_STRIDE = 16;             // (words: 64 bytes)
+constexpr uint32_t ARRIVED = 1u, DONE = 1u << 8, LEFT = 1u << 16;
+constexpr unsigned long long PATIENCE_TICKS = 10000;           // of 10 ns
+
+// Which parts' shares this workgroup finishes, as bits.  One thread.
+__device__ __forceinline__ uint32_t count_in(uint32_t* word, int part, int parts, bool has_share) {
+  const auto add = [&](uint32_t v) { return __hip_atomic_fetch_add(word, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  const uint32_t all = (uint32_t)parts;
+  const auto done = [&](uint32_t before) {                     // the last one done puts the word back
+    if ((before >> 8 & 255u) == all - 1u) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  uint32_t before = add(ARRIVED);
+  const uint32_t mine = has_share ? 1u << part : 0u;
+  if ((before & 255u) == all - 1u) {
+    done(add(DONE));
+    return mine | before >> 16;
+  }
+  if (has_share) {
+    const unsigned long long until = wall_clock64() + PATIENCE_TICKS;
+    while ((__hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 255u) != all) {
+      if (wall_clock64() >= until) {
+        before = add(DONE + (LEFT << part));
+        done(before);
+        return (before & 255u) == all ? mine : 0u;
+      }
+      __builtin_amdgcn_s_sleep(4);
+    }
+  }
+  done(add(DONE));
+  return mine;
+}
+
+// `rows` rows of the wave's part of the tile, from row `row` of the result on, out of its staging area
+template <class C>
+__device__ __forceinline__ void finish_rows(const TileArgs& t, int job, const float* ep, int rows, int row, int n0, int lane, int wave) {
+  constexpr int CH = C::WTN / C::HALVES / 8, RPP = 64 / CH;
+  const int cc = lane % CH, rl = lane / CH, col = n0 + (wave & 1) * (C::SUBN / 2) + cc * 8;
+#pragma unroll 1
+  for (int r = rl; r < rows; r += RPP) {
+    if (C::EDGE && (row + r >= t.rows || col >= t.cols)) continue;
+    const float* const p = ep + r * C::EP_STRIDE + cc * 8;
+    float v[8], u[8] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[e];
+    if constexpr (C::HALVES == 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = p[C::WTN / 2 + e];
+    }
+    finish8<C::HALVES>(t, job, row + r, col, v, u);
+  }
+}
+
+template <class C>
+__device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* pool, float* ep, f32x4 (&acc)[C::MI][C::NI], int cut, int part,
+                                           int job, int m0, int n0, int lane, int wave) {
+  constexpr int SC1 = 16, BYTES = C::BM * C::BN * 4;
+  const int tid = wave * 64 + lane, row0 = m0 + (wave >> 1) * C::WTM;
+  float* const sums = t.partial + (size_t)cut * t.parts * (C::BM * C::BN);
+  const auto rsrc = [&](int p) { return __builtin_amdgcn_make_buffer_rsrc(sums + (size_t)p * (C::BM * C::BN), 0, BYTES, 0x00027000); };
+  // a vector is four rows of one column; one that lies past the last row is neither stored nor read (an offset past the records)
+  const int below = C::EDGE ? t.rows - row0 - 4 * (lane >> 4) : C::BM;
+  const __amdgpu_buffer_rsrc_t own = rsrc(part);
+#pragma unroll
+  for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni) {
+      asm volatile("" : "+a"(acc[mi][ni]));            // (stored from where it is)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[mi][ni]), own, mi * 16 < below ? ((mi * C::NI + ni) * 256 + tid) * 16 : BYTES, 0, SC1);
+    }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): acknowledged
+  __syncthreads();
+  uint32_t* const shared = reinterpret_cast<uint32_t*>(pool + C::EP_BYTES);
+  if (tid == 0) *shared = count_in(t.counters + cut * COUNTER_STRIDE, part, t.parts, part < C::MI);
+  __syncthreads();
+  const uint32_t shares = (uint32_t)__builtin_amdgcn_readfirstlane((int)*shared);
+#pragma unroll 1
+  for (int mi = 0; mi < C::MI; ++mi) {
+    if (!(shares >> mi % t.parts & 1u)) continue;      // (uniform)
+    f32x4 sum[C::NI];
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni) sum[ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int P = 16 / C::NI;                      // parts whose vectors are asked for before the first is used
+#pragma unroll 1
+    for (int p0 = 0; p0 < t.parts; p0 += P) {
+      u32x4 v[P][C::NI];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const bool there = p0 + p < t.parts;           // (one past the last: zeros)
+        const __amdgpu_buffer_rsrc_t r = rsrc(there ? p0 + p : 0);
+#pragma unroll
+        for (int ni = 0; ni < C::NI; ++ni)
+          v[p][ni] = __builtin_amdgcn_raw_buffer_load_b128(r, there && mi * 16 < below ? ((mi * C::NI + ni) * 256 + tid) * 16 : BYTES, 0, SC1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int ni = 0; ni < C::NI; ++ni) sum[ni] += __builtin_bit_cast(f32x4, v[p][ni]);
+    }
+#pragma unroll
+    for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ep[(4 * (lane >> 4) + e) * C::EP_STRIDE + ni * 16 + (lane & 15)] = sum[ni][e];
+    __builtin_amdgcn_wave_barrier();
+    finish_rows<C>(t, job, ep, 16, row0 + mi * 16, n0, lane, wave);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // Workgroups are dealt round-robin to the eight dies: die d takes the d-th run of consecutive blocks, so that neighbouring tiles
 // share panels in one L2.
 __device__ __forceinline__ int by_die(int b, int n) {
@@ -472,14 +594,20 @@ template <class C>
 __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles = t.tiles_m * t.tiles_n;
-  int b = by_die((int)blockIdx.x, (int)gridDim.x), job = 0;
-  if constexpr (C::KIND == DW) {
-    job = b >= tiles ? 1 : 0;
-    b -= job * tiles;
+  const bool is_cut = (int)blockIdx.x >= t.full_tiles;
+  int b, cut = 0, part = 0, job = 0;
+  if (is_cut) {
+    const int r = by_die((int)blockIdx.x - t.full_tiles, t.cut_tiles * t.parts);
+    part = r / t.cut_tiles;
+    cut = r - part * t.cut_tiles;
+    b = t.full_tiles + cut;
+  } else {
+    b = by_die((int)blockIdx.x, t.full_tiles);
   }
-  const int part = b / tiles;
-  b -= part * tiles;
+  if constexpr (C::KIND == DW) {
+    job = b >= t.tiles_m * t.tiles_n ? 1 : 0;
+    b -= job * (t.tiles_m * t.tiles_n);
+  }
   const int band = b / (t.band * t.tiles_n), h = min(t.band, t.tiles_m - band * t.band);
   const int r = b - band * t.band * t.tiles_n;
   const int m0 = (band * t.band + r % h) * C::BM, n0 = r / h * C::SUBN;
@@ -487,7 +615,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
   Pipe<C> pipe;
   pipe.job = job;
   pipe.k0 = part * t.part_slabs;
-  pipe.KT = min(t.part_slabs, t.slabs - pipe.k0);
+  pipe.KT = is_cut ? min(t.part_slabs, t.slabs - pipe.k0) : t.slabs;
   pipe.init(t, pool, m0, n0, wave, lane);
   f32x4 acc[C::MI][C::NI];
 #pragma unroll
@@ -502,38 +630,22 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
 
   // Through LDS, 32 rows at a time: a lane of a 16x16 block holds four rows of one column and gets eight columns of one row.
   float* const ep = reinterpret_cast<float*>(pool) + wave * (32 * C::EP_STRIDE);
-  constexpr int CH = C::WTN / C::HALVES / 8, RPP = 64 / CH;
-  const int cc = lane % CH, rl = lane / CH;
-  const int row0 = m0 + (wave >> 1) * C::WTM, col = n0 + (wave & 1) * (C::SUBN / 2) + cc * 8;
+  if (is_cut) {
+    finish_cut<C>(t, pool, ep, acc, cut, part, job, m0, n0, lane, wave);
+    return;
+  }
 #pragma unroll
   for (int mb = 0; mb < C::WTM / 32; ++mb) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int ni = 0; ni < C::NI; ++ni)
+      for (int ni = 0; ni < C::NI; ++ni) {
+        asm volatile("" : "+a"(acc[2 * mb + s][ni]));      // (it stays in its accumulation registers until here)
 #pragma unroll
         for (int e = 0; e < 4; ++e) ep[(16 * s + 4 * (lane >> 4) + e) * C::EP_STRIDE + ni * 16 + (lane & 15)] = acc[2 * mb + s][ni][e];
+      }
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int it = 0; it < 32 / RPP; ++it) {
-      const int rr = it * RPP + rl, row = row0 + mb * 32 + rr;
-      if (C::EDGE && (row >= t.rows || col >= t.cols)) continue;
-      const float* const p = ep + rr * C::EP_STRIDE + cc * 8;
-      float v[8], u[8] = {};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = p[e];
-      if constexpr (C::HALVES == 2) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = p[C::WTN / 2 + e];
-      }
-      if (t.parts > 1) {
-        const long long at = ((long long)part * t.rows + row) * (C::HALVES * t.cols) + col;
-        store8(t.partial, true, at, v);
-        if constexpr (C::HALVES == 2) store8(t.partial, true, at + t.cols, u);
-      } else {
-        finish8<C::HALVES>(t, job, row, col, v, u);
-      }
-    }
+    finish_rows<C>(t, job, ep, 32, m0 + (wave >> 1) * C::WTM + mb * 32, n0, lane, wave);
     __builtin_amdgcn_wave_barrier();
   }
 }
