@@ -94,12 +94,10 @@ static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Estimated us of a product: rounds of workgroups, each its slabs and its ends.
-static double tile_us(const Shape& sh, long long full, long long cut, int parts, int slabs, int part_slabs) {
-  const int at_once = 256 * sh.per_unit;
-  double us = (double)ceil_div(full, at_once) * (slabs * sh.slab_us + sh.ends_us);
-  if (cut > 0) us += part_slabs * (cut * parts <= 256 ? sh.alone_us : sh.slab_us) + sh.ends_us + sh.join_us;
-  else if (full <= 256) us = slabs * sh.alone_us + sh.ends_us;
-  return us;
+static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int parts, int slabs, int part_slabs) {
+  if (cut == 0 && full <= 256) return slabs * p.alone_us + p.ends_us;
+  const double us = ceil_div(full, 256 * sh.per_unit) * (slabs * p.slab_us + p.ends_us);
+  return cut == 0 ? us : us + part_slabs * (cut * parts <= 256 ? p.alone_us : p.slab_us) + p.ends_us + p.join_us;
 }
 
 // depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
@@ -125,7 +123,7 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
       if (kind >= MX_GEMM) each += each % 2;                    // (scales come for two slabs)
       if (parts > 1 && (rest == 0 || parts > MAX_PARTS || (long long)rest * parts > at_once || each < (want_parts ? 1 : 4) || (long long)each * (parts - 1) >= slabs)) continue;
       const int cut = parts > 1 ? rest : 0;
-      const double us = tile_us(sh, tiles - cut, cut, parts, slabs, each);
+      const double us = tile_us(sh, sh.pace[kind >= MX_GEMM], tiles - cut, cut, parts, slabs, each);
       if (pl.slabs != 0 && !want_parts && us >= pl_us) continue;          // (asked for: the most that fit)
       pl_us = us;
       pl.shape = i;
@@ -192,6 +190,13 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partia
   t.tiles_m = pl.tiles_m;
   t.tiles_n = pl.tiles_n;
   t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
+  // Pieces of 64 bytes that are whole ones may go past the caches, which then keep the operands' panels; pieces that are not may not, and a
+  // plain product of a short contraction has more results than panels.  us, past the caches / kept there: gated 4-bit 8192x4096x1024 57.7 / 66,
+  // bf16 8192x4096x512 78 / 85; plain 4-bit 8192x8192x512 69 / 44, x4096 158 / 140, 8192x12288x6144 322 / 336; ragged weights' gradients
+  // 1496x3400x5112 135 / 125.
+  const int size = t.out_f32 ? 4 : 2;
+  t.stream = t.ld * size % 64 == 0 && aligned(t.out[0], 64) && aligned(t.out[1], 64) && aligned(t.g, 64) && aligned(t.u, 64) &&
+             (halves_of(kind) == 2 || t.slabs >= 20);
   t.counters = static_cast<uint32_t*>(ws);
   t.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_at);
   FFN_HIP(launchers[kind](pl.shape, t, pl.edge, pl.full + pl.cut * pl.parts, s));

@@ -43,6 +43,7 @@ struct TileArgs {
   int32_t full_tiles, cut_tiles, parts, part_slabs;
   int32_t tiles_m, tiles_n, band;
   int32_t act, out_f32, accumulate;
+  int32_t stream;                // results go past the caches
   int64_t ld;                    // pitch of the results, elements
   void* out[2];                  // dW: by weight; else [0]
   __bf16 *g, *u;                 // gated: kept for the backward pass, or null
@@ -66,11 +67,8 @@ struct Cfg {
   // pair are asked for beside the slab ahead of it, those of B beside its first slab; RS is what that takes (see Pipe::load).
   // The last KB takes what waves without a row write.
   static constexpr int RS = (NB + 3) / 2, SC_A = BM * 16, SC_B = BN * 16, SC_BYTES = MX ? RS * (SC_A + SC_B) + 1024 : 0;
-  static constexpr int EP_STRIDE = WTN + 8;
-  static constexpr int EP_BYTES = 4 * 32 * EP_STRIDE * 4;
-  static constexpr int LOOP_BYTES = RING_BYTES + SC_BYTES;
-  static constexpr int POOL_BYTES = LOOP_BYTES > EP_BYTES ? LOOP_BYTES : EP_BYTES;
-  static_assert(POOL_BYTES * OCC <= 160 * 1024 && LOOP_BYTES >= EP_BYTES + 16, "LDS");
+  static constexpr int POOL_BYTES = RING_BYTES + SC_BYTES;
+  static_assert(POOL_BYTES * OCC <= 160 * 1024, "LDS");
   static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || NA == NB), "rings");
 };
 
@@ -249,8 +247,8 @@ struct Pipe {
   // fragment R, in the order the MFMAs want them, of k-step K out of A's slab SA / B's slab SB in LDS
   template <int SA, int SB, int K, int R>
   __device__ __forceinline__ void fetch() {
-    constexpr bool IS_B = R >= 1 && R <= C::NI;
-    constexpr int I = R == 0 ? 0 : (IS_B ? R - 1 : R - C::NI);
+    constexpr bool IS_B = R == 0 || R > C::MI;
+    constexpr int I = R == 0 ? 0 : (IS_B ? R - C::MI : R - 1);
     if constexpr (!IS_B) {
       if constexpr (C::A_T) {
         read_halves<SA * C::A_BYTES + K * 32 * C::BM * 2, C::BM * 2>(af[K][I], a, I);
@@ -299,7 +297,7 @@ struct Pipe {
     const uint32_t at = (uint32_t)(k0 / 2 + pair) * 16u;
     const bool there = 2 * pair < KT && at < t.pitch_s;
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, there ? (int)((uint32_t)rows * t.pitch_s) : 0, 0x00027000);
-    unsigned char* const to = 64 * wave < (operand ? C::BN : C::BM) ? scales(operand, pair % C::RS) + wave * 1024 : pool + C::LOOP_BYTES - 1024;
+    unsigned char* const to = 64 * wave < (operand ? C::BN : C::BM) ? scales(operand, pair % C::RS) + wave * 1024 : pool + C::POOL_BYTES - 1024;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)to, 16, (int)voff_s[operand], (int)at, 0, 0);
   }
 
@@ -371,14 +369,16 @@ struct Pipe {
       constexpr bool LAST = ks == KS - 1;
       flux::static_for<G>([&](auto g_) {
         constexpr int g = decltype(g_)::value;
-        constexpr int mi = g / C::NI, ni = G < 64 || mi % 2 == 0 ? g % C::NI : C::NI - 1 - g % C::NI;
+        // (the columns' fragment is held over a run of MFMAs; with the large tile every second run goes backwards: it begins with the
+        // fragment that the run before ended with)
+        constexpr int ni = g / C::MI, mi = G < 64 || ni % 2 == 0 ? g % C::MI : C::MI - 1 - g % C::MI;
         if constexpr (LAST && g == BAR_AT) {
           // slab kt + 1 is there (this wave's part, then everyone's); this slab has been read by all
           flux::wait_vm_at_most<(NB - 2) * L + LX>();
           flux::barrier_keeping_loads_in_flight();
         }
-        if constexpr (C::MX) mfma_scaled<ks>(acc[mi][ni], af[ks][mi], bf[ks][ni], fs[S % 2][mi], fs[S % 2][C::MI + ni]);
-        else flux::mfma_in_place(acc[mi][ni], flux::frag_value(af[ks][mi]), flux::frag_value(bf[ks][ni]));
+        if constexpr (C::MX) mfma_scaled<ks>(acc[mi][ni], bf[ks][ni], af[ks][mi], fs[S % 2][C::MI + ni], fs[S % 2][mi]);
+        else flux::mfma_in_place(acc[mi][ni], flux::frag_value(bf[ks][ni]), flux::frag_value(af[ks][mi]));
         constexpr int d0 = loads_before(LAST ? g : G + g), d1 = loads_before((LAST ? g : G + g) + 1);
 #pragma unroll
         for (int d = d0; d < d1; ++d) {
@@ -412,55 +412,100 @@ struct Pipe {
 };
 
 // ---- results ---------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store8(void* p, bool f32, long long at, const float (&v)[8]) {
-  if (f32) {
-    float* const q = static_cast<float*>(p) + at;
-    flux::st_stream16(q, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-    flux::st_stream16(q + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
-  } else {
-    flux::st_stream16(static_cast<__bf16*>(p) + at, make_uint4(flux::pack_bf16x2(v[0], v[1]), flux::pack_bf16x2(v[2], v[3]),
-                                                              flux::pack_bf16x2(v[4], v[5]), flux::pack_bf16x2(v[6], v[7])));
+// Nothing passes through LDS.  The columns' fragment goes first into the MFMAs, so a lane holds four consecutive columns of row
+// lane % 16: 16 bytes of an fp32 result.  For bf16 one swap of neighbouring 16-lane rows between two blocks of columns makes that eight.
+// Either way four lanes have 64 bytes of a row side by side.
+//
+// us a tile's ends took through LDS, 256 bytes of a row side by side, and take here: 4-bit 256x256 8.0 / 6.4.  (Pieces exchanged so that a
+// store is eight rows by 128 bytes: the same where results are kept in the caches, 5-8 % slower for gated products.)
+__device__ __forceinline__ void store16(void* p, bool stream, const u32x4& v) {
+  if (stream) flux::st_stream16(p, make_uint4(v[0], v[1], v[2], v[3]));
+  else *static_cast<u32x4*>(p) = v;
+}
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  return u32x4{flux::pack_bf16x2(v[0], v[1]), flux::pack_bf16x2(v[2], v[3]), flux::pack_bf16x2(v[4], v[5]), flux::pack_bf16x2(v[6], v[7])};
+}
+// Columns 32 n' + 16 (g % 2) + 8 (g / 2) .. + 7 of two neighbouring blocks of columns, g = lane / 16.
+__device__ __forceinline__ void eight_columns(const f32x4& x, const f32x4& y, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(y[e]), false, false);
+    v[e] = __uint_as_float(r[0]);
+    v[4 + e] = __uint_as_float(r[1]);
   }
 }
-__device__ __forceinline__ void add8(const void* p, bool f32, long long at, float (&v)[8]) {
-  if (f32) {
-    const float* const q = static_cast<const float*>(p) + at;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += q[e];
-  } else {
-    const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p) + at);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
-  }
-}
-// v = act(g) * u
-__device__ __forceinline__ void gate8(int which, const float (&g)[8], const float (&u)[8], float (&v)[8]) {
+
+// v = act(v) * u
+template <int N>
+__device__ __forceinline__ void gate(int which, float (&v)[N], const float (&u)[N]) {
   if (which == FLUX_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_SILU>(g[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_SILU>(v[e]) * u[e];
   } else if (which == FLUX_ACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_GELU>(g[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU>(v[e]) * u[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act<FLUX_ACT_GELU_TANH>(g[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU_TANH>(v[e]) * u[e];
   }
 }
-// eight columns of one row of the result, from the sums of the products
-template <int HALVES>
-__device__ __forceinline__ void finish8(const TileArgs& t, int job, int row, int col, float (&v)[8], const float (&u)[8]) {
-  const long long at = row * t.ld + col;
-  if constexpr (HALVES == 2) {
+
+// 16 rows of the wave's part of the tile, out of its accumulators
+template <class C>
+__device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const f32x4 (&acc)[C::NI], int row, int col0, int lane) {
+  const int g = lane >> 4;
+  row += lane & 15;
+  if (C::EDGE && row >= t.rows) return;                 // (lanes that swap are of one row)
+  const long long row_at = row * t.ld;
+  if constexpr (C::HALVES == 2) {
     if (t.g != nullptr) {
-      store8(t.g, false, at, v);
-      store8(t.u, false, at, u);
+#pragma unroll
+      for (int n = 0; n < C::NI; n += 2) {
+        const int col = col0 + n % C::NIH * 16 + 16 * (g & 1) + 8 * (g >> 1);
+        float v[8];
+        eight_columns(acc[n], acc[n + 1], v);
+        if (C::EDGE && col >= t.cols) continue;
+        store16((n < C::NIH ? t.g : t.u) + row_at + col, t.stream, pack8(v));
+      }
     }
-    float h[8];
-    gate8(t.act, v, u, h);
-    store8(t.out[0], t.out_f32, at, h);
+  }
+  if (!t.out_f32) {
+#pragma unroll
+    for (int n = 0; n < C::NIH; n += 2) {
+      const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
+      __bf16* const to = static_cast<__bf16*>(t.out[job]) + row_at + col;
+      float v[8];
+      eight_columns(acc[n], acc[n + 1], v);
+      if constexpr (C::HALVES == 2) {
+        float u[8];
+        eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
+        gate(t.act, v, u);
+      }
+      if (C::EDGE && col >= t.cols) continue;
+      if (C::HALVES == 1 && t.accumulate) {
+        const bf16x8 o = *reinterpret_cast<const bf16x8*>(to);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
+      }
+      store16(to, t.stream, pack8(v));
+    }
   } else {
-    if (t.accumulate) add8(t.out[job], t.out_f32, at, v);
-    store8(t.out[job], t.out_f32, at, v);
+#pragma unroll
+    for (int n = 0; n < C::NIH; ++n) {
+      const int col = col0 + n * 16 + 4 * g;
+      if (C::EDGE && col >= t.cols) continue;
+      float* const to = static_cast<float*>(t.out[job]) + row_at + col;
+      float v[4] = {acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
+      if constexpr (C::HALVES == 2) {
+        const float u[4] = {acc[C::NIH + n][0], acc[C::NIH + n][1], acc[C::NIH + n][2], acc[C::NIH + n][3]};
+        gate(t.act, v, u);
+      } else if (t.accumulate) {
+        const f32x4 o = *reinterpret_cast<const f32x4*>(to);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += o[e];
+      }
+      store16(to, t.stream, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+    }
   }
 }
 
@@ -506,35 +551,15 @@ __device__ __forceinline__ uint32_t count_in(uint32_t* word, int part, int parts
   return mine;
 }
 
-// `rows` rows of the wave's part of the tile, from row `row` of the result on, out of its staging area
 template <class C>
-__device__ __forceinline__ void finish_rows(const TileArgs& t, int job, const float* ep, int rows, int row, int n0, int lane, int wave) {
-  constexpr int CH = C::WTN / C::HALVES / 8, RPP = 64 / CH;
-  const int cc = lane % CH, rl = lane / CH, col = n0 + (wave & 1) * (C::SUBN / 2) + cc * 8;
-#pragma unroll 1
-  for (int r = rl; r < rows; r += RPP) {
-    if (C::EDGE && (row + r >= t.rows || col >= t.cols)) continue;
-    const float* const p = ep + r * C::EP_STRIDE + cc * 8;
-    float v[8], u[8] = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p[e];
-    if constexpr (C::HALVES == 2) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = p[C::WTN / 2 + e];
-    }
-    finish8<C::HALVES>(t, job, row + r, col, v, u);
-  }
-}
-
-template <class C>
-__device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* pool, float* ep, f32x4 (&acc)[C::MI][C::NI], int cut, int part,
+__device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* pool, f32x4 (&acc)[C::MI][C::NI], int cut, int part,
                                            int job, int m0, int n0, int lane, int wave) {
   constexpr int SC1 = 16, BYTES = C::BM * C::BN * 4;
   const int tid = wave * 64 + lane, row0 = m0 + (wave >> 1) * C::WTM;
   float* const sums = t.partial + (size_t)cut * t.parts * (C::BM * C::BN);
   const auto rsrc = [&](int p) { return __builtin_amdgcn_make_buffer_rsrc(sums + (size_t)p * (C::BM * C::BN), 0, BYTES, 0x00027000); };
-  // a vector is four rows of one column; one that lies past the last row is neither stored nor read (an offset past the records)
-  const int below = C::EDGE ? t.rows - row0 - 4 * (lane >> 4) : C::BM;
+  // a vector is four columns of one row; one that lies past the last row is neither stored nor read (an offset past the records)
+  const int below = C::EDGE ? t.rows - row0 - (lane & 15) : C::BM;
   const __amdgpu_buffer_rsrc_t own = rsrc(part);
 #pragma unroll
   for (int mi = 0; mi < C::MI; ++mi)
@@ -545,7 +570,7 @@ __device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* poo
     }
   __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): acknowledged
   __syncthreads();
-  uint32_t* const shared = reinterpret_cast<uint32_t*>(pool + C::EP_BYTES);
+  uint32_t* const shared = reinterpret_cast<uint32_t*>(pool);
   if (tid == 0) *shared = count_in(t.counters + cut * COUNTER_STRIDE, part, t.parts, part < C::MI);
   __syncthreads();
   const uint32_t shares = (uint32_t)__builtin_amdgcn_readfirstlane((int)*shared);
@@ -573,13 +598,7 @@ __device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* poo
 #pragma unroll
         for (int ni = 0; ni < C::NI; ++ni) sum[ni] += __builtin_bit_cast(f32x4, v[p][ni]);
     }
-#pragma unroll
-    for (int ni = 0; ni < C::NI; ++ni)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ep[(4 * (lane >> 4) + e) * C::EP_STRIDE + ni * 16 + (lane & 15)] = sum[ni][e];
-    __builtin_amdgcn_wave_barrier();
-    finish_rows<C>(t, job, ep, 16, row0 + mi * 16, n0, lane, wave);
-    __builtin_amdgcn_wave_barrier();
+    finish_rows16<C>(t, job, sum, row0 + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
   }
 }
 
@@ -626,27 +645,28 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
       for (int e = 0; e < 4; ++e) acc[mi][ni][e] = 0.f;
   pipe.start(t);
   pipe.run(t, acc);
-  flux::wait_vm0_and_barrier();          // the staging area lies over slabs that other waves may still be reading
-
-  // Through LDS, 32 rows at a time: a lane of a 16x16 block holds four rows of one column and gets eight columns of one row.
-  float* const ep = reinterpret_cast<float*>(pool) + wave * (32 * C::EP_STRIDE);
+  flux::wait_vm_at_most<0>();            // nothing of this wave is left in flight towards LDS that it gives up
   if (is_cut) {
-    finish_cut<C>(t, pool, ep, acc, cut, part, job, m0, n0, lane, wave);
+    __syncthreads();                     // (a word of LDS is used again)
+    finish_cut<C>(t, pool, acc, cut, part, job, m0, n0, lane, wave);
     return;
   }
+  // (A loop in the code too, its block of accumulators picked by a branch: unrolled, the activations of a gated tile are over 100 KB of
+  // instructions.)
+#pragma unroll 1
+  for (int mi = 0; mi < C::MI; ++mi) {
+    f32x4 x[C::NI];
+    flux::static_for<C::MI>([&](auto k_) {
+      constexpr int k = decltype(k_)::value;
+      if (mi == k) {
 #pragma unroll
-  for (int mb = 0; mb < C::WTM / 32; ++mb) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int ni = 0; ni < C::NI; ++ni) {
-        asm volatile("" : "+a"(acc[2 * mb + s][ni]));      // (it stays in its accumulation registers until here)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ep[(16 * s + 4 * (lane >> 4) + e) * C::EP_STRIDE + ni * 16 + (lane & 15)] = acc[2 * mb + s][ni][e];
+        for (int ni = 0; ni < C::NI; ++ni) {
+          asm volatile("" : "+a"(acc[k][ni]));       // (it stays in its accumulation registers until here)
+          x[ni] = acc[k][ni];
+        }
       }
-    __builtin_amdgcn_wave_barrier();
-    finish_rows<C>(t, job, ep, 32, m0 + (wave >> 1) * C::WTM + mb * 32, n0, lane, wave);
-    __builtin_amdgcn_wave_barrier();
+    });
+    finish_rows16<C>(t, job, x, m0 + (wave >> 1) * C::WTM + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
   }
 }
 
