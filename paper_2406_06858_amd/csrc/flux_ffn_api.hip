@@ -93,11 +93,13 @@ struct Plan {
 static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Estimated us of a product: rounds of workgroups, each its slabs and its ends.
+// Estimated us of a product: whole rounds of workgroups, a last one that is not full, the cut tiles.
 static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int parts, int slabs, int part_slabs) {
-  if (cut == 0 && full <= 256) return slabs * p.alone_us + p.ends_us;
-  const double us = ceil_div(full, 256 * sh.per_unit) * (slabs * p.slab_us + p.ends_us);
-  return cut == 0 ? us : us + part_slabs * (cut * parts <= 256 ? p.alone_us : p.slab_us) + p.ends_us + p.join_us;
+  const int at_once = 256 * sh.per_unit, last = full % at_once;
+  const auto pace = [&](int n) { return p.alone_us + (p.slab_us - p.alone_us) * std::min(1.0, (double)n / at_once); };
+  double us = full / at_once * (slabs * p.slab_us + p.ends_us);
+  if (last != 0) us += slabs * pace(last) + p.ends_us;
+  return cut == 0 ? us : us + part_slabs * pace(cut * parts) + p.ends_us + p.join_us;
 }
 
 // depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
@@ -190,12 +192,12 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partia
   t.tiles_m = pl.tiles_m;
   t.tiles_n = pl.tiles_n;
   t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
-  // Pieces of 64 bytes that are whole ones may go past the caches, which then keep the operands' panels; pieces that are not may not, and a
-  // plain product of a short contraction has more results than panels.  us, past the caches / kept there: gated 4-bit 8192x4096x1024 57.7 / 66,
-  // bf16 8192x4096x512 78 / 85; plain 4-bit 8192x8192x512 69 / 44, x4096 158 / 140, 8192x12288x6144 322 / 336; ragged weights' gradients
-  // 1496x3400x5112 135 / 125.
+  // Whole lines of results may go past the caches, which then keep the operands' panels.  Where rows are no whole lines they may not, nor
+  // where the contraction of a plain product is short: it has more results than panels.  us, past the caches / kept there: 4-bit
+  // 8192x12288x6144 281 / 303, 8192x8192x512 55 / 44, gated 8192x4096x1024 62 / 68; gradients of 8192x3584x8192 1318 / 1342, of
+  // 1496x3400x5112 261 / 250.
   const int size = t.out_f32 ? 4 : 2;
-  t.stream = t.ld * size % 64 == 0 && aligned(t.out[0], 64) && aligned(t.out[1], 64) && aligned(t.g, 64) && aligned(t.u, 64) &&
+  t.stream = t.ld * size % 128 == 0 && aligned(t.out[0], 128) && aligned(t.out[1], 128) && aligned(t.g, 128) && aligned(t.u, 128) &&
              (halves_of(kind) == 2 || t.slabs >= 20);
   t.counters = static_cast<uint32_t*>(ws);
   t.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_at);

@@ -414,13 +414,33 @@ struct Pipe {
 // ---- results ---------------------------------------------------------------------------------------------------
 // Nothing passes through LDS.  The columns' fragment goes first into the MFMAs, so a lane holds four consecutive columns of row
 // lane % 16: 16 bytes of an fp32 result.  For bf16 one swap of neighbouring 16-lane rows between two blocks of columns makes that eight.
-// Either way four lanes have 64 bytes of a row side by side.
-//
-// us a tile's ends took through LDS, 256 bytes of a row side by side, and take here: 4-bit 256x256 8.0 / 6.4.  (Pieces exchanged so that a
-// store is eight rows by 128 bytes: the same where results are kept in the caches, 5-8 % slower for gated products.)
+// Either way four lanes have 64 bytes of a row side by side, a piece.  Of two pieces that are neighbours, lanes 8..15 of every 16 of the one
+// change places with lanes 0..7 of the other, and either store is eight rows by 128 bytes.
 __device__ __forceinline__ void store16(void* p, bool stream, const u32x4& v) {
   if (stream) flux::st_stream16(p, make_uint4(v[0], v[1], v[2], v[3]));
   else *static_cast<u32x4*>(p) = v;
+}
+// The pieces x and y, which lie side by side from byte `at` of the wave's rows row0 .. row0 + 15 on; in_piece: where the lane's 16 bytes lie.
+template <bool EDGE>
+__device__ __forceinline__ void store_pair(const TileArgs& t, void* out, int size, const u32x4& x, const u32x4& y, int row0, int col0, int lane, int in_piece) {
+  u32x4 a, b;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    constexpr int ROR8 = 0x128;
+    a[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)x[e], (int)y[e], ROR8, 0xf, 0xc, false);
+    b[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)y[e], (int)x[e], ROR8, 0xf, 0x3, false);
+  }
+  const int row = row0 + (lane & 7), off = col0 * size + (lane & 8) * 8 + in_piece;
+  const long long pitch = t.ld * size;
+  char* const to = static_cast<char*>(out) + row * pitch + off;
+  const bool in = !EDGE || off < t.cols * size;
+  if (in && (!EDGE || row < t.rows)) store16(to, t.stream, a);
+  if (in && (!EDGE || row + 8 < t.rows)) store16(to + 8 * pitch, t.stream, b);
+}
+template <bool EDGE>
+__device__ __forceinline__ void store_piece(const TileArgs& t, void* out, int size, const u32x4& x, int row0, int col0, int lane, int in_piece) {
+  const int row = row0 + (lane & 15), off = col0 * size + in_piece;
+  if (!EDGE || (row < t.rows && off < t.cols * size)) store16(static_cast<char*>(out) + row * (t.ld * size) + off, t.stream, x);
 }
 __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return u32x4{flux::pack_bf16x2(v[0], v[1]), flux::pack_bf16x2(v[2], v[3]), flux::pack_bf16x2(v[4], v[5]), flux::pack_bf16x2(v[6], v[7])};
@@ -452,59 +472,74 @@ __device__ __forceinline__ void gate(int which, float (&v)[N], const float (&u)[
 
 // 16 rows of the wave's part of the tile, out of its accumulators
 template <class C>
-__device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const f32x4 (&acc)[C::NI], int row, int col0, int lane) {
-  const int g = lane >> 4;
-  row += lane & 15;
-  if (C::EDGE && row >= t.rows) return;                 // (lanes that swap are of one row)
-  const long long row_at = row * t.ld;
+__device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+  const int g = lane >> 4, row = row0 + (lane & 15), in_bf16 = (g & 1) * 32 + (g >> 1) * 16;
+  const auto bf16 = [&](void* out, int col, const u32x4 (&p)[C::NIH / 2]) {
+    if constexpr (C::NIH == 2) {
+      store_piece<C::EDGE>(t, out, 2, p[0], row0, col, lane, in_bf16);
+    } else {
+#pragma unroll
+      for (int n = 0; n < C::NIH / 2; n += 2) store_pair<C::EDGE>(t, out, 2, p[n], p[n + 1], row0, col + n * 32, lane, in_bf16);
+    }
+  };
   if constexpr (C::HALVES == 2) {
     if (t.g != nullptr) {
 #pragma unroll
-      for (int n = 0; n < C::NI; n += 2) {
-        const int col = col0 + n % C::NIH * 16 + 16 * (g & 1) + 8 * (g >> 1);
-        float v[8];
-        eight_columns(acc[n], acc[n + 1], v);
-        if (C::EDGE && col >= t.cols) continue;
-        store16((n < C::NIH ? t.g : t.u) + row_at + col, t.stream, pack8(v));
+      for (int h = 0; h < 2; ++h) {
+        u32x4 p[C::NIH / 2];
+#pragma unroll
+        for (int n = 0; n < C::NIH; n += 2) {
+          float v[8];
+          eight_columns(acc[h * C::NIH + n], acc[h * C::NIH + n + 1], v);
+          p[n / 2] = pack8(v);
+        }
+        bf16(h ? t.u : t.g, col0, p);
       }
     }
   }
   if (!t.out_f32) {
+    u32x4 p[C::NIH / 2];
 #pragma unroll
     for (int n = 0; n < C::NIH; n += 2) {
-      const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
-      __bf16* const to = static_cast<__bf16*>(t.out[job]) + row_at + col;
       float v[8];
       eight_columns(acc[n], acc[n + 1], v);
       if constexpr (C::HALVES == 2) {
         float u[8];
         eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
         gate(t.act, v, u);
-      }
-      if (C::EDGE && col >= t.cols) continue;
-      if (C::HALVES == 1 && t.accumulate) {
-        const bf16x8 o = *reinterpret_cast<const bf16x8*>(to);
+      } else if (t.accumulate) {
+        const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
+        if (!C::EDGE || (row < t.rows && col < t.cols)) {
+          const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(t.out[job]) + row * t.ld + col);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
+          for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
+        }
       }
-      store16(to, t.stream, pack8(v));
+      p[n / 2] = pack8(v);
     }
+    bf16(t.out[job], col0, p);
   } else {
 #pragma unroll
-    for (int n = 0; n < C::NIH; ++n) {
-      const int col = col0 + n * 16 + 4 * g;
-      if (C::EDGE && col >= t.cols) continue;
-      float* const to = static_cast<float*>(t.out[job]) + row_at + col;
-      float v[4] = {acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
-      if constexpr (C::HALVES == 2) {
-        const float u[4] = {acc[C::NIH + n][0], acc[C::NIH + n][1], acc[C::NIH + n][2], acc[C::NIH + n][3]};
-        gate(t.act, v, u);
-      } else if (t.accumulate) {
-        const f32x4 o = *reinterpret_cast<const f32x4*>(to);
+    for (int n = 0; n < C::NIH; n += 2) {
+      u32x4 p[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += o[e];
+      for (int h = 0; h < 2; ++h) {
+        float v[4] = {acc[n + h][0], acc[n + h][1], acc[n + h][2], acc[n + h][3]};
+        if constexpr (C::HALVES == 2) {
+          const f32x4& y = acc[C::NIH + n + h];
+          const float u[4] = {y[0], y[1], y[2], y[3]};
+          gate(t.act, v, u);
+        } else if (t.accumulate) {
+          const int col = col0 + (n + h) * 16 + 4 * g;
+          if (!C::EDGE || (row < t.rows && col < t.cols)) {
+            const f32x4 o = *reinterpret_cast<const f32x4*>(static_cast<const float*>(t.out[job]) + row * t.ld + col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[e];
+          }
+        }
+        p[h] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
       }
-      store16(to, t.stream, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+      store_pair<C::EDGE>(t, t.out[job], 4, p[0], p[1], row0, col0 + n * 16, lane, g * 16);
     }
   }
 }
