@@ -99,7 +99,7 @@ static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int par
   const auto pace = [&](int n) { return p.alone_us + (p.slab_us - p.alone_us) * std::min(1.0, (double)n / at_once); };
   double us = full / at_once * (slabs * p.slab_us + p.ends_us);
   if (last != 0) us += slabs * pace(last) + p.ends_us;
-  return cut == 0 ? us : us + part_slabs * pace(cut * parts) + p.ends_us + p.join_us;
+  return cut == 0 ? us : us + part_slabs * pace(cut * parts) + p.ends_us + p.join_us + p.join_all_us * cut * parts / at_once;
 }
 
 // depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
@@ -153,8 +153,12 @@ static Plan plan_mx4(int op, const flux_mx4_t* p) {
   return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2), p->tile_config, p->split_k);
 }
 
-// Rows of dG and of dU in the workspace start at multiples of 16 bytes (N % 8 == 0).
-static size_t slope_bytes(const flux_glu_t* p) { return 4ull * p->M * p->N; }
+// Rows of dG and of dU in the workspace are whole lines of 128 bytes: loads of a slab, 128 bytes a row, are one line each then.
+static long long pitch_d(const flux_glu_t* p) {
+  const long long whole = (p->N + 63ll) / 64 * 64;
+  return p->M * whole < LIMIT ? whole : p->N;          // (offsets are 32 bits)
+}
+static size_t slope_bytes(const flux_glu_t* p) { return 4ull * p->M * pitch_d(p); }
 
 // The workspace: a word a cut tile, zero between calls; then dG and dU (backward); then the cut tiles' sums.
 constexpr size_t WS_HEADER = 512 * COUNTER_STRIDE * 4;
@@ -311,9 +315,10 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   d.U = static_cast<const __bf16*>(U);
   d.dH = static_cast<const __bf16*>(dH);
   d.dG = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + WS_HEADER);
-  d.dU = d.dG + (long long)p->M * p->N;
+  const long long ld = pitch_d(p);
+  d.dU = d.dG + p->M * ld;
   d.ldh = pitch_h(p);
-  d.ldd = p->N;
+  d.ldd = ld;
   d.M = p->M;
   d.N = p->N;
   const dim3 grid((unsigned)(((long long)p->M * p->N / 8 + 255) / 256));
@@ -323,14 +328,14 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   FFN_HIP(hipGetLastError());
   const long long lw = pitch_w(p), lx = pitch_x(p);
   const uint32_t bytes_w = p->w_is_nk ? extent(p->N, lw * 2, p->K * 2ll) : extent(p->K, lw * 2, p->N * 2ll);
-  const uint32_t bytes_d = (uint32_t)((long long)p->M * p->N * 2), bytes_x = extent(p->M, lx * 2, p->K * 2ll);
+  const uint32_t bytes_d = extent(p->M, ld * 2, p->N * 2ll), bytes_x = extent(p->M, lx * 2, p->K * 2ll);
   if (dX != nullptr) {
     TileArgs t = {};
     t.a[0] = d.dG;
     t.a[1] = d.dU;
     t.b[0] = Wg;
     t.b[1] = Wu;
-    t.pitch_a = (uint32_t)p->N * 2u;
+    t.pitch_a = (uint32_t)(ld * 2);
     t.pitch_b = (uint32_t)(lw * 2);
     t.bytes_a = bytes_d;
     t.bytes_b = bytes_w;
@@ -350,9 +355,9 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
       t.a[h] = p->w_is_nk ? dgu[h] : X;
       t.b[h] = p->w_is_nk ? X : dgu[h];
     }
-    const uint32_t pitch_d = (uint32_t)p->N * 2u, pitch = (uint32_t)(lx * 2);
-    t.pitch_a = p->w_is_nk ? pitch_d : pitch;
-    t.pitch_b = p->w_is_nk ? pitch : pitch_d;
+    const uint32_t pitch = (uint32_t)(ld * 2), pitch_of_x = (uint32_t)(lx * 2);
+    t.pitch_a = p->w_is_nk ? pitch : pitch_of_x;
+    t.pitch_b = p->w_is_nk ? pitch_of_x : pitch;
     t.bytes_a = p->w_is_nk ? bytes_d : bytes_x;
     t.bytes_b = p->w_is_nk ? bytes_x : bytes_d;
     t.rows = p->w_is_nk ? p->N : p->K;
