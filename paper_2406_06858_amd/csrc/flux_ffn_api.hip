@@ -123,7 +123,10 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
     for (int parts = 1; parts <= (want_parts ? want_parts : MAX_PARTS); ++parts) {
       int each = ceil_div(slabs, parts);
       if (kind >= MX_GEMM) each += each % 2;                    // (scales come for two slabs)
-      if (parts > 1 && (rest == 0 || parts > MAX_PARTS || (long long)rest * parts > at_once || each < (want_parts ? 1 : 4) || (long long)each * (parts - 1) >= slabs)) continue;
+      if (parts > 1) {
+        if (rest == 0 || parts > MAX_PARTS || (long long)rest * parts > at_once || each < (want_parts ? 1 : 4)) break;
+        if ((long long)each * (parts - 1) >= slabs) continue;          // (a part would be left without slabs)
+      }
       const int cut = parts > 1 ? rest : 0;
       const double us = tile_us(sh, sh.pace[kind >= MX_GEMM], tiles - cut, cut, parts, slabs, each);
       if (pl.slabs != 0 && !want_parts && us >= pl_us) continue;          // (asked for: the most that fit)
@@ -165,10 +168,7 @@ constexpr size_t WS_HEADER = 512 * COUNTER_STRIDE * 4;
 static size_t after_slopes(const flux_glu_t* p) { return WS_HEADER + (slope_bytes(p) + 255) / 256 * 256; }
 static size_t need_of(const Plan& pl) { return pl.cut ? WS_HEADER + pl.partial_bytes : 0; }
 
-static size_t glu_need(int op, const flux_glu_t* p) {
-  if (op == FLUX_GLU_FORWARD) return need_of(plan_glu(p));
-  return after_slopes(p) + std::max(plan_dx(p).partial_bytes, plan_dw(p).partial_bytes);
-}
+static size_t need_of(const flux_glu_t* p, const Plan& dx, const Plan& dw) { return after_slopes(p) + std::max(dx.partial_bytes, dw.partial_bytes); }
 
 static int workspace_ok(size_t need, const void* ws, size_t bytes) {
   if (need == 0) return FLUX_OK;
@@ -215,7 +215,8 @@ static int mx4(int op, const flux_mx4_t* p, const void* Aq, const void* As, cons
   if (st != FLUX_OK) return st;
   for (const void* x : {Aq, As, B0, S0, B1, S1, static_cast<const void*>(out)})
     if (x == nullptr || !aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
-  st = workspace_ok(flux_mx4_workspace_bytes(op, p), ws, bytes);
+  const Plan pl = plan_mx4(op, p);
+  st = workspace_ok(need_of(pl), ws, bytes);
   if (st != FLUX_OK) return st;
   TileArgs t = {};
   t.a[0] = Aq;
@@ -235,7 +236,7 @@ static int mx4(int op, const flux_mx4_t* p, const void* Aq, const void* As, cons
   t.out_f32 = p->out_dtype == FLUX_F32;
   t.ld = p->ldc ? p->ldc : p->N;
   t.out[0] = out;
-  return launch(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, plan_mx4(op, p), t, ws, WS_HEADER, static_cast<hipStream_t>(stream));
+  return launch(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, pl, t, ws, WS_HEADER, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace flux_ffn
@@ -255,7 +256,10 @@ int flux_ffn_tile_config_info(int32_t id, int32_t* tile_m, int32_t* tile_n) {
   return FLUX_OK;
 }
 
-size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p) { return validate(op, p) == FLUX_OK ? glu_need(op, p) : 0; }
+size_t flux_glu_workspace_bytes(int op, const flux_glu_t* p) {
+  if (validate(op, p) != FLUX_OK) return 0;
+  return op == FLUX_GLU_FORWARD ? need_of(plan_glu(p)) : need_of(p, plan_dx(p), plan_dw(p));
+}
 
 size_t flux_mx4_workspace_bytes(int op, const flux_mx4_t* p) { return validate(op, p) == FLUX_OK ? need_of(plan_mx4(op, p)) : 0; }
 
@@ -276,7 +280,8 @@ int flux_glu(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu,
   for (const void* x : {X, Wg, Wu, static_cast<const void*>(H)})
     if (x == nullptr || !aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
   if ((G == nullptr) != (U == nullptr) || !aligned(G, 16) || !aligned(U, 16)) return FLUX_ERR_INVALID_ARG;
-  st = workspace_ok(glu_need(FLUX_GLU_FORWARD, p), workspace, workspace_bytes);
+  const Plan pl = plan_glu(p);
+  st = workspace_ok(need_of(pl), workspace, workspace_bytes);
   if (st != FLUX_OK) return st;
   TileArgs t = {};
   t.a[0] = X;
@@ -296,7 +301,7 @@ int flux_glu(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu,
   t.out[0] = H;
   t.g = static_cast<__bf16*>(G);
   t.u = static_cast<__bf16*>(U);
-  return launch(p->w_is_nk ? GLU_NK : GLU_KN, plan_glu(p), t, workspace, WS_HEADER, static_cast<hipStream_t>(stream));
+  return launch(p->w_is_nk ? GLU_NK : GLU_KN, pl, t, workspace, WS_HEADER, static_cast<hipStream_t>(stream));
 }
 
 int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu, const void* G, const void* U,
@@ -306,7 +311,8 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   for (const void* x : {X, Wg, Wu, G, U, dH})
     if (x == nullptr || !aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
   if ((dWg == nullptr) != (dWu == nullptr) || !aligned(dX, 16) || !aligned(dWg, 16) || !aligned(dWu, 16)) return FLUX_ERR_INVALID_ARG;
-  st = workspace_ok(glu_need(FLUX_GLU_BACKWARD, p), workspace, workspace_bytes);
+  const Plan for_dx = plan_dx(p), for_dw = plan_dw(p);
+  st = workspace_ok(need_of(p, for_dx, for_dw), workspace, workspace_bytes);
   if (st != FLUX_OK) return st;
   if (dX == nullptr && dWg == nullptr) return FLUX_OK;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -345,7 +351,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
     t.out_f32 = p->out_dtype == FLUX_F32;
     t.ld = lx;
     t.out[0] = dX;
-    st = launch(p->w_is_nk ? DX_KN : DX_NK, plan_dx(p), t, workspace, after_slopes(p), s);
+    st = launch(p->w_is_nk ? DX_KN : DX_NK, for_dx, t, workspace, after_slopes(p), s);
     if (st != FLUX_OK) return st;
   }
   if (dWg != nullptr) {
@@ -368,7 +374,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
     t.ld = lw;
     t.out[0] = dWg;
     t.out[1] = dWu;
-    st = launch(DW, plan_dw(p), t, workspace, after_slopes(p), s);
+    st = launch(DW, for_dw, t, workspace, after_slopes(p), s);
     if (st != FLUX_OK) return st;
   }
   return FLUX_OK;
