@@ -62,7 +62,7 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
         objs = list(ex.map(compile_one, units))
     own = len(units) - len(ffn)
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs[:own]])
-    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", FFN_LIB, *objs[own:]])
+    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-z,defs", "-o", FFN_LIB, *objs[own:]])       # (a kernel without its host side is found here)
     return LIB
 
 

@@ -29,7 +29,8 @@ struct FewArgs {
   __bf16 *g, *u;
 };
 
-// BLOCKS: 16-column blocks of products (gated: 2); MB: 16-row blocks; SLABS: 128-byte slabs of a turn; RING: turns in LDS.
+// BLOCKS: 16-column blocks of products (gated: 2); MB: 16-row blocks; SLABS: 128-byte slabs of a turn; RING: turns in LDS, of which up to
+// two hold all that a wave takes of a short row.
 template <bool MX_, int HALVES_, int BLOCKS_, int MB_, int SLABS_, int RING_>
 struct FewCfg {
   static constexpr bool MX = MX_;
@@ -37,12 +38,13 @@ struct FewCfg {
   static constexpr int WAVES = 4, NT = 256, COLS = 16 * BLOCKS / HALVES;
   static constexpr int ROWS = 16 * (BLOCKS + MB);                          // of both operands: the columns' first
   static constexpr int SLAB_BYTES = ROWS * 128;
-  // 4 bits: a row's scales for a turn are 8 bytes a slab, fetched in pieces of 4 (one slab) or 16 (two).
-  static constexpr int SC_ROW = 8 * SLABS, SC_PIECE = SLABS == 2 ? 16 : 4;
-  static constexpr int SC_LOADS = MX ? (ROWS * SC_ROW + 64 * SC_PIECE - 1) / (64 * SC_PIECE) : 0;
-  static constexpr int TURN_BYTES = SLABS * SLAB_BYTES + SC_LOADS * 64 * SC_PIECE;
-  static constexpr int LOADS = SLABS * ROWS / 8 + SC_LOADS;                // of a wave and turn
-  static constexpr int POOL_BYTES = WAVES * RING * TURN_BYTES;
+  // 4 bits: scales of 8192 numbers (a chunk: 256 bytes) of every row at a time, for all waves, into the one of two places while the other
+  // is in use; a load is four rows.
+  static constexpr int CHUNK = 32 / SLABS, SC_BYTES = MX ? ROWS * 256 : 0, SC_LOADS = MX ? ROWS / 16 : 0;      // turns; bytes; loads of a wave
+  static constexpr int TURN_BYTES = SLABS * SLAB_BYTES;
+  static constexpr int LOADS = SLABS * ROWS / 8;                           // of a wave and turn
+  static constexpr int PLACES = RING > 2 || MB == 4 ? 2 : 1;                // (a short row has one chunk)
+  static constexpr int POOL_BYTES = WAVES * RING * TURN_BYTES + PLACES * SC_BYTES;
   static_assert((RING - 1) * LOADS < 64 && POOL_BYTES <= 160 * 1024, "loads in flight, LDS");
   static_assert(POOL_BYTES >= WAVES * MB * BLOCKS * 1024, "room for the waves' sums");
 };
@@ -60,6 +62,8 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
   constexpr uint32_t OUTSIDE = 0xfffffff0u;
   const auto rsrc = [](const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000); };
   const __amdgpu_buffer_rsrc_t ra = rsrc(t.a, t.bytes_a), rb[2] = {rsrc(t.b[0], t.bytes_b), rsrc(t.b[C::HALVES - 1], t.bytes_b)};
+  const __amdgpu_buffer_rsrc_t rsa = rsrc(t.sa, C::MX ? (uint32_t)t.rows * t.pitch_s : 0u);
+  const __amdgpu_buffer_rsrc_t rsb[2] = {rsrc(t.sb[0], C::MX ? (uint32_t)t.cols * t.pitch_s : 0u), rsrc(t.sb[C::HALVES - 1], C::MX ? (uint32_t)t.cols * t.pitch_s : 0u)};
   unsigned char* const mine = pool + wave * (C::RING * C::TURN_BYTES);
 
   // One load is eight rows by 128 bytes; the swizzle is in which 16 bytes a lane fetches.  A lane outside the matrices loads
@@ -84,20 +88,27 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
         }
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // 4 bits: this wave's share of the scales of chunk c.  Piece p (16 bytes, two slabs) of row r lies in place p ^ (r % 16).
+  unsigned char* const scales = pool + C::WAVES * C::RING * C::TURN_BYTES;
+  const auto ask_scales = [&](int c) {
+    const int r = wave * 4 + (lane >> 4);               // in a block of 16, which the l-th load of the four waves is
+    const uint32_t at = (uint32_t)c * 256u + (uint32_t)(((lane & 15) ^ r) * 16);
+    const bool in = at < t.pitch_s;
 #pragma unroll
     for (int l = 0; l < C::SC_LOADS; ++l) {
-      const int piece = l * 64 + lane, r = piece / (C::SC_ROW / C::SC_PIECE), row = r - 16 * C::BLOCKS;
-      const bool is_b = r < 16 * C::BLOCKS;
-      const int half = C::HALVES == 2 ? r / 16 : 0, col = n0 + (C::HALVES == 2 ? r % 16 : r);
-      const uint32_t at = (uint32_t)(q * C::SC_ROW + piece % (C::SC_ROW / C::SC_PIECE) * C::SC_PIECE);
-      const bool in = at < t.pitch_s && (is_b ? col < t.cols : row < t.rows && r < C::ROWS);
-      const uint8_t* const base = is_b ? (half ? t.sb[1] : t.sb[0]) + (uint64_t)(uint32_t)col * t.pitch_s : t.sa + (uint64_t)(uint32_t)row * t.pitch_s;
-      uint64_t p = reinterpret_cast<uint64_t>(base + at);
-      if (!in) p = reinterpret_cast<uint64_t>(&flux::zero_vec);
-      typedef const __attribute__((address_space(1))) void* global_ptr;
-      flux::lds_void_t* const to = (flux::lds_void_t*)(mine + slot * C::TURN_BYTES + C::SLABS * C::SLAB_BYTES + l * 64 * C::SC_PIECE);
-      if constexpr (C::SC_PIECE == 16) __builtin_amdgcn_global_load_lds((global_ptr)p, to, 16, 0, 0);      // (a size has to be a literal)
-      else __builtin_amdgcn_global_load_lds((global_ptr)p, to, 4, 0, 0);
+      unsigned char* const to = scales + c % C::PLACES * C::SC_BYTES + (l * C::WAVES + wave) * 1024;
+      if (l < C::BLOCKS) {
+        const int half = C::HALVES == 2 ? l : 0, col = n0 + (C::HALVES == 2 ? 0 : 16 * l) + r;
+        const uint32_t off = in && col < t.cols ? (uint32_t)col * t.pitch_s + at : OUTSIDE;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb[half], (flux::lds_void_t*)to, 16, (int)off, 0, 0, 0);
+      } else {
+        const int row = 16 * (l - C::BLOCKS) + r;
+        const uint32_t off = in && row < t.rows ? (uint32_t)row * t.pitch_s + at : OUTSIDE;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (flux::lds_void_t*)to, 16, (int)off, 0, 0, 0);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -110,20 +121,23 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
   uint32_t frag[2];
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) frag[ks] = flux::lds_address(mine) + i * 128 + (((C::MX ? 2 * g + ks : ks * 4 + g) ^ swizzle<C::MX>(i)) << 4);
-  const uint32_t scale = flux::lds_address(mine) + C::SLABS * C::SLAB_BYTES + i * C::SC_ROW + 2 * g;
+  const uint32_t scale = flux::lds_address(scales) + i * 256 + 2 * g;
 
-  const auto multiply = [&](int slot) {
+  const auto multiply = [&](int slot, int q) {
     const uint32_t base = (uint32_t)(slot * C::TURN_BYTES);
+    // (the chunk's place; in it the piece of this turn's slabs, and which half of it)
+    const int in_chunk = q % C::CHUNK * C::SLABS;
+    const uint32_t from = scale + (uint32_t)(q / C::CHUNK % C::PLACES * C::SC_BYTES) + (uint32_t)(((in_chunk >> 1) ^ i) << 4) + (uint32_t)((in_chunk & 1) * 8);
     flux::static_for<C::SLABS>([&](auto s_) {
       constexpr int s = decltype(s_)::value;
       u32x4 f[2][C::BLOCKS + C::MB];
       uint32_t sc[C::MX ? C::BLOCKS + C::MB : 1];
-      const uint32_t f0 = frag[0] + base, f1 = frag[1] + base, fs = scale + base + s * 8;
+      const uint32_t f0 = frag[0] + base, f1 = frag[1] + base, fs = from + s * 8;
       flux::static_for<C::BLOCKS + C::MB>([&](auto b_) {
         constexpr int b = decltype(b_)::value, OFF = s * C::SLAB_BYTES + b * 2048;
         lds_read16<OFF>(f[0][b], f0);
         lds_read16<OFF>(f[1][b], f1);
-        if constexpr (C::MX) lds_read2<b * 16 * C::SC_ROW>(sc[b], fs);
+        if constexpr (C::MX) lds_read2<b * 16 * 256>(sc[b], fs);
       });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
@@ -151,14 +165,21 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
   };
 
   const int turns = (t.row_vecs + 8 * C::SLABS - 1) / (8 * C::SLABS);
+  if constexpr (C::MX) ask_scales(0);
 #pragma unroll
   for (int j = 0; j < C::RING - 1; ++j) ask(j, wave + j * C::WAVES);
   int slot = 0, next = C::RING - 1;
-  for (int q = wave; q < turns; q += C::WAVES) {
-    ask(next, q + (C::RING - 1) * C::WAVES);            // (a turn past the end is asked for as zeros)
+  // (every wave goes through as many rounds as the first: a chunk begins with a barrier; a turn past the end is asked for as zeros)
+  for (int q0 = 0; q0 < turns; q0 += C::WAVES) {
+    ask(next, q0 + wave + (C::RING - 1) * C::WAVES);
     flux::wait_vm_at_most<(C::RING - 1) * C::LOADS>();
     asm volatile("" ::: "memory");
-    multiply(slot);
+    if (C::MX && q0 % C::CHUNK == 0) {
+      // this chunk's scales are there (older than this turn's loads), everybody's; the place of the chunk before is free
+      flux::barrier_keeping_loads_in_flight();
+      if (C::PLACES > 1 && q0 + C::CHUNK < turns) ask_scales(q0 / C::CHUNK + 1);
+    }
+    multiply(slot, q0 + wave);
     slot = slot + 1 == C::RING ? 0 : slot + 1;
     next = next + 1 == C::RING ? 0 : next + 1;
   }

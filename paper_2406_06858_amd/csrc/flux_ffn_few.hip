@@ -12,12 +12,20 @@ static hipError_t go(const FewArgs& a, hipStream_t s) {
 
 template <bool MX, int HALVES, int BLOCKS>
 static hipError_t by_rows(const FewArgs& a, hipStream_t s) {
-  // Rows of up to 1 KB are two turns of one slab a wave: nothing to look further ahead for, and with half of the LDS two
-  // workgroups share a unit.
-  const bool is_short = a.row_vecs <= 64;
-  if (a.rows <= 16) return is_short ? go<MX, HALVES, BLOCKS, 1, 1, 2>(a, s) : go<MX, HALVES, BLOCKS, 1, 2, 3>(a, s);
-  if (a.rows <= 32) return is_short ? go<MX, HALVES, BLOCKS, 2, 1, 2>(a, s) : go<MX, HALVES, BLOCKS, 2, 1, 4>(a, s);
-  return go<MX, HALVES, BLOCKS, 4, 1, 3>(a, s);
+  // Rows of up to 512 bytes are one turn of one slab a wave, of up to 1 KB two: nothing to look further ahead for, and with less LDS two to
+  // four workgroups share a unit.  us, 4-bit gated 5x10328x544: 4.5 so, 8.8 with a ring for long rows.
+  const bool one = a.row_vecs <= 32, two = a.row_vecs <= 64;
+  if (a.rows <= 16) {
+    if (one) return go<MX, HALVES, BLOCKS, 1, 1, 1>(a, s);
+    if (two) return go<MX, HALVES, BLOCKS, 1, 1, 2>(a, s);
+    if constexpr (MX) return go<MX, HALVES, BLOCKS, 1, 1, 5>(a, s);
+    else return go<MX, HALVES, BLOCKS, 1, 2, 3>(a, s);
+  }
+  if (a.rows <= 32) {
+    if (one) return go<MX, HALVES, BLOCKS, 2, 1, 1>(a, s);
+    return two ? go<MX, HALVES, BLOCKS, 2, 1, 2>(a, s) : go<MX, HALVES, BLOCKS, 2, 1, 4>(a, s);
+  }
+  return go<MX, HALVES, BLOCKS, 4, 1, MX ? 2 : 3>(a, s);
 }
 
 hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s) {
