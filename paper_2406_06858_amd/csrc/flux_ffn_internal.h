@@ -37,6 +37,11 @@ hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s);
 int hip_failed(hipError_t e);
 #define FFN_HIP(call) do { const hipError_t e_ = (call); if (e_ != hipSuccess) return ::flux_ffn::hip_failed(e_); } while (0)
 
+// A matrix spans fewer elements than this.
+constexpr long long LIMIT = 1ll << 31;
+inline bool below_limit(long long rows, long long pitch, long long cols) {
+  return rows == 1 ? cols < LIMIT : pitch < LIMIT && (rows - 1) * pitch + cols < LIMIT;          // (a pitch of any size: no overflow)
+}
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline long long row_bytes(long long K) { return (K + 31) / 32 * 16; }
 inline long long scale_row_bytes(long long K) { return ((K + 31) / 32 + 15) / 16 * 16; }

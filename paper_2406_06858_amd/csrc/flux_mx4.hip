@@ -25,6 +25,10 @@ struct CastArgs {
   uint32_t row_bytes, scale_row_bytes;
 };
 
+// Four waves a workgroup; a grid is at most 2^23 workgroups wide (2^32 threads are too many for the hardware's count).
+constexpr long long GRID_X = 1ll << 23;
+__device__ __forceinline__ long long wave_id() { return ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6); }
+
 __device__ __forceinline__ float from_bf16(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
 // The lane's numbers, zeros past the end of the row.  Rows need no alignment beyond their type's.
@@ -47,9 +51,9 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&x)[PER_LANE]
 template <class T>
 __global__ void __launch_bounds__(256) quantize_kernel(const CastArgs c) {
   const int lane = threadIdx.x & 63;
-  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long w = wave_id();
+  if (w >= (long long)c.rows * c.waves_per_row) return;
   const int row = (int)(w / c.waves_per_row), seg = (int)(w % c.waves_per_row);
-  if (row >= c.rows) return;
   const int k = seg * PER_WAVE + lane * PER_LANE;
   float x[PER_LANE];
   load8(static_cast<const T*>(c.src) + (long long)row * c.ld + k, c.K - k, x);
@@ -109,9 +113,9 @@ constexpr int SEGS = 4;
 template <class T>
 __global__ void __launch_bounds__(256) dequantize_kernel(const CastArgs c) {
   const int lane = threadIdx.x & 63;
-  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long w = wave_id();
+  if (w >= (long long)c.rows * c.waves_per_row) return;
   const int row = (int)(w / c.waves_per_row), seg = (int)(w % c.waves_per_row) * SEGS;
-  if (row >= c.rows) return;
   uint32_t codes[SEGS], e[SEGS];
 #pragma unroll
   for (int s = 0; s < SEGS; ++s) {
@@ -129,9 +133,9 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const CastArgs c) {
 static int cast_args(int32_t rows, int32_t K, int32_t dtype, const void* wide, int64_t ld, const void* q, const void* scales, int segs, CastArgs* c) {
   if (wide == nullptr || q == nullptr || scales == nullptr || (dtype != FLUX_BF16 && dtype != FLUX_F32)) return FLUX_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(scales, 16) || !aligned(wide, dtype == FLUX_BF16 ? 2 : 4)) return FLUX_ERR_INVALID_ARG;
-  if (rows < 1 || K < 1) return FLUX_ERR_SHAPE;
+  if (rows < 1 || K < 1 || K > (1 << 30)) return FLUX_ERR_SHAPE;          // (what a wave takes of a row may end past the row's end)
   const long long pitch = ld ? ld : K;
-  if (pitch < K || (long long)(rows - 1) * pitch + K >= (1ll << 31)) return FLUX_ERR_SHAPE;
+  if (pitch < K || !below_limit(rows, pitch, K)) return FLUX_ERR_SHAPE;
   c->q = static_cast<uint8_t*>(const_cast<void*>(q));
   c->scales = static_cast<uint8_t*>(const_cast<void*>(scales));
   c->ld = pitch;
@@ -143,7 +147,10 @@ static int cast_args(int32_t rows, int32_t K, int32_t dtype, const void* wide, i
   return FLUX_OK;
 }
 
-static dim3 cast_grid(const CastArgs& c) { return dim3((unsigned)(((long long)c.rows * c.waves_per_row + 3) / 4)); }
+static dim3 cast_grid(const CastArgs& c) {
+  const long long n = ((long long)c.rows * c.waves_per_row + 3) / 4, x = n < GRID_X ? n : GRID_X;
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
 
 }  // namespace flux_ffn
 

@@ -185,3 +185,19 @@ def test_oracle_packing_round_trip():
     assert q.shape == (3, 80) and s.shape == (3, 16) and not s[:, 5:].any()
     c2, s2 = oo.mx4_unpack(q, s)
     assert (c2 == codes).all() and (s2 == scales).all()
+
+
+def test_pitches_and_rows_whose_extent_passes_64_bits():
+    """A row's pitch times the rows may wrap to something small: refused all the same.  So is a row whose last wave would pass 32 bits."""
+    L = ffn.lib()
+    for backward in (False, True):
+        for name in ("ldx", "ldw", "ldh"):
+            p = ffn.glu_problem(5, 128, 256)
+            setattr(p, name, 1 << 62)
+            assert _glu(p, backward=backward) == fb.FLUX_ERR_SHAPE, name
+    p = ffn.mx4_problem(5, 128, 256)
+    p.ldc = 1 << 62
+    assert L.flux_mx4_gemm(ctypes.byref(p), *[PTR] * 5, PTR, 1 << 40, None) == fb.FLUX_ERR_SHAPE
+    for rows, K, ld in ((5, 64, 1 << 62), (1, (1 << 31) - 1, 0), (1, (1 << 30) + 1, 0)):
+        assert L.flux_mx4_quantize(rows, K, 0, PTR, ld, PTR, PTR, None) == fb.FLUX_ERR_SHAPE
+        assert L.flux_mx4_dequantize(rows, K, PTR, PTR, 0, PTR, ld, None) == fb.FLUX_ERR_SHAPE
