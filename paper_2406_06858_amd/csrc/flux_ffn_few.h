@@ -10,6 +10,10 @@
 // come from.  With eight or more lanes to a row it is 110 and 40.  So rows go to LDS as runs of 128 bytes and the operands come out of LDS.
 //
 // bf16: MFMA 16x16x32, a lane of a fragment holds 8 numbers of one row.  4 bits: 16x16x128, a lane holds one block of 32.
+//
+// Measured: gated bf16 1x3584x8192 20 us (5.9 TB/s of weights); 4 bits 8x8192x3584 5.5 us (2.9 TB/s), gated 4 bits 64x3584x8192 10.5 us
+// (2.9 TB/s; each of 224 workgroups reads the 64 rows, 64 MB out of the L2).  The tile kernel with cut tiles took 32, 13.8 and 17.8 us for
+// them, launch included.
 #pragma once
 #include "flux_ffn_tile.h"
 
