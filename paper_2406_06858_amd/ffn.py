@@ -141,20 +141,38 @@ def flux_glu_backward(p, X, Wg, Wu, G, U, dH, dX, dWg, dWu, workspace, stream=No
 
 
 def _rows(t):
-    """(rows, K, dtype, pitch) of a matrix whose rows are runs of memory."""
+    """(rows, K, dtype, pitch) of a matrix whose rows are runs of memory, one behind the other.  (A pitch of 0 would say "packed" to the
+    library, so an expanded row must not get there.)"""
     rows, K = t.shape
-    if K > 1 and t.stride(1) != 1:
+    step, one = t.stride()
+    if K > 1 and one != 1:
         raise ValueError("the rows of the matrix have to be contiguous")
-    return rows, K, _DT[t.dtype], t.stride(0) if rows > 1 else 0
+    if rows > 1 and step < K:
+        raise ValueError("the rows of the matrix overlap")
+    return rows, K, _DT[t.dtype], step if rows > 1 else 0
+
+
+def _whole(t, nbytes, what):
+    """Blocks have no pitch: row r lies r rows behind the first."""
+    if t is not None and not (t.is_contiguous() and t.nbytes >= nbytes):
+        raise ValueError(f"{what} has to be contiguous and hold {nbytes} bytes")
+
+
+def _packed(q, scales, rows, K):
+    blocks = (K + 31) // 32
+    _whole(q, rows * blocks * 16, "q")
+    _whole(scales, rows * ((blocks + 15) // 16 * 16), "scales")
 
 
 def flux_mx4_quantize(src, q, scales, stream=None):
     rows, K, dtype, ld = _rows(src)
+    _packed(q, scales, rows, K)
     _check(lib().flux_mx4_quantize(rows, K, dtype, _ptr(src), ld, _ptr(q), _ptr(scales), _stream(stream)), "flux_mx4_quantize")
 
 
 def flux_mx4_dequantize(q, scales, dst, stream=None):
     rows, K, dtype, ld = _rows(dst)
+    _packed(q, scales, rows, K)
     _check(lib().flux_mx4_dequantize(rows, K, _ptr(q), _ptr(scales), dtype, _ptr(dst), ld, _stream(stream)), "flux_mx4_dequantize")
 
 
