@@ -424,9 +424,9 @@ struct Pipe {
 // Either way four lanes have 64 bytes of a row side by side, a piece.  Of two pieces that are neighbours, lanes 8..15 of every 16 of the one
 // change places with lanes 0..7 of the other, and either store is eight rows by 128 bytes.
 __device__ __forceinline__ void store16(void* p, bool stream, const u32x4& v) {
-  // (written out: of two stores of the same value to the same place the compiler makes one, without the hint; and with the wait state that
-  // a write to the registers of a 16-byte store wants, which the compiler does not see here)
-  if (stream) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 0" : : "v"(p), "v"(v) : "memory");
+  // (written out: of two stores of the same value to the same place the compiler makes one, without the hint; and with the two wait states
+  // that a write to the registers of a 16-byte store wants, which the compiler does not see here)
+  if (stream) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" : : "v"(p), "v"(v) : "memory");
   else *(flux::global_u32x4*)p = v;
 }
 // The pieces x and y, which lie side by side from byte `at` of the wave's rows row0 .. row0 + 15 on; in_piece: where the lane's 16 bytes lie.
