@@ -8,6 +8,7 @@ namespace flux_ffn {
 static thread_local int g_last_hip_error = 0;
 int hip_failed(hipError_t e) {
   g_last_hip_error = (int)e;
+  (void)hipGetLastError();              // (reported here, not again by the caller's next call)
   return FLUX_ERR_HIP;
 }
 
@@ -267,8 +268,7 @@ int flux_ffn_init(void* workspace, size_t workspace_bytes, void* stream) {
   if (!aligned(workspace, 16)) return FLUX_ERR_WORKSPACE;
   const long long vecs = (long long)(std::min(workspace_bytes, WS_HEADER) / 16);           // (nothing else has to be zero)
   if (vecs == 0) return FLUX_OK;
-  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<uint4*>(workspace), vecs);
-  FFN_HIP(hipGetLastError());
+  FFN_HIP(start(zero_kernel, dim3((unsigned)((vecs + 255) / 256)), static_cast<hipStream_t>(stream), static_cast<uint4*>(workspace), vecs));
   return FLUX_OK;
 }
 
@@ -327,10 +327,7 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
   d.M = p->M;
   d.N = p->N;
   const dim3 grid((unsigned)(((long long)p->M * p->N / 8 + 255) / 256));
-  if (p->act == FLUX_ACT_SILU) hipLaunchKernelGGL(slope_kernel<FLUX_ACT_SILU>, grid, dim3(256), 0, s, d);
-  else if (p->act == FLUX_ACT_GELU) hipLaunchKernelGGL(slope_kernel<FLUX_ACT_GELU>, grid, dim3(256), 0, s, d);
-  else hipLaunchKernelGGL(slope_kernel<FLUX_ACT_GELU_TANH>, grid, dim3(256), 0, s, d);
-  FFN_HIP(hipGetLastError());
+  FFN_HIP(start(p->act == FLUX_ACT_SILU ? slope_kernel<FLUX_ACT_SILU> : p->act == FLUX_ACT_GELU ? slope_kernel<FLUX_ACT_GELU> : slope_kernel<FLUX_ACT_GELU_TANH>, grid, s, d));
   const long long lw = pitch_w(p), lx = pitch_x(p);
   const uint32_t bytes_w = p->w_is_nk ? extent(p->N, lw * 2, p->K * 2ll) : extent(p->K, lw * 2, p->N * 2ll);
   const uint32_t bytes_d = extent(p->M, ld * 2, p->N * 2ll), bytes_x = extent(p->M, lx * 2, p->K * 2ll);

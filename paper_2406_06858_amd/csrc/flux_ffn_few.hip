@@ -6,8 +6,8 @@ namespace flux_ffn {
 template <bool MX, int HALVES, int BLOCKS, int MB, int SLABS, int RING>
 static hipError_t go(const FewArgs& a, hipStream_t s) {
   typedef FewCfg<MX, HALVES, BLOCKS, MB, SLABS, RING> C;
-  hipLaunchKernelGGL(few_kernel<C>, dim3((a.cols + C::COLS - 1) / C::COLS), dim3(C::NT), 0, s, a);
-  return hipGetLastError();
+  static_assert(C::NT == 256, "start");
+  return start(few_kernel<C>, dim3((a.cols + C::COLS - 1) / C::COLS), s, a);
 }
 
 template <bool MX, int HALVES, int BLOCKS>

@@ -37,6 +37,14 @@ hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s);
 int hip_failed(hipError_t e);
 #define FFN_HIP(call) do { const hipError_t e_ = (call); if (e_ != hipSuccess) return ::flux_ffn::hip_failed(e_); } while (0)
 
+// A launch of 256 threads a workgroup, with the status of this very launch: the runtime's last error may be an earlier one of the caller's
+// own, which stays the caller's to fetch.
+template <class... A>
+inline hipError_t start(void (*kernel)(A...), dim3 grid, hipStream_t s, A... args) {
+  void* p[] = {static_cast<void*>(&args)...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(256), p, 0, s);
+}
+
 // A matrix spans fewer elements than this.
 constexpr long long LIMIT = 1ll << 31;
 inline bool below_limit(long long rows, long long pitch, long long cols) {

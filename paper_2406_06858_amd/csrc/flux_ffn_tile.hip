@@ -6,9 +6,7 @@ namespace flux_ffn {
 
 template <int BM, int BN, int NA, int NB, int OCC>
 static hipError_t go(const TileArgs& a, bool edge, int grid, hipStream_t s) {
-  if (edge) hipLaunchKernelGGL((tile_kernel<Cfg<FLUX_FFN_KIND, BM, BN, NA, NB, OCC, true>>), dim3(grid), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((tile_kernel<Cfg<FLUX_FFN_KIND, BM, BN, NA, NB, OCC, false>>), dim3(grid), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return start(edge ? tile_kernel<Cfg<FLUX_FFN_KIND, BM, BN, NA, NB, OCC, true>> : tile_kernel<Cfg<FLUX_FFN_KIND, BM, BN, NA, NB, OCC, false>>, dim3(grid), s, a);
 }
 
 #define FFN_CAT2(a, b) a##b

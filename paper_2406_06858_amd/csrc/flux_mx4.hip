@@ -166,9 +166,7 @@ int flux_mx4_quantize(int32_t rows, int32_t K, int32_t src_dtype, const void* sr
   const int st = cast_args(rows, K, src_dtype, src, ld, q, scales, 1, &c);
   if (st != FLUX_OK) return st;
   c.src = src;
-  if (src_dtype == FLUX_BF16) hipLaunchKernelGGL(quantize_kernel<uint16_t>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
-  else hipLaunchKernelGGL(quantize_kernel<float>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
-  FFN_HIP(hipGetLastError());
+  FFN_HIP(start(src_dtype == FLUX_BF16 ? quantize_kernel<uint16_t> : quantize_kernel<float>, cast_grid(c), static_cast<hipStream_t>(stream), c));
   return FLUX_OK;
 }
 
@@ -177,9 +175,7 @@ int flux_mx4_dequantize(int32_t rows, int32_t K, const void* q, const void* scal
   const int st = cast_args(rows, K, dst_dtype, dst, ld, q, scales, SEGS, &c);
   if (st != FLUX_OK) return st;
   c.dst = dst;
-  if (dst_dtype == FLUX_BF16) hipLaunchKernelGGL(dequantize_kernel<uint16_t>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
-  else hipLaunchKernelGGL(dequantize_kernel<float>, cast_grid(c), dim3(256), 0, static_cast<hipStream_t>(stream), c);
-  FFN_HIP(hipGetLastError());
+  FFN_HIP(start(dst_dtype == FLUX_BF16 ? dequantize_kernel<uint16_t> : dequantize_kernel<float>, cast_grid(c), static_cast<hipStream_t>(stream), c));
   return FLUX_OK;
 }
 
