@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
         t.g[to] = (__bf16)v;
         t.u[to] = (__bf16)u;
       }
-      const float a = t.act == FLUX_ACT_SILU ? act<FLUX_ACT_SILU>(v) : t.act == FLUX_ACT_GELU ? act<FLUX_ACT_GELU>(v) : act<FLUX_ACT_GELU_TANH>(v);
+      const float a = t.act == FLUX_ACT_SILU ? act<FLUX_ACT_SILU, true>(v) : t.act == FLUX_ACT_GELU ? act<FLUX_ACT_GELU, true>(v) : act<FLUX_ACT_GELU_TANH, true>(v);
       v = a * u;
     }
     if (t.out_f32) static_cast<float*>(t.out)[to] = v;

@@ -465,17 +465,17 @@ __device__ __forceinline__ void eight_columns(const f32x4& x, const f32x4& y, fl
 }
 
 // v = act(v) * u
-template <int N>
+template <bool FINE, int N>
 __device__ __forceinline__ void gate(int which, float (&v)[N], const float (&u)[N]) {
   if (which == FLUX_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_SILU>(v[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_SILU, FINE>(v[e]) * u[e];
   } else if (which == FLUX_ACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU>(v[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU, FINE>(v[e]) * u[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU_TANH>(v[e]) * u[e];
+    for (int e = 0; e < N; ++e) v[e] = act<FLUX_ACT_GELU_TANH, FINE>(v[e]) * u[e];
   }
 }
 
@@ -515,7 +515,7 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const 
       if constexpr (C::HALVES == 2) {
         float u[8];
         eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
-        gate(t.act, v, u);
+        gate<false>(t.act, v, u);
       } else if (t.accumulate) {
         const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
         if (!C::EDGE || (row < t.rows && col < t.cols)) {
@@ -537,7 +537,7 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const 
         if constexpr (C::HALVES == 2) {
           const f32x4& y = acc[C::NIH + n + h];
           const float u[4] = {y[0], y[1], y[2], y[3]};
-          gate(t.act, v, u);
+          gate<true>(t.act, v, u);
         } else if (t.accumulate) {
           const int col = col0 + (n + h) * 16 + 4 * g;
           if (!C::EDGE || (row < t.rows && col < t.cols)) {
