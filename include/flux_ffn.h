@@ -71,7 +71,8 @@ int flux_glu(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu,
 
 /* Gradients of flux_glu.  G and U are the forward call's; dH [M,N] bf16.  dG and dU are taken in fp32 and rounded to bf16
  * once, as operands of the three products, which accumulate in fp32 and are rounded once at the end (a gradient in fp32 is
- * therefore as exact as bf16 dG and dU make it).  dX, or the pair dWg and dWu, may be NULL and is then not computed.
+ * therefore as exact as bf16 dG and dU make it).  dX, or the pair dWg and dWu, may be NULL and is then not computed;
+ * Wg and Wu are read for dX alone, X for dWg and dWu alone, and may be NULL without it.
  *   workspace         >= flux_glu_workspace_bytes(FLUX_GLU_BACKWARD, p) bytes */
 int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const void* Wu, const void* G, const void* U,
                       const void* dH, void* dX, void* dWg, void* dWu, void* workspace, size_t workspace_bytes, void* stream);

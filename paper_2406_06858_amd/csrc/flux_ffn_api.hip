@@ -307,8 +307,11 @@ int flux_glu_backward(const flux_glu_t* p, const void* X, const void* Wg, const 
                       const void* dH, void* dX, void* dWg, void* dWu, void* workspace, size_t workspace_bytes, void* stream) {
   int st = validate(FLUX_GLU_BACKWARD, p);
   if (st != FLUX_OK) return st;
+  for (const void* x : {G, U, dH})
+    if (x == nullptr) return FLUX_ERR_INVALID_ARG;
+  if ((dX != nullptr && (Wg == nullptr || Wu == nullptr)) || (dWg != nullptr && X == nullptr)) return FLUX_ERR_INVALID_ARG;
   for (const void* x : {X, Wg, Wu, G, U, dH})
-    if (x == nullptr || !aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
+    if (!aligned(x, 16)) return FLUX_ERR_INVALID_ARG;
   if ((dWg == nullptr) != (dWu == nullptr) || !aligned(dX, 16) || !aligned(dWg, 16) || !aligned(dWu, 16)) return FLUX_ERR_INVALID_ARG;
   const Plan for_dx = plan_dx(p), for_dw = plan_dw(p);
   st = workspace_ok(need_of(p, for_dx, for_dw), workspace, workspace_bytes);
