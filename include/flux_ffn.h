@@ -49,8 +49,9 @@ typedef struct flux_glu {
   int32_t dw_accumulate;    /* 1: dWg and dWu are added to what the buffers hold (micro-batches) */
   int64_t ldx, ldw, ldh;    /* pitches: X and dX; Wg, Wu, dWg and dWu; H, G, U and dH           */
   int32_t tile_config;      /* 0 = library picks; else an id from flux_ffn_tile_config_info     */
-  int32_t split_k;          /* 0 = library picks; else the most parts (1..64) that the contraction of the tiles
-                               of a partly filled last round may be cut into; 1 = no cut        */
+  int32_t split_k;          /* 0 = library picks; else the most parts (1..64, more than 16 count as 16) that the contraction of the
+                               tiles of a partly filled last round may be cut into; 1 = no cut.  2 and more ask for tiles:
+                               the kernel for few rows, which cuts nothing, is not picked then */
 } flux_glu_t;
 
 /* Bytes of workspace that `op` wants (0 for a problem that is refused).  A workspace has to go through flux_ffn_init (or be

@@ -107,7 +107,8 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
   const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
-  best.few = config == FEW_CONFIG || (config == 0 && want_parts == 0 && few_fits(kind, rows));
+  // (the kernel for few rows cuts nothing: it is what "no cut" leaves as it is)
+  best.few = config == FEW_CONFIG || (config == 0 && want_parts <= 1 && few_fits(kind, rows));
   if (best.few) return best;
   double best_us = 0;
   for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
