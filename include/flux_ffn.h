@@ -122,7 +122,7 @@ int flux_mx4_glu(const flux_mx4_t* p, const void* Xq, const void* Xs, const void
                  const void* Wus, void* H, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Tile configurations, ids 1 .. count: rows by columns of products (of a gated product half are gate's and half up's), and one,
- * 0 by 0, for products of at most 64 rows whose weights lie along the contraction (4 bits, or [N,K] in flux_glu): it
+ * 0 by 0, for products of at most 64 rows and 2^28 - 16 columns whose weights lie along the contraction (4 bits, or [N,K] in flux_glu): it
  * reads the weights once and is what the library picks there.  FLUX_ERR_UNSUPPORTED where a problem asks for that one and is
  * not of its kind. */
 int flux_ffn_tile_config_count(void);

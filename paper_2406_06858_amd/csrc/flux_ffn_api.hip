@@ -58,7 +58,10 @@ static bool act_ok(int a) { return a >= FLUX_ACT_SILU && a <= FLUX_ACT_GELU_TANH
 
 constexpr int FEW_CONFIG = N_SHAPES + 1;        // id of the kernel for few rows
 static bool choice_ok(int config, int parts) { return config >= 0 && config <= FEW_CONFIG && parts >= 0 && parts <= 64; }
-static bool few_fits(int kind, int rows) { return rows <= FEW_ROWS && (kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU); }
+// (a workgroup of 256 threads has at least 16 columns, and 2^32 threads are too many for a launch)
+static bool few_fits(int kind, int rows, int cols) {
+  return rows <= FEW_ROWS && cols <= (1 << 28) - 16 && (kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU);
+}
 
 static int validate(int op, const flux_glu_t* p) {
   if (p == nullptr || (op != FLUX_GLU_FORWARD && op != FLUX_GLU_BACKWARD)) return FLUX_ERR_INVALID_ARG;
@@ -68,7 +71,7 @@ static int validate(int op, const flux_glu_t* p) {
   if (p->M < 1 || p->N < 1 || p->K < 1 || p->N % 8 != 0 || p->K % 8 != 0) return FLUX_ERR_SHAPE;
   const long long w_rows = p->w_is_nk ? p->N : p->K, w_cols = p->w_is_nk ? p->K : p->N;
   if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), w_rows, w_cols) || !pitch_ok(pitch_h(p), p->M, p->N)) return FLUX_ERR_SHAPE;
-  if (p->tile_config == FEW_CONFIG && (op != FLUX_GLU_FORWARD || !few_fits(p->w_is_nk ? GLU_NK : GLU_KN, p->M))) return FLUX_ERR_UNSUPPORTED;
+  if (p->tile_config == FEW_CONFIG && (op != FLUX_GLU_FORWARD || !few_fits(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N))) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
 
@@ -79,7 +82,7 @@ static int validate(int op, const flux_mx4_t* p) {
   if (p->M < 1 || p->N < 1 || p->K < 1 || p->N % 8 != 0) return FLUX_ERR_SHAPE;
   if (p->M * row_bytes(p->K) >= LIMIT || p->N * row_bytes(p->K) >= LIMIT) return FLUX_ERR_SHAPE;
   if (!pitch_ok(p->ldc ? p->ldc : p->N, p->M, p->N)) return FLUX_ERR_SHAPE;
-  if (p->tile_config == FEW_CONFIG && !few_fits(MX_GEMM, p->M)) return FLUX_ERR_UNSUPPORTED;
+  if (p->tile_config == FEW_CONFIG && !few_fits(MX_GEMM, p->M, p->N)) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
 
@@ -108,7 +111,7 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
   // (the kernel for few rows cuts nothing: it is what "no cut" leaves as it is)
-  best.few = config == FEW_CONFIG || (config == 0 && want_parts <= 1 && few_fits(kind, rows));
+  best.few = config == FEW_CONFIG || (config == 0 && want_parts <= 1 && few_fits(kind, rows, cols));
   if (best.few) return best;
   double best_us = 0;
   for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
