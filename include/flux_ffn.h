@@ -123,8 +123,8 @@ int flux_mx4_glu(const flux_mx4_t* p, const void* Xq, const void* Xs, const void
 
 /* Tile configurations, ids 1 .. count: rows by columns of products (of a gated product half are gate's and half up's), and one,
  * 0 by 0, for products of at most 64 rows and 2^28 - 16 columns whose weights lie along the contraction (4 bits, or [N,K] in flux_glu): it
- * reads the weights once and is what the library picks there.  FLUX_ERR_UNSUPPORTED where a problem asks for that one and is
- * not of its kind. */
+ * reads the weights once, and the library picks it there unless it expects cut tiles to be well ahead (few columns over a long
+ * contraction).  FLUX_ERR_UNSUPPORTED where a problem asks for that one and is not of its kind. */
 int flux_ffn_tile_config_count(void);
 int flux_ffn_tile_config_info(int32_t id, int32_t* tile_m, int32_t* tile_n);
 

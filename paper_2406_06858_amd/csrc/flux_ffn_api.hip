@@ -110,8 +110,19 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
   const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
-  // (the kernel for few rows cuts nothing: it is what "no cut" leaves as it is)
-  best.few = config == FEW_CONFIG || (config == 0 && want_parts <= 1 && few_fits(kind, rows, cols));
+  // Few rows: the kernel that reads weights once and cuts nothing (so "no cut" leaves it as it is), unless cut tiles are well ahead: few
+  // columns over a long contraction give it few workgroups, and above 16 rows all of them read the rows.  The tiles' estimate knows nothing of
+  // memory: it is no less than 3 us and the weights at 5.2 TB/s.  us, few / tiles (bf16, then 4 bits, gated): 1x256x12288 18.9 / 12.4, 7.5 / 9.3;
+  // 64x256x12288 41.3 / 14.6, 13.7 / 10.0; 64x1024x8192 26.5 / 13.4, 10.0 / 11.5; 1x3584x8192 21.7 / 27.4, 8.1 / 12.1; 64x3584x8192 32.0 / 28.7,
+  // 11.8 / 13.9; 64x8192x512 10.2 / 7.3, 7.8 / 5.0.  Over 597 products that the estimates were not fitted to the pick takes 1.7 % (bf16) and 0.8 %
+  // (4 bits) longer in the mean than the faster one; always few would take 22 and 8 %, up to 4.7 times.  (1.3: with less, more products go to
+  // tiles that take longer there.)
+  double few = 0;
+  best.few = config == FEW_CONFIG;
+  if (config == 0 && want_parts <= 1 && few_fits(kind, rows, cols)) {
+    few = few_us(kind, rows, cols, depth / 8);
+    best.few = few <= 1.3 * (3.0 + 2.0 * halves * cols * depth / 5.2e6);
+  }
   if (best.few) return best;
   double best_us = 0;
   for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
@@ -149,6 +160,10 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
     if (best.slabs != 0 && pl_us >= best_us) continue;
     best = pl;
     best_us = pl_us;
+  }
+  if (few > 0 && few <= 1.3 * best_us) {
+    best = Plan();
+    best.few = true;
   }
   return best;
 }

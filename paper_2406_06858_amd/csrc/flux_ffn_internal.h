@@ -32,6 +32,7 @@ FFN_DECLARE(6)
 // Products of at most this many rows whose weights lie along the contraction (GLU_NK and the 4-bit kinds).
 constexpr int FEW_ROWS = 64;
 hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s);
+double few_us(int kind, int rows, int cols, int row_vecs);          // estimate of what that kernel takes
 
 // Remembers a failed runtime call for flux_ffn_last_hip_error and returns the status for it.
 int hip_failed(hipError_t e);
