@@ -128,8 +128,7 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
   for (int i = config ? config - 1 : 0; i < (config ? config : N_SHAPES); ++i) {
     const Shape& sh = SHAPES[i];
     const int sub = sh.bn / halves, tm = ceil_div(rows, sh.bm), tn = ceil_div(cols, sub);
-    const int at_once = 256 * sh.per_unit, tiles = tm * tn * jobs;
-    if ((long long)tm * tn * jobs >= (1ll << 30)) continue;
+    const int at_once = 256 * sh.per_unit, tiles = tm * tn * jobs;          // (results below 2^31 elements, no side over 2^28: below 2^25)
     // Whole rounds of tiles are a workgroup each; what is left over may be cut along the contraction, over no more workgroups than
     // run at once, since its parts wait for each other.
     const int rest = tiles % at_once;

@@ -76,7 +76,7 @@ struct Cfg {
   static constexpr int RS = (NB + 3) / 2, SC_A = BM * 16, SC_B = BN * 16, SC_BYTES = MX ? RS * (SC_A + SC_B) + 1024 : 0;
   static constexpr int POOL_BYTES = RING_BYTES + SC_BYTES;
   static_assert(POOL_BYTES * OCC <= 160 * 1024, "LDS");
-  static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || NA == NB), "rings");
+  static_assert(NB >= 2 && (NA == NB || NA == NB + 1) && (!MX || (NA == NB && NB % 2 == 0)), "rings (4 bits: scales come for two slabs)");
 };
 
 // Which 16-byte slot of a row holds slot s: s ^ swizzle(row).  A fragment's lanes are rows 0..15 of slot q, the next sixteen
@@ -154,7 +154,7 @@ struct Pipe {
   typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX> LdB;
   static constexpr int NA = C::NA, NB = C::NB;
   static constexpr bool A_LEADS = NA > NB;                               // by one slab
-  static constexpr int U = NA != NB ? NA * NB : C::MX && NB % 2 ? 2 * NB : NB;      // slabs after which the rings are where they were
+  static constexpr int U = NA != NB ? NA * NB : NB;      // slabs after which the rings are where they were
   static constexpr int KS = 2;
   static constexpr int G = C::MI * C::NI;                                // MFMAs per k-step
   static constexpr int NF = C::MI + C::NI, NS = C::MX ? NF : 0;          // fragments of a k-step; scales of a slab
