@@ -17,7 +17,9 @@ __global__ void __launch_bounds__(256) zero_kernel(uint4* p, long long n) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// dG = dH U act'(G), dU = dH act(G), rounded to bf16 once: the operands of the three products.  Memory-bound: 8192x3584 46 us (three reads and two
+// dG = dH U act'(G), dU = dH act(G), taken in 32 bits and rounded to bf16 once, since they are operands of the three products: a second
+// MFMA for what the rounding leaves would double the products' work.  It costs the gradients, of either type, 2.3e-3 of their norm
+// against 64 bits, where dG and dU in 32 bits and a gradient in bf16 have 1.7e-3.  Memory-bound: 8192x3584 46 us (three reads and two
 // writes, 6.3 TB/s), 1496x3400 15.6 us.
 struct SlopeArgs {
   const __bf16 *G, *U, *dH;
@@ -214,10 +216,12 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partia
   t.tiles_m = pl.tiles_m;
   t.tiles_n = pl.tiles_n;
   t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
-  // Whole lines of results may go past the caches, which then keep the operands' panels.  Where rows are no whole lines they may not, nor
-  // where the contraction of a plain product is short: it has more results than panels.  us, past the caches / kept there: 4-bit
+  // Results may go past the caches, which then keep the operands' panels.  Where the rows of H, C or the gradients are no whole lines they
+  // may not, nor where the contraction of a plain product is short: it has more results than panels.  us, past the caches / kept there: 4-bit
   // 8192x12288x6144 281 / 303, 8192x8192x512 55 / 44, gated 8192x4096x1024 62 / 68; gradients of 8192x3584x8192 1318 / 1342, of
-  // 1496x3400x5112 261 / 250.
+  // 1496x3400x5112 261 / 250.  G and U go the way of H, also where beside an fp32 H their own rows end in half a line (4096x3616x512 59 / 70,
+  // 4096x3616x2048 127 / 145, 256x128 tiles), and so do the halves of lines that the waves of gated 128-column tiles store in bf16 (with G
+  // and U 2048x8192x1024 77 / 85, 4096x3584x2048 120 / 134; H alone 73 / 75, 112 / 113).
   const int size = t.out_f32 ? 4 : 2;
   t.stream = t.ld * size % 128 == 0 && aligned(t.out[0], 128) && aligned(t.out[1], 128) && aligned(t.g, 128) && aligned(t.u, 128) &&
              (halves_of(kind) == 2 || t.slabs >= 20);

@@ -2,12 +2,13 @@
 //
 // A workgroup takes 16 or 32 columns of products (gated: 16 of gate and the same 16 of up) and the whole contraction, which its
 // four waves share out in turns of 128 or 256 bytes a row; the waves' sums meet in LDS, in ascending order.  Nobody joins
-// anything across workgroups and no barrier stands in the main loop: a wave has LDS of its own and loads of its next turns on
-// their way into it while it multiplies this one.  The rows (up to 16 MB of them) are read by every workgroup, out of the L2.
+// anything across workgroups and no barrier stands in the main loop (4 bits: one in 8192 numbers, for the scales): a wave has LDS of its own
+// and loads of its next turns on their way into it while it multiplies this one.  The rows are read by every workgroup, out of the L2.
 //
 // What bounds it is how a compute unit's loads are answered.  Of a load whose neighbouring lanes lie in different rows, as an
 // MFMA's operand wants them, it answers 16 bytes a clock: 34 GB/s a unit from the L2, 27 from memory, wherever the bytes
-// come from.  With eight or more lanes to a row it is 110 and 40.  So rows go to LDS as runs of 128 bytes and the operands come out of LDS.
+// come from.  With eight or more lanes to a row it is 110 and 40 (one unit's loads in a loop of nothing else; what this kernel reaches in all is in
+// few_us).  So rows go to LDS as runs of 128 bytes and the operands come out of LDS.
 //
 // bf16: MFMA 16x16x32, a lane of a fragment holds 8 numbers of one row.  4 bits: 16x16x128, a lane holds one block of 32.
 //

@@ -25,6 +25,9 @@ static auto by_rows(int rows, int row_vecs, F f) {
 
 template <class F>
 static auto with_config(int kind, int rows, int cols, int row_vecs, F f) {
+  // Plain 4-bit products: 16 columns a workgroup while that gives every unit at most one, 32 beyond.  us, 16 / 32 columns at K = 3584: 8x2048
+  // 3.9 / 4.6, 8x4096 4.1 / 4.9, 8x4104 5.5 / 4.8, 8x8192 6.6 / 5.3, 64x4104 8.5 / 6.6, 8x28672 18.8 / 16.5; at K = 512, where workgroups share a
+  // unit, 8x8192 3.1 / 3.3, 64x8192 6.1 / 4.8.
   if (kind == MX_GEMM) return cols > 256 * 16 ? by_rows<true, 1, 2>(rows, row_vecs, f) : by_rows<true, 1, 1>(rows, row_vecs, f);
   if (kind == MX_GLU) return by_rows<true, 2, 2>(rows, row_vecs, f);
   return by_rows<false, 2, 2>(rows, row_vecs, f);
@@ -39,8 +42,8 @@ hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s) {
 }
 
 // A round of workgroups: its ends, then the weights, as fast as a unit or the memory gives them, and the rows out of the L2.  us and bytes a
-// us, fitted to 1190 products of 1 to 64 rows, 64 to 28672 columns and 128 to 28672 numbers: within 15 % (bf16) and 11 % (4 bits) each, and
-// as near on 597 others.
+// us, fitted to 1190 products of 1 to 64 rows, 64 to 28672 columns and 128 to 28672 numbers: off by 15 % (bf16) and 11 % (4 bits) in the
+// mean square, and no more on 597 others.
 double few_us(int kind, int rows, int cols, int row_vecs) {
   struct Pace { double ends_us, round_us, weights, rows, all; };
   static constexpr Pace paces[2] = {{1.4, 2.1, 43e3, 57e3, 7.0e6}, {1.2, 2.4, 42e3, 46e3, 7.0e6}};

@@ -14,12 +14,17 @@
 //   4 bits   a slab's 128 bytes are 256 numbers, a k-step's MFMA is 16x16x128 with one scale per lane and operand: a lane
 //            holds one block of 32.  Same bytes, same fragment reads and same cycles per slab as bf16, four times the numbers.
 //
-// Measured with random operands (256x256 tiles): gated 4096x3584x8192 with G and U kept 340 us (1.41 PF; MFMA units busy 68 % of the
-// cycles), dX 8192x8192x2*3584 630 us (1.53 PF) and both weights' gradients 638 us (1.51 PF), 4 bits 8192x12288x6144 275 us (4.5 PF; 53 %) and gated
-// 4096x3584x8192 113 us (4.3 PF; 46 %).  What bounds these is power: the card holds 1.7 GHz under the bf16 ones and 1.9 under the 4-bit ones, and
-// 4-bit changes that save cycles at operands of zeros save nothing here.  Conflicts of the LDS: none in bf16, the 17 % of 4 bits are the scales'.
-// Products that fill less than a round of the card are bound by how a unit's loads are answered, about 60 GB/s a unit out of the L2.  Rows
-// that are no whole lines of 128 bytes cost 15 to 30 % (gated backward 1496x3400x5112 beside 1496x3456x5120).
+// Measured with random operands (256x256 tiles), calls in turn: gated 4096x3584x8192 with G and U kept 345 us (1.39 PF), dX
+// 8192x8192x2*3584 622 us (1.55 PF) and both weights' gradients 632 us (1.52 PF), 4 bits 8192x12288x6144 275 to 290 us (4.3 to 4.5 PF) and gated
+// 4096x3584x8192 110 us (4.4 PF).  How busy the MFMA units were, at which clock, in one run of counters: gated 69 % at 1.87 GHz (357 us),
+// gradients 78 % at 1.87 GHz, 4 bits 53 % at 1.94 GHz (287 us), gated 4 bits 47 % at 2.07 GHz (118 us).
+// What bounds the bf16 ones is power: with operands of zeros the gated product takes 282 us, and 14 calls of it back to back take 339 to
+// 446 us as the card's power control lowers the clock and raises it again.  4 bits: power takes 13 to 20 % (zeros: 241 and 96 us), the
+// rest is that a ring of two slabs makes every barrier wait for all loads, those of the scales among them (zeros, us a slab: 1.54; 1.38 without the
+// scales' loads, still waiting for every load; 1.11 without memory traffic).  Conflicts of the LDS: none in bf16, the 17 % of 4 bits are the scales'.
+// Products that fill less than a round of the card wait for their loads: a slab of 256x128 in bf16, 48 KB, takes 0.55 us where few units
+// are at work and 0.78 where all are (fitted, see SHAPES): 87 and 61 GB/s a unit, the latter 16 TB/s out of the L2s together.  Rows
+// that are no whole lines of 128 bytes: gated backward 1496x3400x5112 229 us, 1496x3456x5120 214, most of it dX (115 / 103).
 #pragma once
 #include "flux_device.h"
 #include "flux_ffn_act.h"

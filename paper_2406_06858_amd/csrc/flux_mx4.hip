@@ -108,7 +108,8 @@ __device__ __forceinline__ void store8(const CastArgs& c, int row, int k, uint32
   }
 }
 
-// A wave takes SEGS neighbouring pieces of a row: their loads are out together.
+// A wave takes SEGS neighbouring pieces of a row: their loads are out together.  us by SEGS, 1 / 2 / 4, to bf16: 64x8192 2.9 / 3.3 / 4.0,
+// 1024x8192 6.1 / 5.7 / 5.9, 8192x8192 31.2 / 26.5 / 26.9, 8192x3413 16.3 / 14.7 / 16.1; to fp32: 64x8192 3.1 / 3.5 / 4.1, 8192x8192 105 / 102 / 115.
 constexpr int SEGS = 4;
 template <class T>
 __global__ void __launch_bounds__(256) dequantize_kernel(const CastArgs c) {
