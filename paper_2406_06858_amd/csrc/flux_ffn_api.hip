@@ -52,16 +52,10 @@ static long long pitch_x(const flux_glu_t* p) { return p->ldx ? p->ldx : p->K; }
 static long long pitch_w(const flux_glu_t* p) { return p->ldw ? p->ldw : p->w_is_nk ? p->K : p->N; }
 static long long pitch_h(const flux_glu_t* p) { return p->ldh ? p->ldh : p->N; }
 
-static bool pitch_ok(long long pitch, long long rows, long long cols) {
-  return pitch >= cols && pitch % 8 == 0 && below_limit(rows, pitch, cols);
-}
-static bool dtype_ok(int d) { return d == FLUX_BF16 || d == FLUX_F32; }
 static bool act_ok(int a) { return a >= FLUX_ACT_SILU && a <= FLUX_ACT_GELU_TANH; }
 
-constexpr int FEW_CONFIG = N_SHAPES + 1;        // id of the kernel for few rows
-static bool choice_ok(int config, int parts) { return config >= 0 && config <= FEW_CONFIG && parts >= 0 && parts <= 64; }
 // (a workgroup of 256 threads has at least 16 columns, and 2^32 threads are too many for a launch)
-static bool few_fits(int kind, int rows, int cols) {
+bool few_fits(int kind, int rows, int cols) {
   return rows <= FEW_ROWS && cols <= (1 << 28) - 16 && (kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU);
 }
 
@@ -89,14 +83,7 @@ static int validate(int op, const flux_mx4_t* p) {
 }
 
 // ---- how a product is run --------------------------------------------------------------------------------------
-struct Plan {
-  int shape = 0, full = 0, cut = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0;
-  bool edge = false, few = false;
-  size_t partial_bytes = 0;
-};
-
 static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
-static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Estimated us of a product: whole rounds of workgroups, a last one that is not full, the cut tiles.
 static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int parts, int slabs, int part_slabs) {
@@ -107,9 +94,8 @@ static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int par
   return cut == 0 ? us : us + part_slabs * pace(cut * parts) + p.ends_us + p.join_us + p.join_all_us * cut * parts / at_once;
 }
 
-// depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's.
-static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int want_parts) {
-  const int halves = halves_of(kind), segs = kind == DX_NK || kind == DX_KN ? 2 : 1, jobs = kind == DW ? 2 : 1;
+Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int want_parts, int segs, int jobs) {
+  const int halves = halves_of(kind);
   const int slabs = segs * ceil_div(depth, 64);
   Plan best;
   // Few rows: the kernel that reads weights once and cuts nothing (so "no cut" leaves it as it is), unless cut tiles are well ahead: few
@@ -170,8 +156,8 @@ static Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int 
 }
 
 static Plan plan_glu(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? GLU_NK : GLU_KN, p->M, p->N, p->K, p->tile_config, p->split_k); }
-static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N, p->tile_config, p->split_k); }
-static Plan plan_dw(const flux_glu_t* p) { return plan_tiles(DW, p->w_is_nk ? p->N : p->K, p->w_is_nk ? p->K : p->N, p->M, p->tile_config, p->split_k); }
+static Plan plan_dx(const flux_glu_t* p) { return plan_tiles(p->w_is_nk ? DX_KN : DX_NK, p->M, p->K, p->N, p->tile_config, p->split_k, 2); }
+static Plan plan_dw(const flux_glu_t* p) { return plan_tiles(DW, p->w_is_nk ? p->N : p->K, p->w_is_nk ? p->K : p->N, p->M, p->tile_config, p->split_k, 1, 2); }
 static Plan plan_mx4(int op, const flux_mx4_t* p) {
   return plan_tiles(op == FLUX_MX4_GLU ? MX_GLU : MX_GEMM, p->M, p->N, (int)(row_bytes(p->K) / 2), p->tile_config, p->split_k);
 }
@@ -183,22 +169,14 @@ static long long pitch_d(const flux_glu_t* p) {
 }
 static size_t slope_bytes(const flux_glu_t* p) { return 4ull * p->M * pitch_d(p); }
 
-// The workspace: a word a cut tile, zero between calls; then dG and dU (backward); then the cut tiles' sums.
-constexpr size_t WS_HEADER = 512 * COUNTER_STRIDE * 4;
+// The workspace: the header; then dG and dU (backward); then the cut tiles' sums.
 static size_t after_slopes(const flux_glu_t* p) { return WS_HEADER + (slope_bytes(p) + 255) / 256 * 256; }
 static size_t need_of(const Plan& pl) { return pl.cut ? WS_HEADER + pl.partial_bytes : 0; }
 
 static size_t need_of(const flux_glu_t* p, const Plan& dx, const Plan& dw) { return after_slopes(p) + std::max(dx.partial_bytes, dw.partial_bytes); }
 
-static int workspace_ok(size_t need, const void* ws, size_t bytes) {
-  if (need == 0) return FLUX_OK;
-  return ws != nullptr && aligned(ws, 16) && bytes >= need ? FLUX_OK : FLUX_ERR_WORKSPACE;
-}
-
 // ---- dispatch ------------------------------------------------------------------------------------------------
-static uint32_t extent(long long rows, long long pitch, long long row) { return (uint32_t)((rows - 1) * pitch + row); }
-
-static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partial_at, hipStream_t s) {
+int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partial_at, hipStream_t s) {
   typedef hipError_t (*Launcher)(int, const TileArgs&, bool, int, hipStream_t);
   static constexpr Launcher launchers[KINDS] = {launch_tile0, launch_tile1, launch_tile2, launch_tile3, launch_tile4, launch_tile5, launch_tile6};
   if (pl.few) {
@@ -207,15 +185,7 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partia
     FFN_HIP(launch_few(kind, f, s));
     return FLUX_OK;
   }
-  t.slabs = pl.slabs;
-  t.seg_slabs = (t.depth + 63) / 64;
-  t.full_tiles = pl.full;
-  t.cut_tiles = pl.cut;
-  t.parts = pl.parts;
-  t.part_slabs = pl.part_slabs;
-  t.tiles_m = pl.tiles_m;
-  t.tiles_n = pl.tiles_n;
-  t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
+  set_tiles(t, pl, ws, partial_at);
   // Results may go past the caches, which then keep the operands' panels.  Where the rows of H, C or the gradients are no whole lines they
   // may not, nor where the contraction of a plain product is short: it has more results than panels.  us, past the caches / kept there: 4-bit
   // 8192x12288x6144 281 / 303, 8192x8192x512 55 / 44, gated 8192x4096x1024 62 / 68; gradients of 8192x3584x8192 1318 / 1342, of
@@ -225,8 +195,6 @@ static int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partia
   const int size = t.out_f32 ? 4 : 2;
   t.stream = t.ld * size % 128 == 0 && aligned(t.out[0], 128) && aligned(t.out[1], 128) && aligned(t.g, 128) && aligned(t.u, 128) &&
              (halves_of(kind) == 2 || t.slabs >= 20);
-  t.counters = static_cast<uint32_t*>(ws);
-  t.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_at);
   FFN_HIP(launchers[kind](pl.shape, t, pl.edge, pl.full + pl.cut * pl.parts, s));
   return FLUX_OK;
 }

@@ -30,6 +30,37 @@ FFN_DECLARE(5)
 FFN_DECLARE(6)
 #undef FFN_DECLARE
 
+// How a product is run.
+struct Plan {
+  int shape = 0, full = 0, cut = 0, parts = 1, part_slabs = 0, slabs = 0, tiles_m = 0, tiles_n = 0;
+  bool edge = false, few = false;
+  size_t partial_bytes = 0;
+};
+// depth: pieces of two bytes of (a segment of) the contraction; config, want_parts: the caller's choice, 0 for the library's; segs: segments of the
+// contraction (dX); jobs: products in one grid (dW).
+Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int want_parts, int segs = 1, int jobs = 1);
+int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partial_at, hipStream_t s);
+
+// The workspace begins with a word a cut tile, zero between calls.
+constexpr size_t WS_HEADER = 512 * COUNTER_STRIDE * 4;
+inline void set_tiles(TileArgs& t, const Plan& pl, void* ws, size_t partial_at) {
+  t.slabs = pl.slabs;
+  t.seg_slabs = (t.depth + 63) / 64;
+  t.full_tiles = pl.full;
+  t.cut_tiles = pl.cut;
+  t.parts = pl.parts;
+  t.part_slabs = pl.part_slabs;
+  t.tiles_m = pl.tiles_m;
+  t.tiles_n = pl.tiles_n;
+  t.band = pl.tiles_m < 8 ? pl.tiles_m : 8;
+  t.counters = static_cast<uint32_t*>(ws);
+  t.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_at);
+}
+
+constexpr int FEW_CONFIG = N_SHAPES + 1;        // id of the kernel for few rows
+inline bool choice_ok(int config, int parts) { return config >= 0 && config <= FEW_CONFIG && parts >= 0 && parts <= 64; }
+bool few_fits(int kind, int rows, int cols);
+
 // Products of at most this many rows whose weights lie along the contraction (GLU_NK and the 4-bit kinds).
 constexpr int FEW_ROWS = 64;
 hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s);
@@ -53,6 +84,14 @@ inline bool below_limit(long long rows, long long pitch, long long cols) {
   return rows == 1 ? cols < LIMIT : pitch < LIMIT && (rows - 1) * pitch + cols < LIMIT;          // (a pitch of any size: no overflow)
 }
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline bool pitch_ok(long long pitch, long long rows, long long cols) { return pitch >= cols && pitch % 8 == 0 && below_limit(rows, pitch, cols); }
+inline bool dtype_ok(int d) { return d == FLUX_BF16 || d == FLUX_F32; }
+inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+inline uint32_t extent(long long rows, long long pitch, long long row) { return (uint32_t)((rows - 1) * pitch + row); }
+inline int workspace_ok(size_t need, const void* ws, size_t bytes) {
+  if (need == 0) return FLUX_OK;
+  return ws != nullptr && aligned(ws, 16) && bytes >= need ? FLUX_OK : FLUX_ERR_WORKSPACE;
+}
 inline long long row_bytes(long long K) { return (K + 31) / 32 * 16; }
 inline long long scale_row_bytes(long long K) { return ((K + 31) / 32 + 15) / 16 * 16; }
 

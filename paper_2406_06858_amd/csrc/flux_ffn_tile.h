@@ -59,6 +59,7 @@ struct TileArgs {
   int64_t ld;                    // pitch of the results, elements
   void* out[2];                  // dW: by weight; else [0]
   __bf16 *g, *u;                 // gated: kept for the backward pass, or null
+  const float* addend;           // dX: added to the sums, pitch `ld`; or null
   float* partial;                // [cut_tiles][parts][BM * BN]
   uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
@@ -521,6 +522,13 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const 
         float u[8];
         eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
         gate<false>(t.act, v, u);
+      } else if ((C::KIND == DX_NK || C::KIND == DX_KN) && t.addend != nullptr) {
+        const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
+        if (!C::EDGE || (row < t.rows && col < t.cols)) {
+          const f32x4* const o = reinterpret_cast<const f32x4*>(t.addend + row * t.ld + col);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += o[e / 4][e % 4];
+        }
       } else if (t.accumulate) {
         const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
         if (!C::EDGE || (row < t.rows && col < t.cols)) {
@@ -601,9 +609,9 @@ __device__ __forceinline__ uint32_t count_in(uint32_t* word, int part, int parts
   return mine;
 }
 
-template <class C>
+template <class C, class F>
 __device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* pool, f32x4 (&acc)[C::MI][C::NI], int cut, int part,
-                                           int job, int m0, int n0, int lane, int wave) {
+                                           int job, int m0, int n0, int lane, int wave, const F& finish) {
   constexpr int SC1 = 16, BYTES = C::BM * C::BN * 4;
   const int tid = wave * 64 + lane, row0 = m0 + (wave >> 1) * C::WTM;
   float* const sums = t.partial + (size_t)cut * t.parts * (C::BM * C::BN);
@@ -648,7 +656,7 @@ __device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* poo
 #pragma unroll
         for (int ni = 0; ni < C::NI; ++ni) sum[ni] += __builtin_bit_cast(f32x4, v[p][ni]);
     }
-    finish_rows16<C>(t, job, sum, row0 + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
+    finish(job, sum, row0 + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
   }
 }
 
@@ -659,9 +667,9 @@ __device__ __forceinline__ int by_die(int b, int n) {
   return die * each + (die < more ? die : more) + b / 8;
 }
 
-template <class C>
-__global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
-  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+// One workgroup's tile or part of one; finish(job, sums, row, column, lane) takes 16 rows of a wave's part of the result (see finish_rows16).
+template <class C, class F>
+__device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool, const F& finish) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool is_cut = (int)blockIdx.x >= t.full_tiles;
   int b, cut = 0, part = 0, job = 0;
@@ -698,7 +706,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
   flux::wait_vm_at_most<0>();            // nothing of this wave is left in flight towards LDS that it gives up
   if (is_cut) {
     __syncthreads();                     // (a word of LDS is used again)
-    finish_cut<C>(t, pool, acc, cut, part, job, m0, n0, lane, wave);
+    finish_cut<C>(t, pool, acc, cut, part, job, m0, n0, lane, wave, finish);
     return;
   }
   // (A loop in the code too, its block of accumulators picked by a branch: unrolled, the activations of a gated tile are over 100 KB of
@@ -716,8 +724,14 @@ __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
         }
       }
     });
-    finish_rows16<C>(t, job, x, m0 + (wave >> 1) * C::WTM + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
+    finish(job, x, m0 + (wave >> 1) * C::WTM + mi * 16, n0 + (wave & 1) * (C::SUBN / 2), lane);
   }
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+  tile_body<C>(t, pool, [&](int job, const f32x4 (&x)[C::NI], int row0, int col0, int lane) { finish_rows16<C>(t, job, x, row0, col0, lane); });
 }
 
 }  // namespace flux_ffn

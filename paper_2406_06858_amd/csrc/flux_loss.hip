@@ -1,0 +1,296 @@
+// Softmax cross entropy of a vocabulary projection: checks of arguments, the join of statistics, dispatch.
+#include <algorithm>
+#include "flux_ffn_internal.h"
+#include "flux_loss.h"
+#include "flux_loss_tile.h"
+
+namespace flux_ffn {
+
+hipError_t launch_stats(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
+hipError_t launch_dz(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
+
+// ---- joins ----------------------------------------------------------------------------------------------------
+// lse = m + log(s) over all runs of columns of a row; then the loss.  A workgroup takes ROWS rows, whose statistics lie side by side, and
+// shares out the runs among 256 / ROWS lanes a row; these meet in LDS, in ascending order.
+struct StatsArgs {
+  const float2* stats;           // [runs][rows]
+  int32_t runs, rows, cols;
+  LossArgs loss;
+  float *lse, *logit, *value;
+};
+template <int ROWS>
+__global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
+  constexpr int LANES = 256 / ROWS;
+  __shared__ float2 part[LANES][ROWS];
+  const int r = threadIdx.x % ROWS, lane = threadIdx.x / ROWS, row = blockIdx.x * ROWS + r;
+  float m = -__builtin_inff(), s = 0.f;
+  if (row < a.rows) {
+    for (int i = lane; i < a.runs; i += LANES) {
+      const float2 v = a.stats[(long long)i * a.rows + row];
+      join_stats(m, s, v.x, v.y);
+    }
+  }
+  part[lane][r] = make_float2(m, s);
+  for (int n = LANES / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (lane < n) {
+      join_stats(m, s, part[lane + n][r].x, part[lane + n][r].y);
+      part[lane][r] = make_float2(m, s);
+    }
+  }
+  if (lane != 0 || row >= a.rows) return;
+  const float lse = (__builtin_fabsf(m) == __builtin_inff() ? 0.f : m) + logf(s);
+  bool counts;
+  const int target = target_column(a.loss, row, a.cols, counts);
+  const float z = target >= 0 ? a.logit[row] : 0.f;
+  a.lse[row] = lse;
+  if (target < 0) a.logit[row] = 0.f;
+  if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
+}
+
+struct RanksArgs {
+  const float* lse[FLUX_MAX_RANKS];
+  const float* logit[FLUX_MAX_RANKS];
+  int32_t ranks, rows;
+  LossArgs loss;
+  float *to_lse, *to_logit, *value;
+};
+__global__ void __launch_bounds__(256) ranks_kernel(const RanksArgs a) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= a.rows) return;
+  float m = -__builtin_inff(), s = 0.f, z = 0.f;
+  for (int r = 0; r < a.ranks; ++r) {
+    join_stats(m, s, a.lse[r][row], 1.f);
+    z += a.logit[r][row];
+  }
+  const float lse = (__builtin_fabsf(m) == __builtin_inff() ? 0.f : m) + logf(s);
+  bool counts;
+  (void)target_column(a.loss, row, 0, counts);
+  if (a.to_lse != nullptr) a.to_lse[row] = lse;
+  if (a.to_logit != nullptr) a.to_logit[row] = z;
+  if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
+}
+
+// ---- checks ----------------------------------------------------------------------------------------------------
+static long long pitch_x(const flux_loss_t* p) { return p->ldx ? p->ldx : p->K; }
+static long long pitch_w(const flux_loss_t* p) { return p->ldw ? p->ldw : p->K; }
+static long long vocab_of(const flux_loss_t* p) { return p->vocab ? p->vocab : p->v0 + p->V; }
+constexpr long long MAX_VOCAB = 1ll << 62;
+
+static int validate(int op, const flux_loss_t* p) {
+  if (p == nullptr || (op != FLUX_LOSS_FORWARD && op != FLUX_LOSS_BACKWARD)) return FLUX_ERR_INVALID_ARG;
+  if ((p->target_dtype != FLUX_TARGET_I32 && p->target_dtype != FLUX_TARGET_I64) || !dtype_ok(p->dx_dtype) || !dtype_ok(p->dw_dtype)) return FLUX_ERR_INVALID_ARG;
+  if ((p->dloss_one | 1) != 1 || (p->dw_accumulate | 1) != 1 || p->reserved != 0 || !choice_ok(p->tile_config, p->split_k)) return FLUX_ERR_INVALID_ARG;
+  if (p->ldx < 0 || p->ldw < 0 || p->v0 < 0 || p->vocab < 0 || p->piece < 0) return FLUX_ERR_INVALID_ARG;
+  if (p->M < 1 || p->V < 1 || p->K < 1 || p->K % 8 != 0 || p->piece % 64 != 0) return FLUX_ERR_SHAPE;
+  if (p->v0 > MAX_VOCAB || p->vocab > MAX_VOCAB || vocab_of(p) < p->v0 + p->V) return FLUX_ERR_SHAPE;
+  if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), p->V, p->K)) return FLUX_ERR_SHAPE;
+  if (p->tile_config == FEW_CONFIG) return FLUX_ERR_UNSUPPORTED;
+  return FLUX_OK;
+}
+
+// ---- plans -----------------------------------------------------------------------------------------------------
+static Plan plan_z(const flux_loss_t* p, int cols) { return plan_tiles(LOGITS, p->M, cols, p->K, p->tile_config, p->split_k); }
+static Plan plan_dx(const flux_loss_t* p, int cols) { return plan_tiles(DX_KN, p->M, p->K, (cols + 7) / 8 * 8, 0, 0); }
+static Plan plan_dw(const flux_loss_t* p, int cols) { return plan_tiles(DW, cols, p->K, p->M, 0, 0); }
+
+// Columns of the backward pass's pieces, the last one's apart.
+static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
+static int piece_of(const flux_loss_t* p) {
+  const long long all = whole_lines(p->V);
+  if (p->piece) return (int)std::min<long long>(p->piece, all);
+  const long long most = std::max(2048ll, (128ll << 20) / 2 / p->M / 256 * 256);
+  return (int)std::min(all, most);
+}
+static bool dz_fits(const flux_loss_t* p) { return p->M * (long long)piece_of(p) < LIMIT; }
+static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// The backward pass's workspace: the header, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
+struct Layout { size_t dz, sums, partial, all; };
+static Layout layout(const flux_loss_t* p) {
+  const int piece = piece_of(p), last = p->V - (p->V - 1) / piece * piece;
+  Layout y;
+  y.dz = WS_HEADER;
+  y.sums = y.dz + up256(2ull * p->M * piece);
+  y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
+  size_t most = 0;
+  for (int cols : {std::min(piece, p->V), last})
+    for (const Plan& pl : {plan_z(p, cols), plan_dx(p, cols), plan_dw(p, cols)}) most = std::max(most, pl.partial_bytes);
+  y.all = y.partial + most;
+  return y;
+}
+
+// A forward pass's: the header, the statistics, the cut tiles' sums.
+static int runs_of(const Plan& pl) { return 2 * pl.tiles_n; }
+static size_t stats_bytes(const flux_loss_t* p, const Plan& pl) { return up256(8ull * p->M * runs_of(pl)); }
+
+static LossArgs loss_args(const flux_loss_t* p, const void* target) {
+  LossArgs l = {};
+  l.target = target;
+  l.target_i64 = p->target_dtype == FLUX_TARGET_I64;
+  l.dloss_one = p->dloss_one;
+  l.v0 = p->v0;
+  l.vocab = vocab_of(p);
+  return l;
+}
+
+static TileArgs logits_args(const flux_loss_t* p, const void* X, const void* W, int v, int cols) {
+  TileArgs t = {};
+  const long long lx = pitch_x(p), lw = pitch_w(p);
+  t.a[0] = X;
+  t.b[0] = static_cast<const __bf16*>(W) + v * lw;
+  t.pitch_a = (uint32_t)(lx * 2);
+  t.pitch_b = (uint32_t)(lw * 2);
+  t.bytes_a = extent(p->M, lx * 2, p->K * 2ll);
+  t.bytes_b = extent(cols, lw * 2, p->K * 2ll);
+  t.rows = p->M;
+  t.cols = cols;
+  t.depth = p->K;
+  return t;
+}
+
+}  // namespace flux_ffn
+
+using namespace flux_ffn;
+
+extern "C" {
+
+size_t flux_loss_workspace_bytes(int op, const flux_loss_t* p) {
+  if (validate(op, p) != FLUX_OK) return 0;
+  if (op == FLUX_LOSS_BACKWARD) return dz_fits(p) ? layout(p).all : 0;
+  const Plan pl = plan_z(p, p->V);
+  return WS_HEADER + stats_bytes(p, pl) + pl.partial_bytes;
+}
+
+int flux_loss(const flux_loss_t* p, const void* X, const void* W, const void* target, float* lse, float* logit, float* loss, void* workspace,
+              size_t workspace_bytes, void* stream) {
+  int st = validate(FLUX_LOSS_FORWARD, p);
+  if (st != FLUX_OK) return st;
+  const int target_bytes = p->target_dtype == FLUX_TARGET_I64 ? 8 : 4;
+  if (X == nullptr || W == nullptr || !aligned(X, 16) || !aligned(W, 16) || target == nullptr || !aligned(target, target_bytes)) return FLUX_ERR_INVALID_ARG;
+  if (lse == nullptr || logit == nullptr || !aligned(lse, 4) || !aligned(logit, 4) || !aligned(loss, 4)) return FLUX_ERR_INVALID_ARG;
+  const Plan pl = plan_z(p, p->V);
+  const size_t partial_at = WS_HEADER + stats_bytes(p, pl);
+  st = workspace_ok(partial_at + pl.partial_bytes, workspace, workspace_bytes);
+  if (st != FLUX_OK) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  StatsArgs a = {};
+  a.loss = loss_args(p, target);
+  a.loss.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + WS_HEADER);
+  a.loss.logit = logit;
+  TileArgs t = logits_args(p, X, W, 0, p->V);
+  set_tiles(t, pl, workspace, partial_at);
+  FFN_HIP(launch_stats(pl.shape, t, a.loss, pl.edge, pl.full + pl.cut * pl.parts, s));
+  a.stats = a.loss.stats;
+  a.runs = runs_of(pl);
+  a.rows = p->M;
+  a.cols = p->V;
+  a.lse = lse;
+  a.logit = logit;
+  a.value = loss;
+  if (p->M >= 64) FFN_HIP(start(stats_kernel<16>, dim3(ceil_div(p->M, 16)), s, a));
+  else FFN_HIP(start(stats_kernel<1>, dim3(p->M), s, a));
+  return FLUX_OK;
+}
+
+int flux_loss_join(const flux_loss_t* p, int32_t R, const float* const* lses, const float* const* logits, const void* target, float* lse,
+                   float* logit, float* loss, void* stream) {
+  if (p == nullptr || R < 1 || R > FLUX_MAX_RANKS || lses == nullptr || logits == nullptr || target == nullptr) return FLUX_ERR_INVALID_ARG;
+  if ((p->target_dtype != FLUX_TARGET_I32 && p->target_dtype != FLUX_TARGET_I64) || p->v0 < 0 || p->vocab < 0) return FLUX_ERR_INVALID_ARG;
+  if (p->M < 1 || p->V < 1 || p->v0 > MAX_VOCAB || p->vocab > MAX_VOCAB) return FLUX_ERR_SHAPE;
+  if (!aligned(target, p->target_dtype == FLUX_TARGET_I64 ? 8 : 4)) return FLUX_ERR_INVALID_ARG;
+  RanksArgs a = {};
+  for (int r = 0; r < R; ++r) {
+    if (lses[r] == nullptr || logits[r] == nullptr || !aligned(lses[r], 4) || !aligned(logits[r], 4)) return FLUX_ERR_INVALID_ARG;
+    a.lse[r] = lses[r];
+    a.logit[r] = logits[r];
+  }
+  if (!aligned(lse, 4) || !aligned(logit, 4) || !aligned(loss, 4)) return FLUX_ERR_INVALID_ARG;
+  a.ranks = R;
+  a.rows = p->M;
+  a.loss = loss_args(p, target);
+  a.to_lse = lse;
+  a.to_logit = logit;
+  a.value = loss;
+  FFN_HIP(start(ranks_kernel, dim3(ceil_div(p->M, 256)), static_cast<hipStream_t>(stream), a));
+  return FLUX_OK;
+}
+
+int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const void* target, const float* lse, const float* dloss, void* dX,
+                       void* dW, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = validate(FLUX_LOSS_BACKWARD, p);
+  if (st != FLUX_OK) return st;
+  if (!dz_fits(p)) return FLUX_ERR_SHAPE;
+  const int target_bytes = p->target_dtype == FLUX_TARGET_I64 ? 8 : 4;
+  if (X == nullptr || W == nullptr || !aligned(X, 16) || !aligned(W, 16) || target == nullptr || !aligned(target, target_bytes)) return FLUX_ERR_INVALID_ARG;
+  if (lse == nullptr || dloss == nullptr || !aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dX, 16) || !aligned(dW, 16)) return FLUX_ERR_INVALID_ARG;
+  const Layout y = layout(p);
+  st = workspace_ok(y.all, workspace, workspace_bytes);
+  if (st != FLUX_OK) return st;
+  if (dX == nullptr && dW == nullptr) return FLUX_OK;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  char* const ws = static_cast<char*>(workspace);
+  __bf16* const dz = reinterpret_cast<__bf16*>(ws + y.dz);
+  float* const sums = reinterpret_cast<float*>(ws + y.sums);
+  const long long lx = pitch_x(p), lw = pitch_w(p);
+  const int piece = piece_of(p);
+  for (int v = 0; v < p->V; v += piece) {
+    const int cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
+    const long long ldz = whole_lines(cols);
+    const uint32_t bytes_z = extent(p->M, ldz * 2, held * 2ll);
+    {
+      const Plan pl = plan_z(p, cols);
+      TileArgs t = logits_args(p, X, W, v, cols);
+      set_tiles(t, pl, ws, y.partial);
+      t.ld = ldz;
+      LossArgs l = loss_args(p, target);
+      l.v0 += v;
+      l.lse = lse;
+      l.dloss = dloss;
+      l.dz = dz;
+      FFN_HIP(launch_dz(pl.shape, t, l, pl.edge, pl.full + pl.cut * pl.parts, s));
+    }
+    if (dX != nullptr) {
+      const bool first = v == 0, last = p->V - v <= piece, f32 = p->dx_dtype == FLUX_F32;
+      TileArgs t = {};
+      t.a[0] = dz;
+      t.b[0] = static_cast<const __bf16*>(W) + v * lw;
+      t.pitch_a = (uint32_t)(ldz * 2);
+      t.pitch_b = (uint32_t)(lw * 2);
+      t.bytes_a = bytes_z;
+      t.bytes_b = extent(cols, lw * 2, p->K * 2ll);
+      t.rows = p->M;
+      t.cols = p->K;
+      t.depth = held;
+      t.ld = lx;
+      // sums of pieces stay in fp32: in dX, or in the workspace until the last piece rounds them
+      t.out_f32 = f32 || !last;
+      t.out[0] = f32 || last ? dX : sums;
+      t.accumulate = !first && (f32 || !last);
+      t.addend = !first && !f32 && last ? sums : nullptr;
+      st = launch(DX_KN, plan_dx(p, cols), t, ws, y.partial, s);
+      if (st != FLUX_OK) return st;
+    }
+    if (dW != nullptr) {
+      TileArgs t = {};
+      t.a[0] = dz;
+      t.b[0] = X;
+      t.pitch_a = (uint32_t)(ldz * 2);
+      t.pitch_b = (uint32_t)(lx * 2);
+      t.bytes_a = bytes_z;
+      t.bytes_b = extent(p->M, lx * 2, p->K * 2ll);
+      t.rows = cols;
+      t.cols = p->K;
+      t.depth = p->M;
+      t.out_f32 = p->dw_dtype == FLUX_F32;
+      t.accumulate = p->dw_accumulate;
+      t.ld = lw;
+      t.out[0] = static_cast<char*>(dW) + v * lw * (t.out_f32 ? 4 : 2);
+      st = launch(DW, plan_dw(p, cols), t, ws, y.partial, s);
+      if (st != FLUX_OK) return st;
+    }
+  }
+  return FLUX_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,31 @@
+// Instantiates the tile kernel of logits; compiled once for each of -DFLUX_LOSS_GRADIENT=0 (statistics) and =1 (dZ).
+#include "flux_ffn_internal.h"
+#include "flux_loss_tile.h"
+
+namespace flux_ffn {
+
+template <int BM, int BN, int NA, int NB, int OCC>
+static hipError_t go(const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s) {
+  constexpr bool G = FLUX_LOSS_GRADIENT;
+  return start(edge ? logits_kernel<Cfg<LOGITS, BM, BN, NA, NB, OCC, true>, G> : logits_kernel<Cfg<LOGITS, BM, BN, NA, NB, OCC, false>, G>, dim3(grid), s, a, l);
+}
+
+#if FLUX_LOSS_GRADIENT
+#define LAUNCH launch_dz
+#else
+#define LAUNCH launch_stats
+#endif
+hipError_t LAUNCH(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
+
+hipError_t LAUNCH(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s) {
+  switch (shape) {                     // (SHAPES)
+    case 0: return go<256, 256, 3, 2, 1>(a, l, edge, grid, s);
+    case 1: return go<256, 128, 3, 3, 1>(a, l, edge, grid, s);
+    case 2: return go<128, 128, 2, 2, 2>(a, l, edge, grid, s);
+    case 3: return go<128, 128, 4, 4, 1>(a, l, edge, grid, s);
+    case 4: return go<64, 128, 3, 3, 2>(a, l, edge, grid, s);
+    default: return go<64, 128, 6, 6, 1>(a, l, edge, grid, s);
+  }
+}
+
+}  // namespace flux_ffn

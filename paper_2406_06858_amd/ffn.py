@@ -158,9 +158,9 @@ def _whole(t, nbytes, what):
         raise ValueError(f"{what} has to be contiguous and hold {nbytes} bytes")
 
 
-def _packed(q, scales, rows, K):
+def _packed(q, scales, rows, K, block_bytes=16):
     blocks = (K + 31) // 32
-    _whole(q, rows * blocks * 16, "q")
+    _whole(q, rows * blocks * block_bytes, "q")
     _whole(scales, rows * ((blocks + 15) // 16 * 16), "scales")
 
 

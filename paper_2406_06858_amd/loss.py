@@ -1,0 +1,83 @@
+"""ctypes binding of include/flux_loss.h (in libflux_ffn_mi355.so): the softmax cross entropy of a vocabulary projection, its join over ranks and its
+backward pass.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, or of another device than the current
+one, raises ValueError.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import ffn
+from .binding import _ptr_list
+from .ffn import _check, _stream
+from .norm import _DT, _TYPES, _buf, _device, _space
+
+FLUX_LOSS_FORWARD, FLUX_LOSS_BACKWARD = 0, 1
+FLUX_TARGET_I32, FLUX_TARGET_I64 = 0, 1
+
+EXPORTS = ["flux_loss", "flux_loss_join", "flux_loss_backward", "flux_loss_workspace_bytes"]
+
+
+class flux_loss_t(C.Structure):
+    _fields_ = [
+        ("M", C.c_int32), ("V", C.c_int32), ("K", C.c_int32), ("target_dtype", C.c_int32), ("v0", C.c_int64), ("vocab", C.c_int64),
+        ("dloss_one", C.c_int32), ("dx_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("dw_accumulate", C.c_int32),
+        ("ldx", C.c_int64), ("ldw", C.c_int64), ("piece", C.c_int32), ("tile_config", C.c_int32), ("split_k", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+_lib = None
+
+
+def lib():
+    """The shared library, with this header's functions declared."""
+    global _lib
+    if _lib is None:
+        L = ffn.lib()
+        vp, sz, pl, lists = C.c_void_p, C.c_size_t, C.POINTER(flux_loss_t), C.POINTER(C.c_void_p)
+        L.flux_loss.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.flux_loss_join.argtypes = [pl, C.c_int32, lists, lists, vp, vp, vp, vp, vp]
+        L.flux_loss_backward.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.flux_loss_workspace_bytes.argtypes = [C.c_int, pl]
+        for name in EXPORTS:
+            getattr(L, name).restype = sz if name.endswith("_bytes") else C.c_int
+        _lib = L
+    return _lib
+
+
+_TARGET = {"i32": FLUX_TARGET_I32, "i64": FLUX_TARGET_I64, torch.int32: FLUX_TARGET_I32, torch.int64: FLUX_TARGET_I64}
+_TARGETS = (torch.int32, torch.int64)
+
+
+def loss_problem(M, V, K, v0=0, vocab=0, target_dtype="i64", dloss_one=0, dx_dtype="bf16", dw_dtype="bf16", dw_accumulate=0, ldx=0, ldw=0,
+                 piece=0, tile_config=0, split_k=0) -> flux_loss_t:
+    return flux_loss_t(M, V, K, _TARGET[target_dtype], v0, vocab, dloss_one, _DT[dx_dtype], _DT[dw_dtype], dw_accumulate, ldx, ldw, piece,
+                       tile_config, split_k, 0)
+
+
+def flux_loss_workspace_bytes(op: int, p: flux_loss_t) -> int:
+    return int(lib().flux_loss_workspace_bytes(op, C.byref(p)))
+
+
+def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=None):
+    d, f = _device(), torch.float32
+    _check(lib().flux_loss(C.byref(p), _buf(X, torch.bfloat16, d, "X"), _buf(W, torch.bfloat16, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+                           _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), *_space(workspace, d), _stream(stream)), "flux_loss")
+
+
+def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, stream=None):
+    d, f = _device(), torch.float32
+    if len(lses) != len(logits):
+        raise ValueError("as many lses as logits")
+    for t in (*lses, *logits):
+        _buf(t, f, d, "lses and logits")
+    _check(lib().flux_loss_join(C.byref(p), len(lses), _ptr_list(lses), _ptr_list(logits), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+                                _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), _stream(stream)), "flux_loss_join")
+
+
+def flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace, stream=None):
+    d, b, f = _device(), torch.bfloat16, torch.float32
+    _check(lib().flux_loss_backward(C.byref(p), _buf(X, b, d, "X"), _buf(W, b, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+                                    _buf(lse, f, d, "lse"), _buf(dloss, f, d, "dloss"), _buf(dX, _TYPES[p.dx_dtype & 1], d, "dX"),
+                                    _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_loss_backward")

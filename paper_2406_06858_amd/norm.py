@@ -1,0 +1,101 @@
+"""ctypes binding of include/flux_norm.h (in libflux_ffn_mi355.so): the root-mean-square norm with the residual's addition, its backward pass,
+and 8-bit blocks read back.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, or of another device than the
+current one, raises ValueError.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import ffn
+from .binding import FLUX_BF16, FLUX_F32
+from .ffn import _check, _packed, _rows, _stream, _ws
+
+FLUX_NORM_BF16, FLUX_NORM_F32, FLUX_NORM_MX4, FLUX_NORM_MX8 = range(4)
+
+EXPORTS = ["flux_norm", "flux_norm_backward", "flux_norm_workspace_bytes", "flux_mx8_row_bytes", "flux_mx8_dequantize"]
+
+
+class flux_norm_t(C.Structure):
+    _fields_ = [
+        ("M", C.c_int32), ("K", C.c_int32), ("x_dtype", C.c_int32), ("s_dtype", C.c_int32), ("w_dtype", C.c_int32),
+        ("out", C.c_int32), ("dw_dtype", C.c_int32), ("dw_accumulate", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32),
+        ("ldx", C.c_int64), ("lds", C.c_int64), ("ldy", C.c_int64),
+    ]
+
+
+_lib = None
+
+
+def lib():
+    """The shared library, with this header's functions declared."""
+    global _lib
+    if _lib is None:
+        L = ffn.lib()
+        vp, i32, i64, sz, pn = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.POINTER(flux_norm_t)
+        L.flux_norm.argtypes = [pn, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.flux_norm_backward.argtypes = [pn, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.flux_norm_workspace_bytes.argtypes = [pn]
+        L.flux_mx8_row_bytes.argtypes = [i32]
+        L.flux_mx8_dequantize.argtypes = [i32, i32, vp, vp, i32, vp, i64, vp]
+        for name in EXPORTS:
+            getattr(L, name).restype = sz if name.endswith("_bytes") else C.c_int
+        _lib = L
+    return _lib
+
+
+_DT = {"bf16": FLUX_BF16, "f32": FLUX_F32, torch.bfloat16: FLUX_BF16, torch.float32: FLUX_F32}
+_OUT = {"bf16": FLUX_NORM_BF16, "f32": FLUX_NORM_F32, "mx4": FLUX_NORM_MX4, "mx8": FLUX_NORM_MX8, torch.bfloat16: FLUX_NORM_BF16, torch.float32: FLUX_NORM_F32}
+_TYPES = (torch.bfloat16, torch.float32, torch.uint8, torch.uint8)          # by flux_dtype_t and flux_norm_out_t
+_device = torch._C._cuda_getDevice
+
+
+def _buf(t, dtype, device, what):
+    """The address of a tensor of `dtype` on the current device; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{what} has to be {dtype} on device {device}, not {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _space(workspace, device):
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"the workspace has to be on device {device}, not on {workspace.device}")
+    return _ws(workspace)
+
+
+def norm_problem(M, K, x_dtype="bf16", s_dtype="bf16", out="bf16", w_dtype="bf16", eps=1e-5, dw_dtype="f32", dw_accumulate=0, ldx=0, lds=0,
+                 ldy=0) -> flux_norm_t:
+    return flux_norm_t(M, K, _DT[x_dtype], _DT[s_dtype], _DT[w_dtype], _OUT[out], _DT[dw_dtype], dw_accumulate, eps, 0, ldx, lds, ldy)
+
+
+def flux_norm_workspace_bytes(p: flux_norm_t) -> int:
+    return int(lib().flux_norm_workspace_bytes(C.byref(p)))
+
+
+def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
+    d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
+    _check(lib().flux_norm(C.byref(p), _buf(X, x, d, "X"), _buf(R, s, d, "R"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"), _buf(S, s, d, "S"),
+                           _buf(Y, _TYPES[p.out & 3], d, "Y"), _buf(scales, torch.uint8, d, "scales"), _buf(rstd, torch.float32, d, "rstd"),
+                           _stream(stream)), "flux_norm")
+
+
+def flux_norm_backward(p, dY, S, W, rstd, dS=None, dR=None, dX=None, dW=None, workspace=None, stream=None):
+    d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
+    _check(lib().flux_norm_backward(C.byref(p), _buf(dY, _TYPES[p.out & 1], d, "dY"), _buf(S, s, d, "S"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"),
+                                    _buf(rstd, torch.float32, d, "rstd"), _buf(dS, s, d, "dS"), _buf(dR, s, d, "dR"), _buf(dX, x, d, "dX"),
+                                    _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_norm_backward")
+
+
+def flux_mx8_row_bytes(K: int) -> int:
+    return int(lib().flux_mx8_row_bytes(K))
+
+
+def flux_mx8_dequantize(q, scales, dst, stream=None):
+    rows, K, dtype, ld = _rows(dst)
+    _packed(q, scales, rows, K, 32)
+    d = _device()
+    _check(lib().flux_mx8_dequantize(rows, K, _buf(q, torch.uint8, d, "q"), _buf(scales, torch.uint8, d, "scales"), dtype, _buf(dst, dst.dtype, d, "dst"), ld,
+                                     _stream(stream)), "flux_mx8_dequantize")
