@@ -70,13 +70,15 @@ double few_us(int kind, int rows, int cols, int row_vecs);          // estimate 
 int hip_failed(hipError_t e);
 #define FFN_HIP(call) do { const hipError_t e_ = (call); if (e_ != hipSuccess) return ::flux_ffn::hip_failed(e_); } while (0)
 
-// A launch of 256 threads a workgroup, with the status of this very launch: the runtime's last error may be an earlier one of the caller's
+// A launch of 256 threads a workgroup (or `threads`), with the status of this very launch: the runtime's last error may be an earlier one of the caller's
 // own, which stays the caller's to fetch.
 template <class... A>
-inline hipError_t start(void (*kernel)(A...), dim3 grid, hipStream_t s, A... args) {
+inline hipError_t start_with(void (*kernel)(A...), dim3 grid, int threads, hipStream_t s, A... args) {
   void* p[] = {static_cast<void*>(&args)...};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(256), p, 0, s);
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), p, 0, s);
 }
+template <class... A>
+inline hipError_t start(void (*kernel)(A...), dim3 grid, hipStream_t s, A... args) { return start_with(kernel, grid, 256, s, args...); }
 
 // A matrix spans fewer elements than this.
 constexpr long long LIMIT = 1ll << 31;

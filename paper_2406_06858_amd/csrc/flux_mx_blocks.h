@@ -8,12 +8,15 @@ constexpr int PER_LANE = 8;                      // numbers of a row that a lane
 
 __device__ __forceinline__ float from_bf16(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
-// The lane's numbers, zeros past the end of the row.  Rows need no alignment beyond their type's.
-template <class T>
+// The lane's numbers, zeros past the end of the row.  Rows need no alignment beyond their type's.  WHOLE: `left` is 8 and more, or 0 and less.
+template <bool WHOLE = false, class T>
 __device__ __forceinline__ void load8(const T* p, int left, float (&x)[PER_LANE]) {
   T v[PER_LANE];
   if (left >= PER_LANE) {
     __builtin_memcpy(v, p, sizeof(v));
+  } else if (WHOLE) {
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) v[i] = T(0);
   } else {
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) v[i] = i < left ? p[i] : T(0);
@@ -25,11 +28,44 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&x)[PER_LANE]
   }
 }
 
+// The same, kept as they are in memory, in words, until they are used.
+template <class T>
+struct Raw8 {
+  static constexpr int WORDS = PER_LANE * sizeof(T) / 4;
+  uint32_t v[WORDS];
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const T* p, int left) {
+    if (left >= PER_LANE) {
+      __builtin_memcpy(v, p, sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) v[i] = 0u;
+      if (!WHOLE) {
+#pragma unroll
+        for (int i = 0; i < PER_LANE; ++i) {
+          if (i >= left) continue;
+          if constexpr (sizeof(T) == 2) v[i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
+          else v[i] = __float_as_uint(p[i]);
+        }
+      }
+    }
+  }
+  // What was made of the words so far is forgotten: they alone stay in registers.
+  __device__ __forceinline__ void fold() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) asm volatile("" : "+v"(v[i]));
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(i % 2 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
+    else return __uint_as_float(v[i]);
+  }
+};
+
 // 16 bytes at any address that the matrix's type allows
 typedef uint32_t vec16 __attribute__((ext_vector_type(4), aligned(2)));
 
 // The lane's numbers to a row that has `left` more; STREAM: past the caches.
-template <bool STREAM, class T>
+template <bool STREAM, bool WHOLE = false, class T>
 __device__ __forceinline__ void store8(T* p, int left, const T (&v)[PER_LANE]) {
   if (left >= PER_LANE) {
     vec16 w[sizeof(v) / 16];
@@ -39,7 +75,7 @@ __device__ __forceinline__ void store8(T* p, int left, const T (&v)[PER_LANE]) {
       if (STREAM) __builtin_nontemporal_store(w[i], reinterpret_cast<vec16*>(p) + i);
       else reinterpret_cast<vec16*>(p)[i] = w[i];
     }
-  } else {
+  } else if (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i)
       if (i < left) p[i] = v[i];

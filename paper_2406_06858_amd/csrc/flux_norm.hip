@@ -27,8 +27,8 @@ struct NormGradArgs {
   const void *dy, *s, *w, *ds;
   const float* rstd;
   void *dr, *dx;
-  float* partial;                // [row groups][K]
-  long long ldx, lds, ldy;
+  float* partial;                // [groups of rows], pitch `pitch`; or null
+  long long ldx, lds, ldy, pitch;
   int32_t M, K;
   int32_t w_f32, x_f32;
 };
@@ -46,30 +46,36 @@ __device__ __forceinline__ void round8(const float (&x)[PER_LANE], T (&v)[PER_LA
     else v[i] = __builtin_bit_cast(uint16_t, (__bf16)x[i]);
   }
 }
-template <class T>
+template <class T, bool PAST, bool WHOLE = false>
 __device__ __forceinline__ void write8(void* p, long long at, int left, const float (&x)[PER_LANE]) {
   T v[PER_LANE];
   round8(x, v);
-  store8<false>(static_cast<T*>(p) + at, left, v);
+  store8<PAST, WHOLE>(static_cast<T*>(p) + at, left, v);
 }
 
-// Sum over the workgroup's 256 lanes, everybody's.
-__device__ __forceinline__ float sum_of_256(float v) {
-  __shared__ float part[4];
+// Sum over a row's LANES lanes, everybody's: in a wave by exchange, over waves through LDS, `turn` telling one sum's place from the next one's.
+template <int LANES>
+__device__ __forceinline__ float sum_of(float v, int turn = 0) {
 #pragma unroll
-  for (int n = 1; n < 64; n *= 2) v += __shfl_xor(v, n);
-  __syncthreads();               // (of the sum before)
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
-  __syncthreads();
-  return part[0] + part[1] + part[2] + part[3];
+  for (int n = 1; n < (LANES < 64 ? LANES : 64); n *= 2) v += __shfl_xor(v, n);
+  if constexpr (LANES > 64) {
+    __shared__ float part[2][LANES / 64];
+    if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANES / 64; ++i) v += part[turn][i];
+  }
+  return v;
 }
 
 // Y of a lane: numbers, or its part of a block of 32; k may lie past the row's end, where blocks' padding is.
-__device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, const float (&y)[PER_LANE]) {
+template <bool PAST, bool WHOLE>
+__device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, int left, const float (&y)[PER_LANE]) {
   if (a.out == FLUX_NORM_BF16) {
-    if (k < a.K) write8<uint16_t>(a.y, row * a.ldy + k, a.K - k, y);
+    write8<uint16_t, PAST, WHOLE>(a.y, row * a.ldy + k, left, y);
   } else if (a.out == FLUX_NORM_F32) {
-    if (k < a.K) write8<float>(a.y, row * a.ldy + k, a.K - k, y);
+    write8<float, false, WHOLE>(a.y, row * a.ldy + k, left, y);
   } else {
     const int blocks = (a.K + 31) / 32, row_scales = (blocks + 15) / 16 * 16;
     uint32_t byte;
@@ -85,6 +91,66 @@ __device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, const
 }
 
 // ---- kernels --------------------------------------------------------------------------------------------------
+// The row in registers: LANES lanes a row, VECS pieces of 8 numbers a lane, 256 / LANES rows a workgroup where LANES is less.  WHOLE: K is a multiple of 8,
+// a piece is in the row or is not.
+template <class TX, class TS, bool RESIDUAL, int LANES, int VECS, bool WHOLE>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(const NormArgs a) {
+  constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
+  const int lane = threadIdx.x % LANES, row = blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (row >= a.M) return;                        // (with more than one row a workgroup there is no barrier)
+  const TX* const x = static_cast<const TX*>(a.x) + row * a.ldx;
+  const TS* const r = static_cast<const TS*>(a.r) + row * a.lds;
+  TS* const s = static_cast<TS*>(a.s) + row * a.lds;
+  const auto left = [&](int k) { return WHOLE ? (k < a.K ? PER_LANE : 0) : a.K - k; };
+  float v[VECS][PER_LANE], w[VECS][PER_LANE];
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+    load8<WHOLE>(x + k, left(k), v[i]);
+  }
+  if constexpr (RESIDUAL) {
+    float u[VECS][PER_LANE];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int k = (i * LANES + lane) * PER_LANE;
+      load8<WHOLE>(r + k, left(k), u[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int k = (i * LANES + lane) * PER_LANE;
+      TS t[PER_LANE];
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) v[i][e] += u[i][e];
+      round8(v[i], t);
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) {
+        if constexpr (sizeof(TS) == 2) v[i][e] = from_bf16(t[e]);
+      }
+      store8<sizeof(TS) == 2, WHOLE>(s + k, left(k), t);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+    if (a.w_f32) load8<WHOLE>(static_cast<const float*>(a.w) + k, left(k), w[i]);
+    else load8<WHOLE>(static_cast<const uint16_t*>(a.w) + k, left(k), w[i]);
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < VECS; ++i)
+#pragma unroll
+    for (int e = 0; e < PER_LANE; ++e) sum += v[i][e] * v[i][e];
+  const float rstd = 1.f / sqrtf(sum_of<LANES>(sum) / (float)a.K + a.eps);
+  if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+#pragma unroll
+    for (int e = 0; e < PER_LANE; ++e) v[i][e] = v[i][e] * rstd * w[i][e];
+    write_y<true, WHOLE>(a, row, k, left(k), v[i]);
+  }
+}
+
 // A workgroup a row; the row is read twice.
 template <class TX, class TS, bool RESIDUAL>
 __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
@@ -112,7 +178,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) sum += v[i] * v[i];
   }
-  const float rstd = 1.f / sqrtf(sum_of_256(sum) / (float)a.K + a.eps);
+  const float rstd = 1.f / sqrtf(sum_of<256>(sum) / (float)a.K + a.eps);
   if (threadIdx.x == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
   const int end = a.out >= FLUX_NORM_MX4 ? (a.K + 511) / 512 * 512 : a.K;
   for (int k0 = 0; k0 < end; k0 += 256 * PER_LANE) {
@@ -125,7 +191,110 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) v[i] = v[i] * rstd * w[i];
-    write_y(a, row, k, v);
+    write_y<false, false>(a, row, k, a.K - k, v);
+  }
+}
+
+// The row in registers, as norm_row_kernel has it; a workgroup takes rows from its first one on in steps of all workgroups' rows, keeps its lanes' part of dW
+// beside them, and leaves it as one row of `partial`.  AHEAD: the next row's numbers are asked for ahead of this one's sum.
+template <class TY, class TS, int LANES, int VECS, bool AHEAD, bool WHOLE>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kernel(const NormGradArgs a) {
+  constexpr int NT = LANES < 256 ? 256 : LANES, ROWS = NT / LANES;
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, step = gridDim.x * ROWS;
+  const auto left = [&](int k) { return WHOLE ? (k < a.K ? PER_LANE : 0) : a.K - k; };
+  struct Row {
+    Raw8<TY> g[VECS];
+    Raw8<TS> h[VECS], d[VECS];
+    float rstd = 0.f;
+  };
+  const auto ask = [&](Row& x, int row) {
+    if (row >= a.M) return;
+    x.rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int k = (i * LANES + lane) * PER_LANE;
+      x.g[i].template load<WHOLE>(static_cast<const TY*>(a.dy) + row * a.ldy + k, left(k));
+      x.h[i].template load<WHOLE>(static_cast<const TS*>(a.s) + row * a.lds + k, left(k));
+      if (a.ds != nullptr) x.d[i].template load<WHOLE>(static_cast<const TS*>(a.ds) + row * a.lds + k, left(k));
+    }
+  };
+  int row = blockIdx.x * ROWS + slot;
+  Row next;
+  if (AHEAD) ask(next, row);
+  float w[VECS][PER_LANE], dw[VECS][PER_LANE];
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+    if (a.w_f32) load8<WHOLE>(static_cast<const float*>(a.w) + k, left(k), w[i]);
+    else load8<WHOLE>(static_cast<const uint16_t*>(a.w) + k, left(k), w[i]);
+#pragma unroll
+    for (int e = 0; e < PER_LANE; ++e) dw[i][e] = 0.f;
+  }
+  // (every slot of a workgroup takes as many turns as its first)
+  for (int turn = 0; blockIdx.x * ROWS + turn * step < a.M; ++turn, row += step) {
+    Row x;
+    if (AHEAD) {
+      x = next;
+      ask(next, row + step);
+    } else {
+      ask(x, row);
+    }
+    const float r = x.rstd;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < VECS; ++i)
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) {
+        const float t = x.g[i].at(e) * (x.h[i].at(e) * r);
+        if (row < a.M) dw[i][e] += t;
+        sum += t * w[i][e];
+      }
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      x.g[i].fold();
+      x.h[i].fold();
+      x.d[i].fold();
+    }
+    const float mean = sum_of<LANES>(sum, turn & 1) / (float)a.K;
+    if (row < a.M) {
+#pragma unroll
+      for (int i = 0; i < VECS; ++i) {
+        const int k = (i * LANES + lane) * PER_LANE;
+        float v[PER_LANE];
+#pragma unroll
+        for (int e = 0; e < PER_LANE; ++e) {
+          v[e] = r * (x.g[i].at(e) * w[i][e] - x.h[i].at(e) * r * mean);
+          if (a.ds != nullptr) v[e] += x.d[i].at(e);
+        }
+        if (a.dr != nullptr) write8<TS, sizeof(TS) == 2, WHOLE>(a.dr, row * a.lds + k, left(k), v);
+        if (a.dx != nullptr) {
+          if (a.x_f32) write8<float, false, WHOLE>(a.dx, row * a.ldx + k, left(k), v);
+          else write8<uint16_t, true, WHOLE>(a.dx, row * a.ldx + k, left(k), v);
+        }
+      }
+    }
+  }
+  if (a.partial == nullptr) return;
+  // the slots' sums, in their order
+  if constexpr (ROWS > 1) {
+    __shared__ float part[ROWS][LANES * VECS * PER_LANE];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i)
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) part[slot][(i * LANES + lane) * PER_LANE + e] = dw[i][e];
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.K; k += NT) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < ROWS; ++j) sum += part[j][k];
+      a.partial[blockIdx.x * a.pitch + k] = sum;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int k = (i * LANES + lane) * PER_LANE;
+      store8<false, WHOLE>(a.partial + blockIdx.x * a.pitch + k, left(k), dw[i]);
+    }
   }
 }
 
@@ -145,7 +314,7 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormGradArgs a) {
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) sum += g[i] * w[i] * (h[i] * rstd);
   }
-  const float mean = sum_of_256(sum) / (float)a.K;
+  const float mean = sum_of<256>(sum) / (float)a.K;
   for (int k = threadIdx.x * PER_LANE; k < a.K; k += 256 * PER_LANE) {
     float g[PER_LANE], h[PER_LANE], w[PER_LANE], d[PER_LANE] = {};
     load8(dy + k, a.K - k, g);
@@ -154,10 +323,10 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const NormGradArgs a) {
     if (a.ds != nullptr) load8(static_cast<const TS*>(a.ds) + row * a.lds + k, a.K - k, d);
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) d[i] += rstd * (g[i] * w[i] - h[i] * rstd * mean);
-    if (a.dr != nullptr) write8<TS>(a.dr, row * a.lds + k, a.K - k, d);
+    if (a.dr != nullptr) write8<TS, false>(a.dr, row * a.lds + k, a.K - k, d);
     if (a.dx != nullptr) {
-      if (a.x_f32) write8<float>(a.dx, row * a.ldx + k, a.K - k, d);
-      else write8<uint16_t>(a.dx, row * a.ldx + k, a.K - k, d);
+      if (a.x_f32) write8<float, false>(a.dx, row * a.ldx + k, a.K - k, d);
+      else write8<uint16_t, false>(a.dx, row * a.ldx + k, a.K - k, d);
     }
   }
 }
@@ -177,21 +346,32 @@ __global__ void __launch_bounds__(256) norm_dw_kernel(const NormGradArgs a, int 
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) sum[i] += g[i] * (h[i] * rstd);
   }
-  store8<false>(a.partial + (long long)blockIdx.y * a.K + k, a.K - k, sum);
+  store8<false>(a.partial + blockIdx.y * a.pitch + k, a.K - k, sum);
 }
 
-// dW out of the groups' sums, in their order.
-__global__ void __launch_bounds__(256) norm_dw_join_kernel(const float* partial, int groups, int K, void* dw, int f32, int accumulate) {
-  const int k = blockIdx.x * 256 + threadIdx.x;
-  if (k >= K) return;
-  float sum = 0.f;
-  for (int g = 0; g < groups; ++g) sum += partial[(long long)g * K + k];
+// dW out of the groups' sums.  A workgroup has 32 columns, a line of every group's; 32 lanes a column, each a run of groups in their order, then the
+// runs in theirs.
+__global__ void __launch_bounds__(256) norm_dw_join_kernel(const float* partial, long long pitch, int groups, int K, void* dw, int f32, int accumulate) {
+  __shared__ float part[32][33];
+  const int c = threadIdx.x % 8 * 4, run = threadIdx.x / 8, each = (groups + 31) / 32, first = run * each, last = min(first + each, groups);
+  flux::f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  const float* const from = partial + blockIdx.x * 32ll + c;
+#pragma unroll 8
+  for (int g = first; g < last; ++g) sum += *reinterpret_cast<const flux::f32x4*>(from + g * pitch);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[run][c + e] = sum[e];
+  __syncthreads();
+  const int k = blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || k >= K) return;
+  float v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v += part[i][threadIdx.x];
   if (f32) {
     float* const p = static_cast<float*>(dw) + k;
-    *p = accumulate ? *p + sum : sum;
+    *p = accumulate ? *p + v : v;
   } else {
     __bf16* const p = static_cast<__bf16*>(dw) + k;
-    *p = (__bf16)(accumulate ? (float)*p + sum : sum);
+    *p = (__bf16)(accumulate ? (float)*p + v : v);
   }
 }
 
@@ -210,8 +390,70 @@ static int validate(const flux_norm_t* p) {
   return FLUX_OK;
 }
 
-// Groups of rows whose part of dW is summed by itself.
-static int row_groups(const flux_norm_t* p) { return std::min(p->M, 64); }
+template <class TX, class TS, bool RESIDUAL, int LANES, int VECS>
+static hipError_t go_row(const NormArgs& a, hipStream_t s) {
+  constexpr int NT = LANES < 256 ? 256 : LANES, ROWS = NT / LANES;
+  return start_with(a.K % PER_LANE == 0 ? norm_row_kernel<TX, TS, RESIDUAL, LANES, VECS, true> : norm_row_kernel<TX, TS, RESIDUAL, LANES, VECS, false>,
+                    dim3(ceil_div(a.M, ROWS)), NT, s, a);
+}
+template <class TX, class TS, bool RESIDUAL>
+static hipError_t go(const NormArgs& a, hipStream_t s) {
+  const int K = in_blocks(a.out) ? (a.K + 511) / 512 * 512 : a.K;          // (the padding of a row's scales is written too)
+  if (K <= 128) return go_row<TX, TS, RESIDUAL, 16, 1>(a, s);
+  if (K <= 512) return go_row<TX, TS, RESIDUAL, 64, 1>(a, s);
+  if (K <= 1024) return go_row<TX, TS, RESIDUAL, 64, 2>(a, s);
+  if (K <= 2048) return go_row<TX, TS, RESIDUAL, 256, 1>(a, s);
+  if (K <= 4096) return go_row<TX, TS, RESIDUAL, 512, 1>(a, s);
+  if (K <= 6144) return go_row<TX, TS, RESIDUAL, 256, 3>(a, s);
+  if (K <= 8192) return go_row<TX, TS, RESIDUAL, 1024, 1>(a, s);
+  if (K <= 12288) return go_row<TX, TS, RESIDUAL, 768, 2>(a, s);
+  if (K <= 16384) return go_row<TX, TS, RESIDUAL, 1024, 2>(a, s);
+  if (K <= 32768) return go_row<TX, TS, RESIDUAL, 1024, 4>(a, s);
+  return start(norm_kernel<TX, TS, RESIDUAL>, dim3(a.M), s, a);
+}
+static hipError_t launch_norm(const flux_norm_t* p, const NormArgs& a, bool residual, hipStream_t s) {
+  const bool xf = p->x_dtype == FLUX_F32, sf = p->s_dtype == FLUX_F32;
+  if (!residual) return xf ? go<float, float, false>(a, s) : go<uint16_t, uint16_t, false>(a, s);
+  if (xf) return sf ? go<float, float, true>(a, s) : go<float, uint16_t, true>(a, s);
+  return sf ? go<uint16_t, float, true>(a, s) : go<uint16_t, uint16_t, true>(a, s);
+}
+
+// How the backward pass runs: lanes and pieces of norm_grad_row_kernel (0: rows too long for it), and groups of rows whose part of dW is summed by itself.
+struct GradPlan { int lanes, vecs, groups; };
+static GradPlan grad_plan(const flux_norm_t* p) {
+  static constexpr GradPlan plans[] = {{16, 1, 512}, {64, 1, 512}, {64, 2, 512}, {256, 1, 768}, {512, 1, 512}, {768, 1, 256}, {1024, 1, 256}, {768, 2, 256}, {1024, 2, 256}};
+  for (GradPlan g : plans)
+    if (p->K <= g.lanes * g.vecs * PER_LANE) {
+      g.groups = std::min(g.groups, ceil_div(p->M, std::max(1, 256 / g.lanes)));
+      return g;
+    }
+  return GradPlan{0, 0, std::min(p->M, 64)};
+}
+static long long partial_pitch(const flux_norm_t* p) { return (p->K + 31ll) / 32 * 32; }
+
+template <class TY, class TS>
+static hipError_t go_grad(const GradPlan& g, const NormGradArgs& a, hipStream_t s) {
+#define GO(LANES, VECS, AHEAD) \
+  if (g.lanes == LANES && g.vecs == VECS) \
+    return start_with(a.K % PER_LANE == 0 ? norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD, true> : norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD, false>, \
+                      dim3(g.groups), LANES < 256 ? 256 : LANES, s, a)
+  GO(16, 1, true);
+  GO(64, 1, true);
+  GO(64, 2, true);
+  GO(256, 1, true);
+  GO(512, 1, true);
+  GO(1024, 1, true);
+  GO(768, 1, true);
+  GO(768, 2, sizeof(TS) == 2);
+  GO(1024, 2, false);
+#undef GO
+  if (a.partial != nullptr) {
+    // (ahead of dR, which may take dS's place)
+    const hipError_t e = start(norm_dw_kernel<TY, TS>, dim3(ceil_div(a.K, 256 * PER_LANE), g.groups), s, a, ceil_div(a.M, g.groups));
+    if (e != hipSuccess) return e;
+  }
+  return a.dr != nullptr || a.dx != nullptr ? start(norm_grad_kernel<TY, TS>, dim3(a.M), s, a) : hipSuccess;
+}
 
 }  // namespace flux_ffn
 
@@ -242,18 +484,13 @@ int flux_norm(const flux_norm_t* p, const void* X, const void* R, const void* W,
   a.eps = p->eps;
   a.out = p->out;
   a.w_f32 = p->w_dtype == FLUX_F32;
-  const bool xf = p->x_dtype == FLUX_F32, sf = p->s_dtype == FLUX_F32;
-  void (*const kernel)(NormArgs) =
-      R == nullptr ? (xf ? norm_kernel<float, float, false> : norm_kernel<uint16_t, uint16_t, false>)
-      : xf ? (sf ? norm_kernel<float, float, true> : norm_kernel<float, uint16_t, true>)
-           : (sf ? norm_kernel<uint16_t, float, true> : norm_kernel<uint16_t, uint16_t, true>);
-  FFN_HIP(start(kernel, dim3(p->M), static_cast<hipStream_t>(stream), a));
+  FFN_HIP(launch_norm(p, a, R != nullptr, static_cast<hipStream_t>(stream)));
   return FLUX_OK;
 }
 
 size_t flux_norm_workspace_bytes(const flux_norm_t* p) {
   if (validate(p) != FLUX_OK || in_blocks(p->out)) return 0;
-  return WS_HEADER + 4ull * row_groups(p) * p->K;
+  return WS_HEADER + 4ull * grad_plan(p).groups * partial_pitch(p);
 }
 
 int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, const void* W, const float* rstd, const void* dS, void* dR, void* dX,
@@ -274,7 +511,8 @@ int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, cons
   a.rstd = rstd;
   a.dr = dR;
   a.dx = dX;
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + WS_HEADER);
+  a.partial = dW != nullptr ? reinterpret_cast<float*>(static_cast<char*>(workspace) + WS_HEADER) : nullptr;
+  a.pitch = partial_pitch(p);
   a.ldx = pitch(p->ldx, p->K);
   a.lds = pitch(p->lds, p->K);
   a.ldy = pitch(p->ldy, p->K);
@@ -282,19 +520,12 @@ int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, cons
   a.K = p->K;
   a.w_f32 = p->w_dtype == FLUX_F32;
   a.x_f32 = p->x_dtype == FLUX_F32;
+  if (dR == nullptr && dX == nullptr && dW == nullptr) return FLUX_OK;
   const bool yf = p->out == FLUX_NORM_F32, sf = p->s_dtype == FLUX_F32;
-  if (dW != nullptr) {
-    // (ahead of dR, which may take dS's place, but not S's)
-    const int groups = row_groups(p), each = ceil_div(p->M, groups);
-    const dim3 grid(ceil_div(p->K, 256 * PER_LANE), groups);
-    void (*const kernel)(NormGradArgs, int) = yf ? (sf ? norm_dw_kernel<float, float> : norm_dw_kernel<float, uint16_t>) : (sf ? norm_dw_kernel<uint16_t, float> : norm_dw_kernel<uint16_t, uint16_t>);
-    FFN_HIP(start(kernel, grid, s, a, each));
-    FFN_HIP(start(norm_dw_join_kernel, dim3(ceil_div(p->K, 256)), s, (const float*)a.partial, groups, (int)p->K, dW, (int)(p->dw_dtype == FLUX_F32), (int)p->dw_accumulate));
-  }
-  if (dR != nullptr || dX != nullptr) {
-    void (*const kernel)(NormGradArgs) = yf ? (sf ? norm_grad_kernel<float, float> : norm_grad_kernel<float, uint16_t>) : (sf ? norm_grad_kernel<uint16_t, float> : norm_grad_kernel<uint16_t, uint16_t>);
-    FFN_HIP(start(kernel, dim3(p->M), s, a));
-  }
+  const GradPlan g = grad_plan(p);
+  FFN_HIP(yf ? (sf ? go_grad<float, float>(g, a, s) : go_grad<float, uint16_t>(g, a, s)) : (sf ? go_grad<uint16_t, float>(g, a, s) : go_grad<uint16_t, uint16_t>(g, a, s)));
+  if (dW != nullptr)
+    FFN_HIP(start(norm_dw_join_kernel, dim3(ceil_div(p->K, 32)), s, (const float*)a.partial, a.pitch, g.groups, (int)p->K, dW, (int)(p->dw_dtype == FLUX_F32), (int)p->dw_accumulate));
   return FLUX_OK;
 }
 
