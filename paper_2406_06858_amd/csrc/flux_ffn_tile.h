@@ -122,29 +122,32 @@ struct OperandLoader {
   static_assert(RPI == 2 || RPI == 4 || RPI == 8, "the swizzle must not depend on the instruction");
 
   uint32_t voff, pitch, lds_wave;
-  int lim, k_vec;                  // along: loads that have a row, the lane's place in the contraction; across: k_vec alone
+  int k_vec;                       // along: the lane's place in the contraction
   __device__ __forceinline__ void init(uint32_t pitch_, int rows, int r0, int wave, int lane) {
     pitch = pitch_;
     lds_wave = (uint32_t)(wave_row(wave) * (1024 / RPI));
     if constexpr (T) {
       const int k = wave_row(wave) + lane / SLOTS, s = lane % SLOTS ^ flux::swz_b<SLOTS>(wave_row(wave) + lane / SLOTS);
-      voff = (uint32_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
-      if (EDGE) k_vec = r0 + s * 8 < rows ? k : 0x40000000;
+      voff = EDGE && r0 + s * 8 >= rows ? OUTSIDE : (uint32_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
     } else {
       const int row = 8 * wave + lane / 8, s = lane % 8 ^ swizzle<MX>(row);
       voff = (uint32_t)(r0 + row) * pitch + (uint32_t)s * 16u;
-      if (EDGE) {
-        k_vec = s * 8;
-        lim = (rows - r0 - row + 31) / 32;
-      }
+      k_vec = s * 8;
     }
   }
-  // the d-th of the wave's loads of the slab that starts at k (`depth` in all) into `tile`
+  // The d-th of the wave's loads of the slab that starts at k (`depth` in all) into `tile`.  Rows past the last one end up past the buffer's records by themselves
+  // where the whole offset is the lane's (a sum that stays at the largest number instead of wrapping): what is left to ask is whether a slab's last
+  // pieces are in the row (once a slab), and whether rows of a contraction that lies across begin at all (uniform).  With a mask for every load the
+  // 256x256 tile ran out of scalar registers: logits of 8192x4000x8192 409 us, 366 for 4096 columns without masks.
   __device__ __forceinline__ void load(int d, const __amdgpu_buffer_rsrc_t& rsrc, int k, int depth, unsigned char* tile) const {
-    const bool in = !EDGE || (T ? k_vec < depth - k - instr_row(d) : d < (k_vec < depth - k ? lim : 0));
-    const uint32_t from = T ? (uint32_t)(k + instr_row(d)) * pitch : (uint32_t)k * 2u + (uint32_t)instr_row(d) * pitch;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(tile + instr_row(d) * (1024 / RPI) + lds_wave), 16,
-                                             (int)(in ? voff : OUTSIDE), (int)from, 0, 0);
+    uint32_t at = voff, from = T ? (uint32_t)(k + instr_row(d)) * pitch : (uint32_t)k * 2u + (uint32_t)instr_row(d) * pitch;
+    if constexpr (EDGE) {
+      if constexpr (T) from = k + instr_row(d) < depth ? from : OUTSIDE;
+      else at = k_vec < depth - k ? voff : OUTSIDE;
+      at = __builtin_elementwise_add_sat(at, from);
+      from = 0u;
+    }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(tile + instr_row(d) * (1024 / RPI) + lds_wave), 16, (int)at, (int)from, 0, 0);
   }
 };
 
