@@ -56,7 +56,7 @@ static bool act_ok(int a) { return a >= FLUX_ACT_SILU && a <= FLUX_ACT_GELU_TANH
 
 // (a workgroup of 256 threads has at least 16 columns, and 2^32 threads are too many for a launch)
 bool few_fits(int kind, int rows, int cols) {
-  return rows <= FEW_ROWS && cols <= (1 << 28) - 16 && (kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU);
+  return rows <= FEW_ROWS && cols <= (1 << 28) - 16 && (kind == LOGITS || kind == GLU_NK || kind == MX_GEMM || kind == MX_GLU);
 }
 
 static int validate(int op, const flux_glu_t* p) {
@@ -85,6 +85,15 @@ static int validate(int op, const flux_mx4_t* p) {
 // ---- how a product is run --------------------------------------------------------------------------------------
 static int halves_of(int kind) { return kind == GLU_NK || kind == GLU_KN || kind == MX_GLU ? 2 : 1; }
 
+// Logits: the columns are a vocabulary's, and many: rows of 64x128 tiles read them as fast, and the rows they meet half as often.  Where few columns or
+// long rows leave those a part of a round, the kernel for few rows is ahead.  us, it / the best tile: 1x32000x8192 84 / 103, 16x4000x8192 16.7 / 19.9,
+// 7x1488x3008 9.8 / 12.5; 16x32000x2048 37 / 34, 54x12617x832 20.4 / 11.8, 48x89455x384 82 / 21.  Over 150 random problems of up to 64 rows the pick takes
+// 1.6 % longer in the mean than the faster one; the estimates alone 8 %, tiles alone 4 %.
+static bool few_pays(int kind, int rows, int cols, int depth) {
+  if (kind != LOGITS) return true;
+  return rows <= 16 ? cols <= 8192 || (depth >= 6144 && depth % 64 == 0) : cols <= 2048;
+}
+
 // Estimated us of a product: whole rounds of workgroups, a last one that is not full, the cut tiles.
 static double tile_us(const Shape& sh, const Pace& p, int full, int cut, int parts, int slabs, int part_slabs) {
   const int at_once = 256 * sh.per_unit, last = full % at_once;
@@ -107,7 +116,7 @@ Plan plan_tiles(int kind, int rows, int cols, int depth, int config, int want_pa
   // tiles that take longer there.)
   double few = 0;
   best.few = config == FEW_CONFIG;
-  if (config == 0 && want_parts <= 1 && few_fits(kind, rows, cols)) {
+  if (config == 0 && want_parts <= 1 && few_fits(kind, rows, cols) && few_pays(kind, rows, cols, depth)) {
     few = few_us(kind, rows, cols, depth / 8);
     best.few = few <= 1.3 * (3.0 + 2.0 * halves * cols * depth / 5.2e6);
   }

@@ -59,11 +59,11 @@ __device__ __forceinline__ void lds_read16(u32x4& v, uint32_t base) { asm volati
 template <int OFF>
 __device__ __forceinline__ void lds_read2(uint32_t& v, uint32_t base) { asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(v) : "v"(base), "n"(OFF)); }
 
+// A workgroup's columns n0 .. n0 + COLS - 1 of the product: its waves' sums, in LDS for few_sum.
 template <class C>
-__global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
-  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+__device__ __forceinline__ const float* few_body(const FewArgs& t, unsigned char* pool, int n0) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i = lane & 15, g = lane >> 4, n0 = by_die((int)blockIdx.x, (int)gridDim.x) * C::COLS;
+  const int i = lane & 15, g = lane >> 4;
   constexpr uint32_t OUTSIDE = 0xfffffff0u;
   const auto rsrc = [](const void* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000); };
   const __amdgpu_buffer_rsrc_t ra = rsrc(t.a, t.bytes_a), rb[2] = {rsrc(t.b[0], t.bytes_b), rsrc(t.b[C::HALVES - 1], t.bytes_b)};
@@ -196,17 +196,29 @@ __global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
 #pragma unroll
     for (int h = 0; h < C::BLOCKS; ++h) *reinterpret_cast<f32x4*>(red + ((wave * C::MB + m) * C::BLOCKS + h) * 256 + lane * 4) = acc[m][h];
   __syncthreads();
-  // a lane of a 16x16 block held rows 4g .. 4g+3 of column i
-  for (int e = tid; e < C::MB * 16 * C::COLS; e += C::NT) {
-    const int c = e % C::COLS, row = e / C::COLS, col = n0 + c, m = row >> 4;
-    if (row >= t.rows || col >= t.cols) continue;
-    const int at = (m * C::BLOCKS + c / 16) * 256 + ((row >> 2 & 3) * 16 + c % 16) * 4 + (row & 3);
-    float v = 0.f, u = 0.f;
+  return red;
+}
+
+// The sum of row `row`, column c of the workgroup's, `half` of a gated product.  (A lane of a 16x16 block held rows 4g .. 4g+3 of column i.)
+template <class C>
+__device__ __forceinline__ float few_sum(const float* red, int row, int c, int half = 0) {
+  const int at = ((row >> 4) * C::BLOCKS + c / 16 + half) * 256 + ((row >> 2 & 3) * 16 + c % 16) * 4 + (row & 3);
+  float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < C::WAVES; ++w) {
-      v += red[w * C::MB * C::BLOCKS * 256 + at];
-      if constexpr (C::HALVES == 2) u += red[w * C::MB * C::BLOCKS * 256 + at + 256];
-    }
+  for (int w = 0; w < C::WAVES; ++w) v += red[w * C::MB * C::BLOCKS * 256 + at];
+  return v;
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::NT) few_kernel(const FewArgs t) {
+  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+  const int n0 = by_die((int)blockIdx.x, (int)gridDim.x) * C::COLS;
+  const float* const red = few_body<C>(t, pool, n0);
+  for (int e = threadIdx.x; e < C::MB * 16 * C::COLS; e += C::NT) {
+    const int c = e % C::COLS, row = e / C::COLS, col = n0 + c;
+    if (row >= t.rows || col >= t.cols) continue;
+    float v = few_sum<C>(red, row, c);
+    const float u = C::HALVES == 2 ? few_sum<C>(red, row, c, 1) : 0.f;
     const long long to = row * t.ld + col;
     if constexpr (C::HALVES == 2) {
       if (t.g != nullptr) {

@@ -1,6 +1,7 @@
 // Instantiates the kernel for few rows.
 #include <algorithm>
 #include "flux_ffn_internal.h"
+#include "flux_loss_few.h"
 
 namespace flux_ffn {
 
@@ -29,6 +30,7 @@ static auto with_config(int kind, int rows, int cols, int row_vecs, F f) {
   // 3.9 / 4.6, 8x4096 4.1 / 4.9, 8x4104 5.5 / 4.8, 8x8192 6.6 / 5.3, 64x4104 8.5 / 6.6, 8x28672 18.8 / 16.5; at K = 512, where workgroups share a
   // unit, 8x8192 3.1 / 3.3, 64x8192 6.1 / 4.8.
   if (kind == MX_GEMM) return cols > 256 * 16 ? by_rows<true, 1, 2>(rows, row_vecs, f) : by_rows<true, 1, 1>(rows, row_vecs, f);
+  if (kind == LOGITS) return cols > 256 * 16 ? by_rows<false, 1, 2>(rows, row_vecs, f) : by_rows<false, 1, 1>(rows, row_vecs, f);
   if (kind == MX_GLU) return by_rows<true, 2, 2>(rows, row_vecs, f);
   return by_rows<false, 2, 2>(rows, row_vecs, f);
 }
@@ -37,7 +39,21 @@ hipError_t launch_few(int kind, const FewArgs& a, hipStream_t s) {
   return with_config(kind, a.rows, a.cols, a.row_vecs, [&](auto c) {
     typedef decltype(c) C;
     static_assert(C::NT == 256, "start");
-    return start(few_kernel<C>, dim3((a.cols + C::COLS - 1) / C::COLS), s, a);
+    if constexpr (!C::MX && C::HALVES == 1) return hipErrorInvalidValue;          // (logits: launch_few_logits)
+    else return start(few_kernel<C>, dim3((a.cols + C::COLS - 1) / C::COLS), s, a);
+  });
+}
+
+int few_columns(int kind, int rows, int cols, int row_vecs) {
+  return with_config(kind, rows, cols, row_vecs, [](auto c) { return decltype(c)::COLS; });
+}
+
+hipError_t launch_few_logits(bool gradient, const FewArgs& a, const LossArgs& l, hipStream_t s) {
+  return with_config(LOGITS, a.rows, a.cols, a.row_vecs, [&](auto c) {
+    typedef decltype(c) C;
+    // (one of with_config's kinds is meant; the others are not built for it)
+    if constexpr (!C::MX && C::HALVES == 1) return start(gradient ? few_logits_kernel<C, true> : few_logits_kernel<C, false>, dim3(ceil_div(a.cols, C::COLS)), s, a, l);
+    else return hipErrorInvalidValue;
   });
 }
 

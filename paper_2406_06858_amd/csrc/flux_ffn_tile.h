@@ -37,7 +37,8 @@ using flux::FragHalves;
 using flux::u32x2;
 using flux::u32x4;
 
-enum Kind : int { GLU_NK = 0, GLU_KN = 1, DX_NK = 2, DX_KN = 3, DW = 4, MX_GEMM = 5, MX_GLU = 6, KINDS = 7 };
+// (LOGITS: the plan of a plain product along the contraction, whose tiles run the loop of DX_NK on one segment)
+enum Kind : int { LOGITS = -1, GLU_NK = 0, GLU_KN = 1, DX_NK = 2, DX_KN = 3, DW = 4, MX_GEMM = 5, MX_GLU = 6, KINDS = 7 };
 
 struct TileArgs {
   const void* a[2];              // dX: by segment; dW: by weight; else [0]
@@ -64,10 +65,11 @@ struct TileArgs {
   uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
 
-template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_>
+template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_, bool B_ONCE_ = false>
 struct Cfg {
   static constexpr int KIND = KIND_, BM = BM_, BN = BN_, NA = NA_, NB = NB_, OCC = OCC_;
   static constexpr bool EDGE = EDGE_;                                        // the tile does not divide the product
+  static constexpr bool B_ONCE = B_ONCE_;                                    // one row of tiles: B's lines are read once, past the caches
   static constexpr bool MX = KIND == MX_GEMM || KIND == MX_GLU, A_T = KIND == DW;
   static constexpr bool B_NK = MX || KIND == GLU_NK || KIND == DX_NK;
   static constexpr int HALVES = KIND == GLU_NK || KIND == GLU_KN || KIND == MX_GLU ? 2 : 1;
@@ -109,7 +111,7 @@ __device__ __forceinline__ void mfma_scaled(f32x4& acc, const u32x4& a, const u3
 //   along   rows of 128 bytes, one instruction 8 rows;
 //   across  (T) one row per step of the contraction, R values each, one instruction 512 / R of those.
 // (The same patterns as DmaLoader's.)  A lane outside the matrix loads from outside the buffer's records: zeros.
-template <int R, bool T, bool EDGE, bool MX>
+template <int R, bool T, bool EDGE, bool MX, bool ONCE = false>
 struct OperandLoader {
   static constexpr int RPI = T ? 512 / R : 8;
   static constexpr int INSTR = (T ? 64 : R) / RPI / 4;         // per wave
@@ -147,7 +149,7 @@ struct OperandLoader {
       at = __builtin_elementwise_add_sat(at, from);
       from = 0u;
     }
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(tile + instr_row(d) * (1024 / RPI) + lds_wave), 16, (int)at, (int)from, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (flux::lds_void_t*)(tile + instr_row(d) * (1024 / RPI) + lds_wave), 16, (int)at, (int)from, 0, ONCE ? 2 : 0);
   }
 };
 
@@ -160,7 +162,7 @@ struct Slab {
 template <class C>
 struct Pipe {
   typedef OperandLoader<C::BM, C::A_T, C::EDGE, C::MX> LdA;
-  typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX> LdB;
+  typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX, C::B_ONCE> LdB;
   static constexpr int NA = C::NA, NB = C::NB;
   static constexpr bool A_LEADS = NA > NB;                               // by one slab
   static constexpr int U = NA != NB ? NA * NB : NB;      // slabs after which the rings are where they were
@@ -515,27 +517,51 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const 
       }
     }
   }
+  // What is added to, asked for before the first of it is used (it may lie where the results go, so no load would pass a store).
+  f32x4 old[C::HALVES == 2 ? 1 : C::NI];
+  if constexpr (C::HALVES == 1) {
+    const bool sums = (C::KIND == DX_NK || C::KIND == DX_KN) && t.addend != nullptr;
+    if (sums || (t.accumulate && t.out_f32)) {
+      // four columns a block
+      const float* const from = (sums ? t.addend : static_cast<const float*>(t.out[job])) + row * t.ld;
+#pragma unroll
+      for (int n = 0; n < C::NI; ++n) {
+        const int col = col0 + n * 16 + 4 * g;
+        if (!C::EDGE || (row < t.rows && col < t.cols)) old[n] = *reinterpret_cast<const f32x4*>(from + col);
+      }
+    } else if (t.accumulate) {
+      // eight columns of two blocks, in bf16
+#pragma unroll
+      for (int n = 0; n < C::NI; n += 2) {
+        const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
+        if (!C::EDGE || (row < t.rows && col < t.cols))
+          old[n] = __builtin_bit_cast(f32x4, *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(t.out[job]) + row * t.ld + col));
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (sums || (t.accumulate && t.out_f32)) {
+#pragma unroll
+      for (int n = 0; n < C::NI; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) old[n][e] += acc[n][e];
+    }
+  }
   if (!t.out_f32) {
     u32x4 p[C::NIH / 2];
 #pragma unroll
     for (int n = 0; n < C::NIH; n += 2) {
       float v[8];
-      eight_columns(acc[n], acc[n + 1], v);
       if constexpr (C::HALVES == 2) {
         float u[8];
+        eight_columns(acc[n], acc[n + 1], v);
         eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
         gate<false>(t.act, v, u);
       } else if ((C::KIND == DX_NK || C::KIND == DX_KN) && t.addend != nullptr) {
-        const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
-        if (!C::EDGE || (row < t.rows && col < t.cols)) {
-          const f32x4* const o = reinterpret_cast<const f32x4*>(t.addend + row * t.ld + col);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += o[e / 4][e % 4];
-        }
-      } else if (t.accumulate) {
-        const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
-        if (!C::EDGE || (row < t.rows && col < t.cols)) {
-          const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(t.out[job]) + row * t.ld + col);
+        eight_columns(old[n], old[n + 1], v);
+      } else {
+        eight_columns(acc[n], acc[n + 1], v);
+        if (t.accumulate) {
+          const bf16x8 o = __builtin_bit_cast(bf16x8, old[n]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
         }
@@ -555,12 +581,8 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const 
           const float u[4] = {y[0], y[1], y[2], y[3]};
           gate<true>(t.act, v, u);
         } else if (t.accumulate) {
-          const int col = col0 + (n + h) * 16 + 4 * g;
-          if (!C::EDGE || (row < t.rows && col < t.cols)) {
-            const f32x4 o = *reinterpret_cast<const f32x4*>(static_cast<const float*>(t.out[job]) + row * t.ld + col);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-          }
+          for (int e = 0; e < 4; ++e) v[e] = old[n + h][e];
         }
         p[h] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
       }

@@ -25,6 +25,7 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   const int r = threadIdx.x % ROWS, lane = threadIdx.x / ROWS, row = blockIdx.x * ROWS + r;
   float m = -__builtin_inff(), s = 0.f;
   if (row < a.rows) {
+#pragma unroll 4
     for (int i = lane; i < a.runs; i += LANES) {
       const float2 v = a.stats[(long long)i * a.rows + row];
       join_stats(m, s, v.x, v.y);
@@ -46,6 +47,12 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   a.lse[row] = lse;
   if (target < 0) a.logit[row] = 0.f;
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
+}
+
+// X in rows of whole lines, for products that read it many times.
+__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int row_vecs, long long vecs) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i < vecs) to[i / row_vecs * to_pitch + i % row_vecs] = from[i / row_vecs * pitch + i % row_vecs];
 }
 
 struct RanksArgs {
@@ -85,7 +92,7 @@ static int validate(int op, const flux_loss_t* p) {
   if (p->M < 1 || p->V < 1 || p->K < 1 || p->K % 8 != 0 || p->piece % 64 != 0) return FLUX_ERR_SHAPE;
   if (p->v0 > MAX_VOCAB || p->vocab > MAX_VOCAB || vocab_of(p) < p->v0 + p->V) return FLUX_ERR_SHAPE;
   if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), p->V, p->K)) return FLUX_ERR_SHAPE;
-  if (p->tile_config == FEW_CONFIG) return FLUX_ERR_UNSUPPORTED;
+  if (p->tile_config == FEW_CONFIG && !few_fits(LOGITS, p->M, p->V)) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
 
@@ -99,18 +106,30 @@ static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
 static int piece_of(const flux_loss_t* p) {
   const long long all = whole_lines(p->V);
   if (p->piece) return (int)std::min<long long>(p->piece, all);
-  const long long most = std::max(2048ll, (128ll << 20) / 2 / p->M / 256 * 256);
+  const long long most = std::max(2048ll, (256ll << 20) / 2 / p->M / 256 * 256);
   return (int)std::min(all, most);
 }
 static bool dz_fits(const flux_loss_t* p) { return p->M * (long long)piece_of(p) < LIMIT; }
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// The backward pass's workspace: the header, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
-struct Layout { size_t dz, sums, partial, all; };
+// Whether X is laid out anew: a slab's loads, 128 bytes a row, are two lines each where rows are no whole lines, and every column tile reads X.  us, X as it is / laid
+// out anew by the caller: statistics of 1496x50257x5112 729 / 678, 1496x4000x5112 82.6 / 68.0, 200x4000x5112 24.7 / 23.6; gradients of 1496x6283x5112 279 / 262:
+// 7 % of the products that read X, for 3 us and a pass of 4.5 TB/s.
+static bool lays_out_x(int op, const flux_loss_t* p, const Plan& z) {
+  if (pitch_x(p) % 64 == 0 || z.few) return false;
+  const double product_us = 2.0 * p->M * p->V * p->K / 1.3e9;
+  return 0.07 * product_us * (op == FLUX_LOSS_BACKWARD ? 2 : 1) > 3.0 + 4.0 * p->M * p->K / 4.5e6;
+}
+static size_t x_bytes(int op, const flux_loss_t* p, const Plan& z) { return lays_out_x(op, p, z) ? up256(2ull * p->M * whole_lines(p->K)) : 0; }
+
+// The backward pass's workspace: the header, X in whole lines, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
+struct Layout { size_t dz, sums, partial, all; bool lays_out; };
 static Layout layout(const flux_loss_t* p) {
   const int piece = piece_of(p), last = p->V - (p->V - 1) / piece * piece;
   Layout y;
-  y.dz = WS_HEADER;
+  const size_t x = x_bytes(FLUX_LOSS_BACKWARD, p, plan_z(p, std::min(piece, p->V)));
+  y.lays_out = x != 0;
+  y.dz = WS_HEADER + x;
   y.sums = y.dz + up256(2ull * p->M * piece);
   y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
   size_t most = 0;
@@ -120,9 +139,9 @@ static Layout layout(const flux_loss_t* p) {
   return y;
 }
 
-// A forward pass's: the header, the statistics, the cut tiles' sums.
-static int runs_of(const Plan& pl) { return 2 * pl.tiles_n; }
-static size_t stats_bytes(const flux_loss_t* p, const Plan& pl) { return up256(8ull * p->M * runs_of(pl)); }
+// A forward pass's: the header, X in whole lines, the statistics, the cut tiles' sums.
+static int runs_of(const flux_loss_t* p, const Plan& pl) { return pl.few ? ceil_div(p->V, few_columns(LOGITS, p->M, p->V, p->K / 8)) : 2 * pl.tiles_n; }
+static size_t stats_bytes(const flux_loss_t* p, const Plan& pl) { return up256(8ull * p->M * runs_of(p, pl)); }
 
 static LossArgs loss_args(const flux_loss_t* p, const void* target) {
   LossArgs l = {};
@@ -134,9 +153,9 @@ static LossArgs loss_args(const flux_loss_t* p, const void* target) {
   return l;
 }
 
-static TileArgs logits_args(const flux_loss_t* p, const void* X, const void* W, int v, int cols) {
+static TileArgs logits_args(const flux_loss_t* p, const void* X, long long lx, const void* W, int v, int cols) {
   TileArgs t = {};
-  const long long lx = pitch_x(p), lw = pitch_w(p);
+  const long long lw = pitch_w(p);
   t.a[0] = X;
   t.b[0] = static_cast<const __bf16*>(W) + v * lw;
   t.pitch_a = (uint32_t)(lx * 2);
@@ -149,6 +168,36 @@ static TileArgs logits_args(const flux_loss_t* p, const void* X, const void* W, 
   return t;
 }
 
+// From here on X and its pitch are those of the copy.
+static int lay_out_x(const flux_loss_t* p, const void*& X, long long& lx, char* to, hipStream_t s) {
+  const long long vecs = (long long)p->M * (p->K / 8), pitch = whole_lines(p->K);
+  FFN_HIP(start(whole_rows_kernel, dim3((unsigned)((vecs + 255) / 256)), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, p->K / 8, vecs));
+  X = to;
+  lx = pitch;
+  return FLUX_OK;
+}
+
+static int launch_logits(bool gradient, const Plan& pl, TileArgs& t, const LossArgs& l, void* ws, size_t partial_at, hipStream_t s) {
+  if (pl.few) {
+    FewArgs f = {};
+    f.a = t.a[0];
+    f.b[0] = f.b[1] = t.b[0];
+    f.pitch_a = t.pitch_a;
+    f.pitch_b = t.pitch_b;
+    f.bytes_a = t.bytes_a;
+    f.bytes_b = t.bytes_b;
+    f.rows = t.rows;
+    f.cols = t.cols;
+    f.row_vecs = t.depth / 8;
+    f.ld = t.ld;
+    FFN_HIP(launch_few_logits(gradient, f, l, s));
+    return FLUX_OK;
+  }
+  set_tiles(t, pl, ws, partial_at);
+  FFN_HIP((gradient ? launch_dz : launch_stats)(pl.shape, t, l, pl.edge, pl.full + pl.cut * pl.parts, s));
+  return FLUX_OK;
+}
+
 }  // namespace flux_ffn
 
 using namespace flux_ffn;
@@ -159,7 +208,7 @@ size_t flux_loss_workspace_bytes(int op, const flux_loss_t* p) {
   if (validate(op, p) != FLUX_OK) return 0;
   if (op == FLUX_LOSS_BACKWARD) return dz_fits(p) ? layout(p).all : 0;
   const Plan pl = plan_z(p, p->V);
-  return WS_HEADER + stats_bytes(p, pl) + pl.partial_bytes;
+  return WS_HEADER + x_bytes(op, p, pl) + stats_bytes(p, pl) + pl.partial_bytes;
 }
 
 int flux_loss(const flux_loss_t* p, const void* X, const void* W, const void* target, float* lse, float* logit, float* loss, void* workspace,
@@ -170,25 +219,31 @@ int flux_loss(const flux_loss_t* p, const void* X, const void* W, const void* ta
   if (X == nullptr || W == nullptr || !aligned(X, 16) || !aligned(W, 16) || target == nullptr || !aligned(target, target_bytes)) return FLUX_ERR_INVALID_ARG;
   if (lse == nullptr || logit == nullptr || !aligned(lse, 4) || !aligned(logit, 4) || !aligned(loss, 4)) return FLUX_ERR_INVALID_ARG;
   const Plan pl = plan_z(p, p->V);
-  const size_t partial_at = WS_HEADER + stats_bytes(p, pl);
+  const size_t stats_at = WS_HEADER + x_bytes(FLUX_LOSS_FORWARD, p, pl), partial_at = stats_at + stats_bytes(p, pl);
   st = workspace_ok(partial_at + pl.partial_bytes, workspace, workspace_bytes);
   if (st != FLUX_OK) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   StatsArgs a = {};
   a.loss = loss_args(p, target);
-  a.loss.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + WS_HEADER);
+  a.loss.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + stats_at);
   a.loss.logit = logit;
-  TileArgs t = logits_args(p, X, W, 0, p->V);
-  set_tiles(t, pl, workspace, partial_at);
-  FFN_HIP(launch_stats(pl.shape, t, a.loss, pl.edge, pl.full + pl.cut * pl.parts, s));
+  long long lx = pitch_x(p);
+  if (stats_at != WS_HEADER) {
+    st = lay_out_x(p, X, lx, static_cast<char*>(workspace) + WS_HEADER, s);
+    if (st != FLUX_OK) return st;
+  }
+  TileArgs t = logits_args(p, X, lx, W, 0, p->V);
+  st = launch_logits(false, pl, t, a.loss, workspace, partial_at, s);
+  if (st != FLUX_OK) return st;
   a.stats = a.loss.stats;
-  a.runs = runs_of(pl);
+  a.runs = runs_of(p, pl);
   a.rows = p->M;
   a.cols = p->V;
   a.lse = lse;
   a.logit = logit;
   a.value = loss;
-  if (p->M >= 64) FFN_HIP(start(stats_kernel<16>, dim3(ceil_div(p->M, 16)), s, a));
+  if (p->M > 4096) FFN_HIP(start(stats_kernel<16>, dim3(ceil_div(p->M, 16)), s, a));
+  else if (p->M > 256) FFN_HIP(start(stats_kernel<4>, dim3(ceil_div(p->M, 4)), s, a));
   else FFN_HIP(start(stats_kernel<1>, dim3(p->M), s, a));
   return FLUX_OK;
 }
@@ -232,23 +287,28 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
   char* const ws = static_cast<char*>(workspace);
   __bf16* const dz = reinterpret_cast<__bf16*>(ws + y.dz);
   float* const sums = reinterpret_cast<float*>(ws + y.sums);
-  const long long lx = pitch_x(p), lw = pitch_w(p);
+  long long lx = pitch_x(p);
+  const long long lw = pitch_w(p);
   const int piece = piece_of(p);
+  if (y.lays_out) {
+    st = lay_out_x(p, X, lx, ws + WS_HEADER, s);
+    if (st != FLUX_OK) return st;
+  }
   for (int v = 0; v < p->V; v += piece) {
     const int cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
     const long long ldz = whole_lines(cols);
     const uint32_t bytes_z = extent(p->M, ldz * 2, held * 2ll);
     {
       const Plan pl = plan_z(p, cols);
-      TileArgs t = logits_args(p, X, W, v, cols);
-      set_tiles(t, pl, ws, y.partial);
+      TileArgs t = logits_args(p, X, lx, W, v, cols);
       t.ld = ldz;
       LossArgs l = loss_args(p, target);
       l.v0 += v;
       l.lse = lse;
       l.dloss = dloss;
       l.dz = dz;
-      FFN_HIP(launch_dz(pl.shape, t, l, pl.edge, pl.full + pl.cut * pl.parts, s));
+      st = launch_logits(true, pl, t, l, ws, y.partial, s);
+      if (st != FLUX_OK) return st;
     }
     if (dX != nullptr) {
       const bool first = v == 0, last = p->V - v <= piece, f32 = p->dx_dtype == FLUX_F32;
@@ -262,7 +322,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.rows = p->M;
       t.cols = p->K;
       t.depth = held;
-      t.ld = lx;
+      t.ld = pitch_x(p);
       // sums of pieces stay in fp32: in dX, or in the workspace until the last piece rounds them
       t.out_f32 = f32 || !last;
       t.out[0] = f32 || last ? dX : sums;

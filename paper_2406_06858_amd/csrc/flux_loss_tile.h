@@ -7,8 +7,6 @@
 
 namespace flux_ffn {
 
-constexpr Kind LOGITS = DX_NK;       // the main loop of Z: both operands along the contraction, one segment of it
-
 struct LossArgs {
   const void* target;            // [rows], 32 or 64 bits
   int32_t target_i64, dloss_one;

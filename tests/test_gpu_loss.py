@@ -165,6 +165,17 @@ def test_every_tile(config, split):
         c.check_backward(c.backward(c.dloss, lse, tile_config=config, split_k=split), lse, c.dloss)
 
 
+@pytest.mark.parametrize("M", [1, 8, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("V,K", [(1, 8), (15, 256), (33, 264), (4096, 512), (4099, 520), (777, 1544), (300, 4096)])
+def test_few_rows_on_their_own_kernel(M, V, K):
+    """Short and long rows, with whole pieces and without, 16 and 32 columns a workgroup; and the tiles for the same."""
+    c = Case(M, V, K, M * V + K, pad=(8, 16))
+    lse = torch.from_numpy(c.lse).float().to(DEV)
+    for config in (ffn.flux_ffn_tile_config_count(), 5):
+        c.check_forward(c.forward(tile_config=config))
+        c.check_backward(c.backward(c.dloss, lse, tile_config=config), lse, c.dloss)
+
+
 @pytest.mark.parametrize("piece", [64, 128, 192, 512, 1 << 20])
 @pytest.mark.parametrize("dx,dw", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 def test_pieces_of_the_vocabulary(piece, dx, dw):
@@ -267,6 +278,32 @@ def test_long_lists_of_columns():
     c.check_forward(c.forward())
     lse = torch.from_numpy(c.lse).float().to(DEV)
     c.check_backward(c.backward(c.dloss, lse, piece=1 << 16), lse, c.dloss)
+
+
+def test_rows_that_are_no_whole_lines():
+    """X in rows that begin anywhere in a line is laid out anew where that pays: the bits are those of X in rows of whole lines."""
+    M, V, K = 1000, 20001, 4104
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    X = torch.randn(M, K, generator=gen, device=DEV).to(torch.bfloat16)
+    W = (0.02 * torch.randn(V, K, generator=gen, device=DEV)).to(torch.bfloat16)
+    target, dloss = torch.randint(0, V, (M,), generator=gen, device=DEV), torch.randn(M, generator=gen, device=DEV)
+    got = []
+    for pitch in (K, K + 8, (K + 63) // 64 * 64):
+        x, _ = padded(M, K, pitch, torch.bfloat16)
+        x.copy_(X)
+        p = loss.loss_problem(M, V, K, ldx=pitch, piece=4096)
+        out = [torch.empty(M, device=DEV) for _ in range(3)]
+        loss.flux_loss(p, x, W, target, *out, workspace(loss.FLUX_LOSS_FORWARD, p))
+        (dX, buf), dW = padded(M, K, pitch, torch.bfloat16), torch.empty_like(W)
+        loss.flux_loss_backward(p, x, W, target, out[0], dloss, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+        torch.cuda.synchronize()
+        untouched(dX, buf)
+        got.append((*out, dX, dW))
+    sizes = [loss.flux_loss_workspace_bytes(op, loss.loss_problem(M, V, K, ldx=ld, piece=4096)) for op in (0, 1) for ld in (K, (K + 63) // 64 * 64)]
+    assert sizes[0] > sizes[1] and sizes[2] > sizes[3]                # (the copy was made)
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a, b)
 
 
 def test_captured_and_replayed():
