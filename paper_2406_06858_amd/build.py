@@ -39,7 +39,7 @@ def ffn_units():
              for k in range(FFN_KINDS)]
     units += [(os.path.join(CSRC, "flux_loss_tile.hip"), os.path.join(OBJ, f"flux_loss_tile{g}.o"), [f"-DFLUX_LOSS_GRADIENT={g}"]) for g in (0, 1)]
     return units + [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), [])
-                    for name in ("flux_ffn_few", "flux_ffn_api", "flux_mx4", "flux_norm", "flux_loss")]
+                    for name in ("flux_ffn_few", "flux_ffn_api", "flux_mx4", "flux_norm", "flux_loss", "flux_loss_few_grad")]
 
 
 def build(verbose: bool = False, jobs: int | None = None) -> str:

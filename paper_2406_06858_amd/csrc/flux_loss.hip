@@ -9,6 +9,9 @@ namespace flux_ffn {
 hipError_t launch_stats(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
 hipError_t launch_dz(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
 
+hipError_t launch_dx_few(int shape, const TileArgs& a, int grid, hipStream_t s);
+hipError_t launch_dw_few(const TileArgs& t, const void* dz, long long ldz, const void* X, long long ldx, void* scratch, int M, hipStream_t s);
+
 // ---- joins ----------------------------------------------------------------------------------------------------
 // lse = m + log(s) over all runs of columns of a row; then the loss.  A workgroup takes ROWS rows, whose statistics lie side by side, and
 // shares out the runs among 256 / ROWS lanes a row; these meet in LDS, in ascending order.
@@ -106,7 +109,7 @@ static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
 static int piece_of(const flux_loss_t* p) {
   const long long all = whole_lines(p->V);
   if (p->piece) return (int)std::min<long long>(p->piece, all);
-  const long long most = std::max(2048ll, (256ll << 20) / 2 / p->M / 256 * 256);
+  const long long most = std::max(2048ll, (256ll << 20) / 2 / std::max(p->M, FEW_ROWS) / 256 * 256);
   return (int)std::min(all, most);
 }
 static bool dz_fits(const flux_loss_t* p) { return p->M * (long long)piece_of(p) < LIMIT; }
@@ -132,7 +135,7 @@ static Layout layout(const flux_loss_t* p) {
   y.dz = WS_HEADER + x;
   y.sums = y.dz + up256(2ull * p->M * piece);
   y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
-  size_t most = 0;
+  size_t most = p->M <= FEW_ROWS ? 128ull * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
   for (int cols : {std::min(piece, p->V), last})
     for (const Plan& pl : {plan_z(p, cols), plan_dx(p, cols), plan_dw(p, cols)}) most = std::max(most, pl.partial_bytes);
   y.all = y.partial + most;
@@ -328,7 +331,13 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.out[0] = f32 || last ? dX : sums;
       t.accumulate = !first && (f32 || !last);
       t.addend = !first && !f32 && last ? sums : nullptr;
-      st = launch(DX_KN, plan_dx(p, cols), t, ws, y.partial, s);
+      const Plan pl = plan_dx(p, cols);
+      if (pl.tiles_m == 1 && pl.shape >= 4 && t.bytes_b >= 96u << 20 && lw % 64 == 0) {
+        set_tiles(t, pl, ws, y.partial);
+        FFN_HIP(launch_dx_few(pl.shape, t, pl.full + pl.cut * pl.parts, s));
+      } else {
+        st = launch(DX_KN, pl, t, ws, y.partial, s);
+      }
       if (st != FLUX_OK) return st;
     }
     if (dW != nullptr) {
@@ -346,7 +355,12 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.accumulate = p->dw_accumulate;
       t.ld = lw;
       t.out[0] = static_cast<char*>(dW) + v * lw * (t.out_f32 ? 4 : 2);
-      st = launch(DW, plan_dw(p, cols), t, ws, y.partial, s);
+      if (p->M <= FEW_ROWS) {
+        t.stream = 1;
+        FFN_HIP(launch_dw_few(t, dz, ldz, X, lx, ws + y.partial, p->M, s));
+      } else {
+        st = launch(DW, plan_dw(p, cols), t, ws, y.partial, s);
+      }
       if (st != FLUX_OK) return st;
     }
   }

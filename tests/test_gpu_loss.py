@@ -220,8 +220,9 @@ def test_shards_and_their_join(ranks):
         c.check_backward(c.backward(dloss, lse), lse, dloss)
 
 
-def test_one_number_for_every_row_and_gradients_added_up():
-    c = Case(65, 300, 136, 8, pad=(0, 8))
+@pytest.mark.parametrize("M", [65, 40, 9])
+def test_one_number_for_every_row_and_gradients_added_up(M):
+    c = Case(M, 300, 136, 8, pad=(0, 8))
     lse = torch.from_numpy(c.lse).float().to(DEV)
     one = torch.tensor([0.125])
     got = c.backward(one, lse, dloss_one=1)
@@ -304,6 +305,30 @@ def test_rows_that_are_no_whole_lines():
     for other in got[1:]:
         for a, b in zip(got[0], other):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M", [1, 40])
+def test_weights_that_are_read_past_the_caches(M):
+    """Large matrices in whole lines are, others are not: the same bits."""
+    V, K = 13001, 4096
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    X = torch.randn(M, K, generator=gen, device=DEV).to(torch.bfloat16)
+    W = (0.02 * torch.randn(V, K, generator=gen, device=DEV)).to(torch.bfloat16)
+    target, dloss = torch.randint(0, V, (M,), generator=gen, device=DEV), torch.randn(M, generator=gen, device=DEV)
+    got = []
+    for pitch in (K, K + 8):
+        w, _ = padded(V, K, pitch, torch.bfloat16)
+        w.copy_(W)
+        p = loss.loss_problem(M, V, K, ldw=pitch, tile_config=6)
+        out = [torch.empty(M, device=DEV) for _ in range(3)]
+        loss.flux_loss(p, X, w, target, *out, workspace(loss.FLUX_LOSS_FORWARD, p))
+        dX, (dW, buf) = torch.empty_like(X), padded(V, K, pitch, torch.bfloat16)
+        loss.flux_loss_backward(p, X, w, target, out[0], dloss, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+        torch.cuda.synchronize()
+        untouched(dW, buf)
+        got.append((*out, dX, dW))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
 
 
 def test_captured_and_replayed():
