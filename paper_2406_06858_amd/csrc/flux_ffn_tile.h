@@ -636,7 +636,7 @@ __device__ __forceinline__ uint32_t count_in(uint32_t* word, int part, int parts
 
 template <class C, class F>
 __device__ __forceinline__ void finish_cut(const TileArgs& t, unsigned char* pool, f32x4 (&acc)[C::MI][C::NI], int cut, int part,
-                                           int job, int m0, int n0, int lane, int wave, const F& finish) {
+                                           int job, int m0, int n0, int lane, int wave, F& finish) {
   constexpr int SC1 = 16, BYTES = C::BM * C::BN * 4;
   const int tid = wave * 64 + lane, row0 = m0 + (wave >> 1) * C::WTM;
   float* const sums = t.partial + (size_t)cut * t.parts * (C::BM * C::BN);
@@ -692,9 +692,10 @@ __device__ __forceinline__ int by_die(int b, int n) {
   return die * each + (die < more ? die : more) + b / 8;
 }
 
-// One workgroup's tile or part of one; finish(job, sums, row, column, lane) takes 16 rows of a wave's part of the result (see finish_rows16).
+// One workgroup's tile or part of one.  finish(job, sums, row, column, lane) takes 16 rows of a wave's part of the result (see finish_rows16);
+// finish.ask(row, cols) asks for what it needs of the tile's rows ahead of the main loop, finish.keep(pool) leaves it in LDS behind it.
 template <class C, class F>
-__device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool, const F& finish) {
+__device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool, F& finish) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool is_cut = (int)blockIdx.x >= t.full_tiles;
   int b, cut = 0, part = 0, job = 0;
@@ -714,6 +715,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool
   const int r = b - band * t.band * t.tiles_n;
   const int m0 = (band * t.band + r % h) * C::BM, n0 = r / h * C::SUBN;
 
+  finish.ask(t, m0);
   Pipe<C> pipe;
   pipe.job = job;
   pipe.k0 = part * t.part_slabs;
@@ -729,6 +731,7 @@ __device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool
   pipe.start(t);
   pipe.run(t, acc);
   flux::wait_vm_at_most<0>();            // nothing of this wave is left in flight towards LDS that it gives up
+  finish.keep(pool);
   if (is_cut) {
     __syncthreads();                     // (a word of LDS is used again)
     finish_cut<C>(t, pool, acc, cut, part, job, m0, n0, lane, wave, finish);
@@ -754,9 +757,18 @@ __device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool
 }
 
 template <class C>
+struct Results {
+  const TileArgs& t;
+  __device__ __forceinline__ void ask(const TileArgs&, int) {}
+  __device__ __forceinline__ void keep(unsigned char*) {}
+  __device__ __forceinline__ void operator()(int job, const f32x4 (&x)[C::NI], int row0, int col0, int lane) const { finish_rows16<C>(t, job, x, row0, col0, lane); }
+};
+
+template <class C>
 __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
-  tile_body<C>(t, pool, [&](int job, const f32x4 (&x)[C::NI], int row0, int col0, int lane) { finish_rows16<C>(t, job, x, row0, col0, lane); });
+  Results<C> results{t};
+  tile_body<C>(t, pool, results);
 }
 
 }  // namespace flux_ffn

@@ -52,10 +52,11 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
 }
 
-// X in rows of whole lines, for products that read it many times.
-__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int row_vecs, long long vecs) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i < vecs) to[i / row_vecs * to_pitch + i % row_vecs] = from[i / row_vecs * pitch + i % row_vecs];
+// X in rows of whole lines, for products that read it many times.  A workgroup a row.
+__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int row_vecs) {
+  from += blockIdx.x * pitch;
+  to += blockIdx.x * to_pitch;
+  for (int i = threadIdx.x; i < row_vecs; i += 256) to[i] = from[i];
 }
 
 struct RanksArgs {
@@ -173,8 +174,8 @@ static TileArgs logits_args(const flux_loss_t* p, const void* X, long long lx, c
 
 // From here on X and its pitch are those of the copy.
 static int lay_out_x(const flux_loss_t* p, const void*& X, long long& lx, char* to, hipStream_t s) {
-  const long long vecs = (long long)p->M * (p->K / 8), pitch = whole_lines(p->K);
-  FFN_HIP(start(whole_rows_kernel, dim3((unsigned)((vecs + 255) / 256)), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, p->K / 8, vecs));
+  const long long pitch = whole_lines(p->K);
+  FFN_HIP(start(whole_rows_kernel, dim3(p->M), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, p->K / 8));
   X = to;
   lx = pitch;
   return FLUX_OK;

@@ -10,7 +10,8 @@ namespace flux_ffn {
 template <class C>
 __global__ void __launch_bounds__(C::NT, C::OCC) streamed_kernel(const TileArgs t) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
-  tile_body<C>(t, pool, [&](int job, const f32x4 (&x)[C::NI], int row0, int col0, int lane) { finish_rows16<C>(t, job, x, row0, col0, lane); });
+  Results<C> results{t};
+  tile_body<C>(t, pool, results);
 }
 
 hipError_t launch_dx_few(int shape, const TileArgs& a, int grid, hipStream_t s) {

@@ -38,63 +38,89 @@ __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s
   m = top;
 }
 
+// The largest of three.  (Of what the compiler does not know to be no signalling NaN it would make a quiet one first, an instruction a number.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+  return m;
+}
+
 // 16 rows of a wave's part of the tile: a lane holds columns 16 n + 4 (lane / 16) .. + 3 of row lane % 16.
-template <class C>
-__device__ __forceinline__ void finish_stats16(const TileArgs& t, const LossArgs& l, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
-  const int g = lane >> 4, row = row0 + (lane & 15);
-  const bool in_row = !C::EDGE || row < t.rows;
-  bool counts;
-  const int target = in_row ? target_column(l, row, t.cols, counts) : -1;
-  float m = -__builtin_inff();
+//
+// A logit costs half a max, a multiplication and addition, an exp2 (four slots) and an addition; where the contraction is short these are what takes the time.
+// exp(Z - m) is 2^(Z log2 e - m log2 e) with the second product rounded once a row: off by |m| 2^-24, as lse itself is.  Which lane has the target's
+// logit is only asked where a row of the wave has its target among these columns.  Of 7490x44009x64 us, with a comparison a logit for
+// the target and for the edge, difference and product in two and maxima made quiet / so: 235 / 113.
+template <class C, bool ALL>
+__device__ __forceinline__ void stats_of(const f32x4 (&acc)[C::NI], int left, int g, float& m, float& s) {
+  const auto in = [&](int n, int e) { return ALL || n * 16 + 4 * g + e < left; };
+  const float none = -__builtin_inff();
+  m = none;
 #pragma unroll
   for (int n = 0; n < C::NI; ++n)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (!C::EDGE || col0 + n * 16 + 4 * g + e < t.cols) m = fmaxf(m, acc[n][e]);
+    for (int e = 0; e < 4; e += 2) m = max3(m, in(n, e) ? acc[n][e] : none, in(n, e + 1) ? acc[n][e + 1] : none);
   m = fmaxf(m, __shfl_xor(m, 16));
   m = fmaxf(m, __shfl_xor(m, 32));
-  const float at = __builtin_fabsf(m) == __builtin_inff() ? 0.f : m;
-  float s = 0.f, z = 0.f;
+  const float at = __builtin_fabsf(m) == __builtin_inff() ? 0.f : -LOG2E * m;
+  s = 0.f;
 #pragma unroll
   for (int n = 0; n < C::NI; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int col = col0 + n * 16 + 4 * g + e;
-      if (!C::EDGE || col < t.cols) s += exp_of(acc[n][e] - at);
-      if (col == target) z = acc[n][e];
+      const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][e], LOG2E, at));
+      s += in(n, e) ? v : 0.f;
     }
   s += __shfl_xor(s, 16);
   s += __shfl_xor(s, 32);
-  if (!in_row) return;
-  if (g == 0) l.stats[(long long)(col0 / C::WTN) * t.rows + row] = make_float2(m, s);
-  const int off = target - col0;
-  if (target >= 0 && off >= 0 && off < C::WTN && (off >> 2 & 3) == g) l.logit[row] = z;
+}
+template <class C>
+__device__ __forceinline__ void finish_stats16(const TileArgs& t, const LossArgs& l, int target, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+  const int g = lane >> 4, row = row0 + (lane & 15), off = target - col0;
+  const bool in_row = !C::EDGE || row < t.rows;
+  float m, s;
+  if (!C::EDGE || col0 + C::WTN <= t.cols) stats_of<C, true>(acc, 0, g, m, s);
+  else stats_of<C, false>(acc, t.cols - col0, g, m, s);
+  if (in_row && g == 0) l.stats[(long long)(col0 / C::WTN) * t.rows + row] = make_float2(m, s);
+  const bool here = in_row && off >= 0 && off < C::WTN && (off >> 2 & 3) == g;
+  if (__ballot(here) == 0) return;
+  float z = 0.f;
+#pragma unroll
+  for (int n = 0; n < C::NI; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n * 16 + 4 * g + e == off) z = acc[n][e];
+  if (here) l.logit[row] = z;
 }
 
-// Columns past the last one are zeros as far as the 16 bytes that hold it reach: the products read them.
+// Columns past the last one are zeros as far as the 16 bytes that hold it reach: the products read them.  A row that does not count, or counts for 0, is zeros
+// whatever its logits are.
 template <class C>
-__device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
-  const int g = lane >> 4, row = row0 + (lane & 15), in_bf16 = (g & 1) * 32 + (g >> 1) * 16;
-  int target = -1;
-  float lse = 0.f, d = 0.f;
-  if (!C::EDGE || row < t.rows) {
-    bool counts;
-    target = target_column(l, row, t.cols, counts);
-    lse = l.lse[row];
-    d = counts ? l.dloss[l.dloss_one ? 0 : row] : 0.f;
-  }
+__device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l, int target, float at, float d, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+  const int g = lane >> 4, in_bf16 = (g & 1) * 32 + (g >> 1) * 16, off = target - col0;      // (the target's place among the wave's columns)
+  const bool target_here = __ballot(off >= 0 && off < C::WTN) != 0, all = !C::EDGE || col0 + C::WTN <= t.cols;
+  const uint32_t keep = d == 0.f ? 0u : 0xffffffffu;
   u32x4 p[C::NI / 2];
 #pragma unroll
   for (int n = 0; n < C::NI; n += 2) {
     float v[8];
     eight_columns(acc[n], acc[n + 1], v);
-    const int col = col0 + n * 16 + 16 * (g & 1) + 8 * (g >> 1);
+    const int col = n * 16 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float dz = d * (exp_of(v[e] - lse) - (col + e == target ? 1.f : 0.f));
-      v[e] = d == 0.f || (C::EDGE && col + e >= t.cols) ? 0.f : dz;      // (a row that does not count, whatever its logits are)
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, at));
+    if (target_here) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] -= col + e == off ? 1.f : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= d;
+    if (!all) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = col0 + col + e < t.cols ? v[e] : 0.f;
     }
     p[n / 2] = pack8(v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[n / 2][e] &= keep;
   }
   if constexpr (C::NI == 2) {
     store_piece<C::EDGE>(t, l.dz, 2, p[0], row0, col0, lane, in_bf16);
@@ -104,13 +130,49 @@ __device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l
   }
 }
 
+// What the rows of a tile need beside their sums: a lane asks for one row's ahead of the main loop, all lanes read them out of LDS behind it.  (Asked for 16 rows at a time where
+// they are used, every 16 rows wait for memory: 7490x44009x64 214 us.)
+template <class C, bool GRADIENT>
+struct Logits {
+  const TileArgs& t;
+  const LossArgs& l;
+  int m0, target;
+  float at, d;
+  struct Row { int target; float at, d; };
+  const Row* rows;
+  __device__ __forceinline__ void ask(const TileArgs&, int m0_) {
+    m0 = m0_;
+    const int row = m0 + (int)threadIdx.x;
+    target = -1;
+    at = d = 0.f;
+    if ((int)threadIdx.x >= C::BM || row >= t.rows) return;
+    bool counts;
+    target = target_column(l, row, t.cols, counts);
+    if constexpr (GRADIENT) {
+      at = -LOG2E * l.lse[row];
+      d = counts ? l.dloss[l.dloss_one ? 0 : row] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void keep(unsigned char* pool) {
+    static_assert(C::POOL_BYTES >= 1024 + C::BM * (int)sizeof(Row) && C::BM <= C::NT, "rows of a tile");
+    Row* const to = reinterpret_cast<Row*>(pool + 1024);          // (the words before are finish_cut's)
+    __syncthreads();                                              // all waves are done with the ring
+    if ((int)threadIdx.x < C::BM) to[threadIdx.x] = Row{target, at, d};
+    __syncthreads();
+    rows = to;
+  }
+  __device__ __forceinline__ void operator()(int, const f32x4 (&x)[C::NI], int row0, int col0, int lane) const {
+    const Row r = rows[row0 - m0 + (lane & 15)];
+    if constexpr (GRADIENT) finish_dz16<C>(t, l, r.target, r.at, r.d, x, row0, col0, lane);
+    else finish_stats16<C>(t, l, r.target, x, row0, col0, lane);
+  }
+};
+
 template <class C, bool GRADIENT>
 __global__ void __launch_bounds__(C::NT, C::OCC) logits_kernel(const TileArgs t, const LossArgs l) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
-  tile_body<C>(t, pool, [&](int, const f32x4 (&x)[C::NI], int row0, int col0, int lane) {
-    if constexpr (GRADIENT) finish_dz16<C>(t, l, x, row0, col0, lane);
-    else finish_stats16<C>(t, l, x, row0, col0, lane);
-  });
+  Logits<C, GRADIENT> logits{t, l};
+  tile_body<C>(t, pool, logits);
 }
 
 }  // namespace flux_ffn

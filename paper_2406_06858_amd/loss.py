@@ -62,7 +62,7 @@ def flux_loss_workspace_bytes(op: int, p: flux_loss_t) -> int:
 
 def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=None):
     d, f = _device(), torch.float32
-    _check(lib().flux_loss(C.byref(p), _buf(X, torch.bfloat16, d, "X"), _buf(W, torch.bfloat16, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+    _check(lib().flux_loss(p, _buf(X, torch.bfloat16, d, "X"), _buf(W, torch.bfloat16, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
                            _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), *_space(workspace, d), _stream(stream)), "flux_loss")
 
 
@@ -72,12 +72,12 @@ def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, str
         raise ValueError("as many lses as logits")
     for t in (*lses, *logits):
         _buf(t, f, d, "lses and logits")
-    _check(lib().flux_loss_join(C.byref(p), len(lses), _ptr_list(lses), _ptr_list(logits), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+    _check(lib().flux_loss_join(p, len(lses), _ptr_list(lses), _ptr_list(logits), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
                                 _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), _stream(stream)), "flux_loss_join")
 
 
 def flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace, stream=None):
     d, b, f = _device(), torch.bfloat16, torch.float32
-    _check(lib().flux_loss_backward(C.byref(p), _buf(X, b, d, "X"), _buf(W, b, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
+    _check(lib().flux_loss_backward(p, _buf(X, b, d, "X"), _buf(W, b, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
                                     _buf(lse, f, d, "lse"), _buf(dloss, f, d, "dloss"), _buf(dX, _TYPES[p.dx_dtype & 1], d, "dX"),
                                     _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_loss_backward")

@@ -77,14 +77,14 @@ def flux_norm_workspace_bytes(p: flux_norm_t) -> int:
 
 def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
     d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
-    _check(lib().flux_norm(C.byref(p), _buf(X, x, d, "X"), _buf(R, s, d, "R"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"), _buf(S, s, d, "S"),
+    _check(lib().flux_norm(p, _buf(X, x, d, "X"), _buf(R, s, d, "R"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"), _buf(S, s, d, "S"),
                            _buf(Y, _TYPES[p.out & 3], d, "Y"), _buf(scales, torch.uint8, d, "scales"), _buf(rstd, torch.float32, d, "rstd"),
                            _stream(stream)), "flux_norm")
 
 
 def flux_norm_backward(p, dY, S, W, rstd, dS=None, dR=None, dX=None, dW=None, workspace=None, stream=None):
     d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
-    _check(lib().flux_norm_backward(C.byref(p), _buf(dY, _TYPES[p.out & 1], d, "dY"), _buf(S, s, d, "S"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"),
+    _check(lib().flux_norm_backward(p, _buf(dY, _TYPES[p.out & 1], d, "dY"), _buf(S, s, d, "S"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"),
                                     _buf(rstd, torch.float32, d, "rstd"), _buf(dS, s, d, "dS"), _buf(dR, s, d, "dR"), _buf(dX, x, d, "dX"),
                                     _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_norm_backward")
 
