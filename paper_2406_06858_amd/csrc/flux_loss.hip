@@ -10,6 +10,7 @@ hipError_t launch_stats(int shape, const TileArgs& a, const LossArgs& l, bool ed
 hipError_t launch_dz(int shape, const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s);
 
 hipError_t launch_dx_few(int shape, const TileArgs& a, int grid, hipStream_t s);
+int outer_terms(int M);
 hipError_t launch_dw_few(const TileArgs& t, const void* dz, long long ldz, const void* X, long long ldx, void* scratch, int M, hipStream_t s);
 
 // ---- joins ----------------------------------------------------------------------------------------------------
@@ -126,6 +127,10 @@ static bool lays_out_x(int op, const flux_loss_t* p, const Plan& z) {
 }
 static size_t x_bytes(int op, const flux_loss_t* p, const Plan& z) { return lays_out_x(op, p, z) ? up256(2ull * p->M * whole_lines(p->K)) : 0; }
 
+// Whether dW is taken as an outer product, and not on tiles.  us of the whole call, so / on tiles: 1x32000x8192 288 / 320, 100x32000x8192 392 / 454, 100x4000x8192
+// 70 / 73; 200x4000x8192 107 / 90 (its registers leave room for two workgroups a unit then), 100x1000x1000 25.4 / 21.7 (two launches).
+static bool outer(const flux_loss_t* p) { return p->M <= 128 && (long long)p->V * p->K >= 1 << 23; }
+
 // The backward pass's workspace: the header, X in whole lines, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
 struct Layout { size_t dz, sums, partial, all; bool lays_out; };
 static Layout layout(const flux_loss_t* p) {
@@ -136,7 +141,7 @@ static Layout layout(const flux_loss_t* p) {
   y.dz = WS_HEADER + x;
   y.sums = y.dz + up256(2ull * p->M * piece);
   y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
-  size_t most = p->M <= FEW_ROWS ? 128ull * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
+  size_t most = outer(p) ? 2ull * outer_terms(p->M) * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
   for (int cols : {std::min(piece, p->V), last})
     for (const Plan& pl : {plan_z(p, cols), plan_dx(p, cols), plan_dw(p, cols)}) most = std::max(most, pl.partial_bytes);
   y.all = y.partial + most;
@@ -356,7 +361,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.accumulate = p->dw_accumulate;
       t.ld = lw;
       t.out[0] = static_cast<char*>(dW) + v * lw * (t.out_f32 ? 4 : 2);
-      if (p->M <= FEW_ROWS) {
+      if (outer(p)) {
         t.stream = 1;
         FFN_HIP(launch_dw_few(t, dz, ldz, X, lx, ws + y.partial, p->M, s));
       } else {

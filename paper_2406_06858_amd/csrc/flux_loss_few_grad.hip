@@ -1,4 +1,4 @@
-// Gradients of the loss for at most 64 rows, where the weights are everything: dX reads them once, dW writes their gradient once.
+// Gradients of the loss for few rows, where the weights are everything: dX reads them once, dW writes their gradient once.
 #include <algorithm>
 #include "flux_ffn_internal.h"
 #include "flux_loss_tile.h"
@@ -25,8 +25,8 @@ hipError_t launch_dx_few(int shape, const TileArgs& a, int grid, hipStream_t s) 
 // 16 at a time: dZ transposed, a line a row as well.
 struct OuterArgs {
   TileArgs t;                    // rows, cols, ld, out[0], out_f32, accumulate, stream
-  const __bf16* zt;              // [rows][64]
-  const __bf16* xt;              // [cols][64]
+  const __bf16* zt;              // [rows][32 KS]
+  const __bf16* xt;              // [cols][32 KS]
   int32_t rows_each;             // of a workgroup, a multiple of 16
 };
 template <int KS>
@@ -39,10 +39,10 @@ __global__ void __launch_bounds__(256) outer_kernel(const OuterArgs o) {
 #pragma unroll
   for (int k = 0; k < KS; ++k)
 #pragma unroll
-    for (int n = 0; n < 4; ++n) x[k][n] = *reinterpret_cast<const bf16x8*>(o.xt + min(col0 + n * 16 + i, o.t.cols - 1) * 64ll + k * 32 + g * 8);
+    for (int n = 0; n < 4; ++n) x[k][n] = *reinterpret_cast<const bf16x8*>(o.xt + min(col0 + n * 16 + i, o.t.cols - 1) * (32ll * KS) + k * 32 + g * 8);
   const auto ask = [&](bf16x8 (&to)[KS], int row) {
 #pragma unroll
-    for (int k = 0; k < KS; ++k) to[k] = *reinterpret_cast<const bf16x8*>(o.zt + min(row + i, o.t.rows - 1) * 64ll + k * 32 + g * 8);
+    for (int k = 0; k < KS; ++k) to[k] = *reinterpret_cast<const bf16x8*>(o.zt + min(row + i, o.t.rows - 1) * (32ll * KS) + k * 32 + g * 8);
   };
   const auto rows16 = [&](const bf16x8 (&a)[KS], int row) {
     f32x4 acc[4];
@@ -63,12 +63,12 @@ __global__ void __launch_bounds__(256) outer_kernel(const OuterArgs o) {
   }
 }
 
-// [rows of `from`][cols] to [cols][64], zeros in the place of rows that are not there.  A lane takes eight rows' numbers of one column.
+// [rows of `from`][cols] to [cols][held], zeros in the place of rows that are not there.  A lane takes eight rows' numbers of one column.
 struct TransposeArgs {
   const __bf16* from[2];
   __bf16* to[2];
   long long pitch[2];
-  int32_t rows, cols[2], groups;               // groups: workgroups of the first matrix
+  int32_t rows, held, cols[2], groups;         // groups: workgroups of the first matrix
 };
 __global__ void __launch_bounds__(256) transpose_kernel(const TransposeArgs a) {
   const int which = (int)blockIdx.x >= a.groups ? 1 : 0, col = ((int)blockIdx.x - which * a.groups) * 256 + threadIdx.x, r = blockIdx.y * 8;
@@ -77,21 +77,24 @@ __global__ void __launch_bounds__(256) transpose_kernel(const TransposeArgs a) {
   bf16x8 v;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = r + e < a.rows ? from[(r + e) * a.pitch[which]] : (__bf16)0.f;
-  *reinterpret_cast<bf16x8*>(a.to[which] + col * 64ll + r) = v;
+  *reinterpret_cast<bf16x8*>(a.to[which] + col * (long long)a.held + r) = v;
 }
+
+int outer_terms(int M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
 hipError_t launch_dw_few(const TileArgs& t, const void* dz, long long ldz, const void* X, long long ldx, void* scratch, int M, hipStream_t s) {
   OuterArgs o = {};
   o.t = t;
   __bf16* const zt = static_cast<__bf16*>(scratch);
   o.zt = zt;
-  o.xt = zt + t.rows * 64ll;
-  TransposeArgs a = {{static_cast<const __bf16*>(dz), static_cast<const __bf16*>(X)}, {zt, zt + t.rows * 64ll}, {ldz, ldx}, M, {t.rows, t.cols}, ceil_div(t.rows, 256)};
-  const hipError_t e = start(transpose_kernel, dim3(a.groups + ceil_div(t.cols, 256), M <= 32 ? 4 : 8), s, a);          // (as far as the products below read)
+  const int held = outer_terms(M);
+  o.xt = zt + t.rows * (long long)held;
+  TransposeArgs a = {{static_cast<const __bf16*>(dz), static_cast<const __bf16*>(X)}, {zt, zt + t.rows * (long long)held}, {ldz, ldx}, M, held, {t.rows, t.cols}, ceil_div(t.rows, 256)};
+  const hipError_t e = start(transpose_kernel, dim3(a.groups + ceil_div(t.cols, 256), held / 8), s, a);
   if (e != hipSuccess) return e;
   const int strips = ceil_div(t.cols, 256), groups = std::max(1, std::min(ceil_div(t.rows, 16), ceil_div(1024, strips)));
   o.rows_each = ceil_div(ceil_div(t.rows, groups), 16) * 16;
-  return start(M <= 32 ? outer_kernel<1> : outer_kernel<2>, dim3(strips, ceil_div(t.rows, o.rows_each)), s, o);
+  return start(held == 32 ? outer_kernel<1> : held == 64 ? outer_kernel<2> : outer_kernel<4>, dim3(strips, ceil_div(t.rows, o.rows_each)), s, o);
 }
 
 }  // namespace flux_ffn

@@ -331,6 +331,35 @@ def test_weights_that_are_read_past_the_caches(M):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("M", [1, 31, 33, 64, 65, 128])
+@pytest.mark.parametrize("dw,accumulate", [("bf16", 0), ("f32", 1)])
+def test_large_weight_gradients_of_few_rows(M, dw, accumulate):
+    """dW as an outer product: every count of terms, an odd number of rows, columns that end inside a strip, set and added to."""
+    V, K = 4099, 2056
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    X = torch.randn(M, K, generator=gen, device=DEV).to(torch.bfloat16)
+    W = (0.02 * torch.randn(V, K, generator=gen, device=DEV)).to(torch.bfloat16)
+    target, dloss = torch.randint(0, V, (M,), generator=gen, device=DEV), torch.randn(M, generator=gen, device=DEV)
+    z = X.double() @ W.double().t()
+    lse = torch.logsumexp(z, 1).float()
+    p = loss.loss_problem(M, V, K, ldw=K + 8, dw_dtype=dw, dw_accumulate=accumulate)
+    w, _ = padded(V, K, K + 8, torch.bfloat16)
+    w.copy_(W)
+    dW, buf = padded(V, K, K + 8, TORCH[dw])
+    loss.flux_loss_backward(p, X, w, target, lse, dloss, None, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+    torch.cuda.synchronize()
+    untouched(dW, buf)
+    pr = torch.exp(z - lse.double()[:, None])
+    dz = (pr - torch.nn.functional.one_hot(target, V)) * dloss.double()[:, None]
+    want = dz.t() @ X.double() + 7.0 * accumulate
+    # (bounds as in Case.gradients; what Z is off by from the sum of magnitudes)
+    z_off = X.double().abs() @ W.double().abs().t() * (K / 16 + 16) * 2 * U
+    dz_off = pr * dloss.double().abs()[:, None] * (z_off + (z.abs() + (z - lse.double()[:, None]).abs() + 4) * 2 * U) + dz.abs() * (HALF["bf16"] + 4 * U)
+    off = dz_off.t() @ X.double().abs() + dz.abs().t() @ X.double().abs() * (M / 16 + 16) * 2 * U
+    bad = ~((dW.double() - want).abs() <= off + (want.abs() + off) * (HALF[dw] + U))
+    assert not bad.any(), int(bad.sum())
+
+
 def test_captured_and_replayed():
     c = Case(200, 3000, 512, 14)
     target = c.target.to(DEV)
