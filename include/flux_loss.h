@@ -23,9 +23,10 @@ extern "C" {
 typedef enum { FLUX_LOSS_FORWARD = 0, FLUX_LOSS_BACKWARD = 1 } flux_loss_op_t;
 typedef enum { FLUX_TARGET_I32 = 0, FLUX_TARGET_I64 = 1 } flux_target_t;
 
-/* M, V >= 1; K >= 8, K % 8 == 0; pitches multiples of 8, at least a row long; X and W 16-byte aligned; every matrix below 2^31 elements.
- * A row whose target is not in [0, vocab) does not count: its loss is 0 and it adds nothing to a gradient (unless its X is not finite, which
- * dW does not hide).  A target of another rank's columns gives a logit of 0 here. */
+/* M, V >= 1; M <= 2^27, M V <= 2^36; K % 8 == 0; pitches multiples of 8, at least a row long; X, W, dX and dW 16-byte aligned; every matrix below 2^31
+ * elements.
+ * A row whose target is not in [0, vocab) does not count: its loss is 0 and it adds nothing to a gradient, whatever its lse and dloss are (but X has to be finite: dW is a
+ * sum over all rows, and 0 times infinity is none).  So is a row whose dloss is 0.  A target of another rank's columns gives a logit of 0 here. */
 typedef struct flux_loss {
   int32_t M, V, K;          /* tokens, this rank's columns of the vocabulary, model width       */
   int32_t target_dtype;     /* flux_target_t                                                    */
@@ -35,8 +36,8 @@ typedef struct flux_loss {
   int32_t dw_dtype;         /* of dW                                                            */
   int32_t dw_accumulate;    /* 1: dW is added to what the buffer holds (micro-batches)          */
   int64_t ldx, ldw;         /* pitches in elements, 0 = K: X and dX; W and dW                   */
-  int32_t piece;            /* columns of the vocabulary that the backward pass takes at a time: 0 = library picks; else a multiple of 64.  More
-                               than V counts as V.  M times a piece is what the workspace holds of dZ */
+  int32_t piece;            /* columns of the vocabulary that the backward pass takes at a time: 0 = library picks (up to 256 MiB of dZ); else a
+                               multiple of 64, more than V counts as V.  M times a piece, below 2^31, is what the workspace holds of dZ */
   int32_t tile_config;      /* of the forward pass and of Z in the backward pass, as in flux_glu_t (flux_ffn_tile_config_info) */
   int32_t split_k;          /* as in flux_glu_t                                                 */
   int32_t reserved;         /* must be 0                                                        */

@@ -53,11 +53,10 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
 }
 
-// X in rows of whole lines, for products that read it many times.  A workgroup a row.
-__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int row_vecs) {
-  from += blockIdx.x * pitch;
-  to += blockIdx.x * to_pitch;
-  for (int i = threadIdx.x; i < row_vecs; i += 256) to[i] = from[i];
+// X in rows of whole lines, for products that read it many times.  A workgroup takes rows in steps of all workgroups.
+__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int rows, int row_vecs) {
+  for (int row = blockIdx.x; row < rows; row += gridDim.x)
+    for (int i = threadIdx.x; i < row_vecs; i += 256) to[row * to_pitch + i] = from[row * pitch + i];
 }
 
 struct RanksArgs {
@@ -87,7 +86,8 @@ __global__ void __launch_bounds__(256) ranks_kernel(const RanksArgs a) {
 static long long pitch_x(const flux_loss_t* p) { return p->ldx ? p->ldx : p->K; }
 static long long pitch_w(const flux_loss_t* p) { return p->ldw ? p->ldw : p->K; }
 static long long vocab_of(const flux_loss_t* p) { return p->vocab ? p->vocab : p->v0 + p->V; }
-constexpr long long MAX_VOCAB = 1ll << 62;
+constexpr long long MAX_VOCAB = 1ll << 62, MAX_LOGITS = 1ll << 36;          // (at most 2^23 workgroups of the smallest tile)
+constexpr int MAX_ROWS = 1 << 27;
 
 static int validate(int op, const flux_loss_t* p) {
   if (p == nullptr || (op != FLUX_LOSS_FORWARD && op != FLUX_LOSS_BACKWARD)) return FLUX_ERR_INVALID_ARG;
@@ -97,6 +97,7 @@ static int validate(int op, const flux_loss_t* p) {
   if (p->M < 1 || p->V < 1 || p->K < 1 || p->K % 8 != 0 || p->piece % 64 != 0) return FLUX_ERR_SHAPE;
   if (p->v0 > MAX_VOCAB || p->vocab > MAX_VOCAB || vocab_of(p) < p->v0 + p->V) return FLUX_ERR_SHAPE;
   if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), p->V, p->K)) return FLUX_ERR_SHAPE;
+  if (p->M > MAX_ROWS || (long long)p->M * p->V > MAX_LOGITS) return FLUX_ERR_SHAPE;
   if (p->tile_config == FEW_CONFIG && !few_fits(LOGITS, p->M, p->V)) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;
 }
@@ -111,19 +112,21 @@ static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
 static int piece_of(const flux_loss_t* p) {
   const long long all = whole_lines(p->V);
   if (p->piece) return (int)std::min<long long>(p->piece, all);
-  const long long most = std::max(2048ll, (256ll << 20) / 2 / std::max(p->M, FEW_ROWS) / 256 * 256);
+  long long most = std::max(2048ll, (256ll << 20) / 2 / std::max(p->M, FEW_ROWS) / 256 * 256);
+  while (most > 64 && p->M * most >= LIMIT) most /= 2;
   return (int)std::min(all, most);
 }
 static bool dz_fits(const flux_loss_t* p) { return p->M * (long long)piece_of(p) < LIMIT; }
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // Whether X is laid out anew: a slab's loads, 128 bytes a row, are two lines each where rows are no whole lines, and every column tile reads X.  us, X as it is / laid
-// out anew by the caller: statistics of 1496x50257x5112 729 / 678, 1496x4000x5112 82.6 / 68.0, 200x4000x5112 24.7 / 23.6; gradients of 1496x6283x5112 279 / 262:
-// 7 % of the products that read X, for 3 us and a pass of 4.5 TB/s.
+// out anew by the caller: statistics of 1496x50257x5112 (256x256 tiles) 729 / 678, 8192x4000x5112 252 / 244, 2328x4096x7640 (256x128) 175 / 135, 512x8000x5112
+// (128x128) 58.6 / 49.2; gradients of 1496x6283x5112 279 / 262: 5 to 7 % of the products that read X on the largest tiles, 12 to 23 % on the others, which read X
+// for fewer columns each.  Against that, a launch and a pass of 4.5 TB/s.
 static bool lays_out_x(int op, const flux_loss_t* p, const Plan& z) {
   if (pitch_x(p) % 64 == 0 || z.few) return false;
-  const double product_us = 2.0 * p->M * p->V * p->K / 1.3e9;
-  return 0.07 * product_us * (op == FLUX_LOSS_BACKWARD ? 2 : 1) > 3.0 + 4.0 * p->M * p->K / 4.5e6;
+  const double gflop = 2e-9 * p->M * p->V * p->K, gain_us = z.shape == 0 ? 0.046 * gflop : 0.15 * gflop;
+  return gain_us * (op == FLUX_LOSS_BACKWARD ? 2 : 1) > 2.0 + 4.0 * p->M * p->K / 4.5e6;
 }
 static size_t x_bytes(int op, const flux_loss_t* p, const Plan& z) { return lays_out_x(op, p, z) ? up256(2ull * p->M * whole_lines(p->K)) : 0; }
 
@@ -180,7 +183,7 @@ static TileArgs logits_args(const flux_loss_t* p, const void* X, long long lx, c
 // From here on X and its pitch are those of the copy.
 static int lay_out_x(const flux_loss_t* p, const void*& X, long long& lx, char* to, hipStream_t s) {
   const long long pitch = whole_lines(p->K);
-  FFN_HIP(start(whole_rows_kernel, dim3(p->M), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, p->K / 8));
+  FFN_HIP(start(whole_rows_kernel, dim3(std::min(p->M, 1 << 16)), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, (int)p->M, p->K / 8));
   X = to;
   lx = pitch;
   return FLUX_OK;
@@ -362,7 +365,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.ld = lw;
       t.out[0] = static_cast<char*>(dW) + v * lw * (t.out_f32 ? 4 : 2);
       if (outer(p)) {
-        t.stream = 1;
+        t.stream = lw * (t.out_f32 ? 4 : 2) % 128 == 0 && aligned(t.out[0], 128);          // (parts of lines stay in the caches: us, so / past them, 31x35072x840 19 / 33, 7x2665x11624 17 / 31)
         FFN_HIP(launch_dw_few(t, dz, ldz, X, lx, ws + y.partial, p->M, s));
       } else {
         st = launch(DW, plan_dw(p, cols), t, ws, y.partial, s);

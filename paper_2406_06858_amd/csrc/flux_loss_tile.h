@@ -47,10 +47,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // 16 rows of a wave's part of the tile: a lane holds columns 16 n + 4 (lane / 16) .. + 3 of row lane % 16.
 //
-// A logit costs half a max, a multiplication and addition, an exp2 (four slots) and an addition; where the contraction is short these are what takes the time.
-// exp(Z - m) is 2^(Z log2 e - m log2 e) with the second product rounded once a row: off by |m| 2^-24, as lse itself is.  Which lane has the target's
+// A logit costs half a max, a difference, a product, an exp2 (four slots) and an addition; where the contraction is short these are what takes the time.
+// (Not 2^(Z log2 e - m log2 e) with one rounding: of logits of 10^9 the product m log2 e alone is off by a factor e^50.)  Which lane has the target's
 // logit is only asked where a row of the wave has its target among these columns.  Of 7490x44009x64 us, with a comparison a logit for
-// the target and for the edge, difference and product in two and maxima made quiet / so: 235 / 113.
+// the target and for the edge, and maxima made quiet / so: 235 / 198 (with the rows' targets asked for ahead, see Logits).
 template <class C, bool ALL>
 __device__ __forceinline__ void stats_of(const f32x4 (&acc)[C::NI], int left, int g, float& m, float& s) {
   const auto in = [&](int n, int e) { return ALL || n * 16 + 4 * g + e < left; };
@@ -62,13 +62,13 @@ __device__ __forceinline__ void stats_of(const f32x4 (&acc)[C::NI], int left, in
     for (int e = 0; e < 4; e += 2) m = max3(m, in(n, e) ? acc[n][e] : none, in(n, e + 1) ? acc[n][e + 1] : none);
   m = fmaxf(m, __shfl_xor(m, 16));
   m = fmaxf(m, __shfl_xor(m, 32));
-  const float at = __builtin_fabsf(m) == __builtin_inff() ? 0.f : -LOG2E * m;
+  const float at = __builtin_fabsf(m) == __builtin_inff() ? 0.f : m;
   s = 0.f;
 #pragma unroll
   for (int n = 0; n < C::NI; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[n][e], LOG2E, at));
+      const float v = exp_of(acc[n][e] - at);
       s += in(n, e) ? v : 0.f;
     }
   s += __shfl_xor(s, 16);
@@ -96,7 +96,7 @@ __device__ __forceinline__ void finish_stats16(const TileArgs& t, const LossArgs
 // Columns past the last one are zeros as far as the 16 bytes that hold it reach: the products read them.  A row that does not count, or counts for 0, is zeros
 // whatever its logits are.
 template <class C>
-__device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l, int target, float at, float d, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+__device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l, int target, float lse, float d, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
   const int g = lane >> 4, in_bf16 = (g & 1) * 32 + (g >> 1) * 16, off = target - col0;      // (the target's place among the wave's columns)
   const bool target_here = __ballot(off >= 0 && off < C::WTN) != 0, all = !C::EDGE || col0 + C::WTN <= t.cols;
   const uint32_t keep = d == 0.f ? 0u : 0xffffffffu;
@@ -107,7 +107,7 @@ __device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l
     eight_columns(acc[n], acc[n + 1], v);
     const int col = n * 16 + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, at));
+    for (int e = 0; e < 8; ++e) v[e] = exp_of(v[e] - lse);
     if (target_here) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] -= col + e == off ? 1.f : 0.f;
@@ -137,19 +137,19 @@ struct Logits {
   const TileArgs& t;
   const LossArgs& l;
   int m0, target;
-  float at, d;
-  struct Row { int target; float at, d; };
+  float lse, d;
+  struct Row { int target; float lse, d; };
   const Row* rows;
   __device__ __forceinline__ void ask(const TileArgs&, int m0_) {
     m0 = m0_;
     const int row = m0 + (int)threadIdx.x;
     target = -1;
-    at = d = 0.f;
+    lse = d = 0.f;
     if ((int)threadIdx.x >= C::BM || row >= t.rows) return;
     bool counts;
     target = target_column(l, row, t.cols, counts);
     if constexpr (GRADIENT) {
-      at = -LOG2E * l.lse[row];
+      lse = l.lse[row];
       d = counts ? l.dloss[l.dloss_one ? 0 : row] : 0.f;
     }
   }
@@ -157,13 +157,13 @@ struct Logits {
     static_assert(C::POOL_BYTES >= 1024 + C::BM * (int)sizeof(Row) && C::BM <= C::NT, "rows of a tile");
     Row* const to = reinterpret_cast<Row*>(pool + 1024);          // (the words before are finish_cut's)
     __syncthreads();                                              // all waves are done with the ring
-    if ((int)threadIdx.x < C::BM) to[threadIdx.x] = Row{target, at, d};
+    if ((int)threadIdx.x < C::BM) to[threadIdx.x] = Row{target, lse, d};
     __syncthreads();
     rows = to;
   }
   __device__ __forceinline__ void operator()(int, const f32x4 (&x)[C::NI], int row0, int col0, int lane) const {
     const Row r = rows[row0 - m0 + (lane & 15)];
-    if constexpr (GRADIENT) finish_dz16<C>(t, l, r.target, r.at, r.d, x, row0, col0, lane);
+    if constexpr (GRADIENT) finish_dz16<C>(t, l, r.target, r.lse, r.d, x, row0, col0, lane);
     else finish_stats16<C>(t, l, r.target, x, row0, col0, lane);
   }
 };

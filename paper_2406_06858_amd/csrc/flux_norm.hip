@@ -86,7 +86,7 @@ __device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, int l
       const uint2 codes = encode8(y, byte);
       if (k < blocks * 32) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.y) + (long long)row * (blocks * 32ll) + k) = codes;
     }
-    if (k % 32 == 0 && k / 32 < row_scales) a.scales[(long long)row * row_scales + k / 32] = (uint8_t)byte;
+    if (k % 32 == 0 && k / 32 < row_scales) a.scales[(long long)row * row_scales + k / 32] = (uint8_t)(k / 32 < blocks ? byte : 0u);      // (a row of NaN has padding too)
   }
 }
 
@@ -96,8 +96,10 @@ __device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, int l
 template <class TX, class TS, bool RESIDUAL, int LANES, int VECS, bool WHOLE>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(const NormArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
-  const int lane = threadIdx.x % LANES, row = blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (row >= a.M) return;                        // (with more than one row a workgroup there is no barrier)
+  const int lane = threadIdx.x % LANES;
+  const long long r64 = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / LANES;
+  if (r64 >= a.M) return;                        // (with more than one row a workgroup there is no barrier)
+  const int row = (int)r64;
   const TX* const x = static_cast<const TX*>(a.x) + row * a.ldx;
   const TS* const r = static_cast<const TS*>(a.r) + row * a.lds;
   TS* const s = static_cast<TS*>(a.s) + row * a.lds;
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
     Raw8<TS> h[VECS], d[VECS];
     float rstd = 0.f;
   };
-  const auto ask = [&](Row& x, int row) {
+  const auto ask = [&](Row& x, long long row) {
     if (row >= a.M) return;
     x.rstd = a.rstd[row];
 #pragma unroll
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
       if (a.ds != nullptr) x.d[i].template load<WHOLE>(static_cast<const TS*>(a.ds) + row * a.lds + k, left(k));
     }
   };
-  int row = blockIdx.x * ROWS + slot;
+  long long row = (long long)blockIdx.x * ROWS + slot;
   Row next;
   if (AHEAD) ask(next, row);
   float w[VECS][PER_LANE], dw[VECS][PER_LANE];
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
     for (int e = 0; e < PER_LANE; ++e) dw[i][e] = 0.f;
   }
   // (every slot of a workgroup takes as many turns as its first)
-  for (int turn = 0; blockIdx.x * ROWS + turn * step < a.M; ++turn, row += step) {
+  for (int turn = 0; row - slot < a.M; ++turn, row += step) {
     Row x;
     if (AHEAD) {
       x = next;
@@ -390,11 +392,17 @@ static int validate(const flux_norm_t* p) {
   return FLUX_OK;
 }
 
+// (a grid is at most 2^23 workgroups wide: see flux_mx4.hip)
+static dim3 grid_of(long long n) {
+  const long long x = std::min(n, 1ll << 23);
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
 template <class TX, class TS, bool RESIDUAL, int LANES, int VECS>
 static hipError_t go_row(const NormArgs& a, hipStream_t s) {
   constexpr int NT = LANES < 256 ? 256 : LANES, ROWS = NT / LANES;
   return start_with(a.K % PER_LANE == 0 ? norm_row_kernel<TX, TS, RESIDUAL, LANES, VECS, true> : norm_row_kernel<TX, TS, RESIDUAL, LANES, VECS, false>,
-                    dim3(ceil_div(a.M, ROWS)), NT, s, a);
+                    grid_of(ceil_div(a.M, ROWS)), NT, s, a);
 }
 template <class TX, class TS, bool RESIDUAL>
 static hipError_t go(const NormArgs& a, hipStream_t s) {

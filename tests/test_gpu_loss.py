@@ -256,6 +256,28 @@ def test_rows_that_do_not_count_hide_what_they_hold():
 
 
 @pytest.mark.parametrize("M", [5, 70])
+def test_logits_beyond_all_measure(M):
+    """Rows of equal logits of 2^100: what is left of the difference to the largest is nothing, not its rounding."""
+    V, K = 300, 64
+    X, W = torch.full((M, K), 2.0 ** 47, device=DEV).to(torch.bfloat16), torch.full((V, K), 2.0 ** 47, device=DEV).to(torch.bfloat16)
+    W[:, 0] *= 1.5                                                     # (64.5 2^94: log2 e times that is no number of 24 bits)
+    X[1] *= -1
+    target, one = torch.arange(M, device=DEV), torch.ones(1, device=DEV)
+    for config in (1, 5) + ((ffn.flux_ffn_tile_config_count(),) if M <= 64 else ()):
+        p = loss.loss_problem(M, V, K, tile_config=config, dloss_one=1, dx_dtype="f32", dw_dtype="f32")
+        lse, logit, value = (torch.empty(M, device=DEV) for _ in range(3))
+        loss.flux_loss(p, X, W, target, lse, logit, value, workspace(loss.FLUX_LOSS_FORWARD, p))
+        want = torch.full((M,), 64.5 * 2.0 ** 94, device=DEV)
+        want[1] *= -1
+        assert torch.equal(logit, want) and torch.equal(lse, want) and not value.any()
+        dX, dW = torch.empty(M, K, device=DEV), torch.empty(V, K, device=DEV)
+        loss.flux_loss_backward(p, X, W, target, lse, one, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+        # (lse has no room for log 300: every exp is 1, dZ 1 but 0 at the target)
+        dz = torch.ones(M, V, dtype=torch.float64, device=DEV) - torch.nn.functional.one_hot(target, V)
+        assert torch.equal(dX.double(), dz @ W.double()) and torch.equal(dW.double(), dz.t() @ X.double())
+
+
+@pytest.mark.parametrize("M", [5, 70])
 def test_large_and_infinite_logits(M):
     """Logits of thousands: the sums neither overflow nor vanish.  One of infinity: lse is infinite, and a column of minus infinity counts for nothing."""
     c = Case(M, 300, 64, 6, scale=4000.0)

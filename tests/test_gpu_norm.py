@@ -209,6 +209,13 @@ def test_rows_of_zeros_and_of_what_is_not_finite():
             assert not Y[1].any() and bool(Y[2].isnan().all()) and bool(Y[4, 3].isnan()) and not Y[4, 4:].any()
         else:
             assert (scales[2, :32] == 255).all() and not scales[1].any() and scales[4, 0] == 255 and not scales[4, 1:].any()
+            assert out != "mx4" or not Y[2].any()
+    # (33 numbers: two blocks, fourteen bytes of padding, which are zeros in a row of NaN as well)
+    X, R, W = case(3, 33, 4)
+    X[1, 2] = float("nan")
+    for out in ("mx4", "mx8"):
+        scales = run_forward(X, R, W, out, 1e-5)[2]
+        assert (scales[1, :2] == 255).all() and not scales[:3, 2:].any()
 
 
 def test_a_column_that_dwarfs_the_others():
@@ -282,6 +289,25 @@ def test_backward_without_a_stream_and_added_up(M, K, dw):
     dR, _, dW = run_backward(p, dY, S, W, rstd, None, ("dR", "dW"), dW=held)
     assert_within(dR, dr, dr_off + np.abs(dr) * half("f32") * 2)
     assert_within(dW, want, dw_off + (np.abs(want) + dw_off) * (half(dw) + U))
+
+
+@pytest.mark.parametrize("K", [1, 3])
+def test_more_rows_than_a_grid_is_wide(K):
+    M = (1 << 27) + 33 if K == 1 else (1 << 24) + 5
+    X = torch.randn(1 << 16, K, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(torch.bfloat16).repeat(-(-M // (1 << 16)), 1)[:M]
+    W = torch.full((K,), 2.0, device=DEV)
+    p = norm.norm_problem(M, K, w_dtype="f32")
+    Y, r = torch.zeros_like(X), torch.zeros(M, device=DEV)
+    norm.flux_norm(p, X, None, W, None, Y, None, r)
+    n = 1 << 16
+    assert torch.equal(Y[-(M % n or n):], Y[:M % n or n]) and torch.equal(Y[n:2 * n], Y[:n]) and torch.equal(r[M - M % n:], r[:M % n])
+    y, rstd = no.norm(f64(X[:1000]), f64(W), 1e-5)
+    assert_within(r[:1000], rstd, rstd * (tree(K) + 4 * U))
+    assert_within(Y[:1000], y, np.abs(y) * (tree(K) + 6 * U + half("bf16")))
+    # the gradient: of the last rows as of the first
+    dX = torch.zeros_like(X)
+    norm.flux_norm_backward(p, Y, X, W, r, None, None, dX)
+    assert torch.equal(dX[M - M % n:], dX[:M % n]) and torch.equal(dX[n:2 * n], dX[:n])
 
 
 def test_nothing_asked_for():

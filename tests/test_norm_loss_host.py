@@ -122,6 +122,7 @@ def _loss_bwd(p, ws=(PTR, 1 << 50), **ptrs):
     (dict(ldx=248), fb.FLUX_ERR_SHAPE), (dict(ldw=260), fb.FLUX_ERR_SHAPE), (dict(ldx=-256), fb.FLUX_ERR_INVALID_ARG), (dict(ldw=1 << 62), fb.FLUX_ERR_SHAPE),
     (dict(M=1 << 24), fb.FLUX_ERR_SHAPE), (dict(V=1 << 24), fb.FLUX_ERR_SHAPE), (dict(target_dtype=2), fb.FLUX_ERR_INVALID_ARG),
     (dict(v0=-1), fb.FLUX_ERR_INVALID_ARG), (dict(vocab=-1), fb.FLUX_ERR_INVALID_ARG), (dict(vocab=999), fb.FLUX_ERR_SHAPE), (dict(v0=1, vocab=1000), fb.FLUX_ERR_SHAPE),
+    (dict(M=1 << 20, V=(1 << 16) + 1, K=8), fb.FLUX_ERR_SHAPE), (dict(M=(1 << 27) + 1, V=8, K=8), fb.FLUX_ERR_SHAPE),
     (dict(v0=(1 << 62) + 1), fb.FLUX_ERR_SHAPE), (dict(vocab=(1 << 62) + 1), fb.FLUX_ERR_SHAPE),
     (dict(dloss_one=2), fb.FLUX_ERR_INVALID_ARG), (dict(dx_dtype=2), fb.FLUX_ERR_INVALID_ARG), (dict(dw_dtype=-1), fb.FLUX_ERR_INVALID_ARG),
     (dict(dw_accumulate=2), fb.FLUX_ERR_INVALID_ARG), (dict(piece=-64), fb.FLUX_ERR_INVALID_ARG), (dict(piece=100), fb.FLUX_ERR_SHAPE),
@@ -164,6 +165,14 @@ def test_the_backward_pass_holds_a_piece_and_not_the_logits():
     for piece in (0, 64, 1024, 8192):
         p = loss.loss_problem(M, V, K, piece=piece)
         assert loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_BACKWARD, p) < (2 * M * piece or 256 << 20) + 4 * M * K + (100 << 20)
+
+
+def test_many_rows_get_small_pieces():
+    p = loss.loss_problem(1 << 22, 1 << 14, 64)
+    need = loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_BACKWARD, p)
+    assert 0 < need < 2 << 32
+    p = loss.loss_problem(1 << 25, 1 << 11, 8)                        # (even 64 columns are too many)
+    assert loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_BACKWARD, p) == 0 and _loss_bwd(p) == fb.FLUX_ERR_SHAPE
 
 
 def _join(p, R, lses=(PTR, PTR), logits=(PTR, PTR), target=PTR, out=(PTR, PTR, PTR)):
