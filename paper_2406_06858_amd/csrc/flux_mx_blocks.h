@@ -28,26 +28,46 @@ __device__ __forceinline__ void load8(const T* p, int left, float (&x)[PER_LANE]
   }
 }
 
-// The same, kept as they are in memory, in words, until they are used.
+// The same, kept as they are in memory, in words, until they are used.  The lane at the end of a row that is no multiple of 8 asks for the row's last 8 numbers
+// in one load as well, and they are put in their places when they are there: an answer for each number, waited for one after another, would keep the
+// whole row's workgroup waiting.  (Rows of fewer than 8 numbers are read one by one.)
 template <class T>
 struct Raw8 {
   static constexpr int WORDS = PER_LANE * sizeof(T) / 4;
   uint32_t v[WORDS];
+  // numbers k .. k + 7 of the row of K that `row` points to
   template <bool WHOLE>
-  __device__ __forceinline__ void load(const T* p, int left) {
-    if (left >= PER_LANE) {
-      __builtin_memcpy(v, p, sizeof(v));
-    } else {
+  __device__ __forceinline__ void ask(const T* row, int k, int K) {
+    if (k + PER_LANE <= K || (!WHOLE && K >= PER_LANE && k < K)) {
+      __builtin_memcpy(v, row + (WHOLE ? k : min(k, K - PER_LANE)), sizeof(v));
+      return;
+    }
 #pragma unroll
-      for (int i = 0; i < WORDS; ++i) v[i] = 0u;
-      if (!WHOLE) {
+    for (int i = 0; i < WORDS; ++i) v[i] = 0u;
+    if (WHOLE || k >= K) return;
 #pragma unroll
-        for (int i = 0; i < PER_LANE; ++i) {
-          if (i >= left) continue;
-          if constexpr (sizeof(T) == 2) v[i / 2] |= (uint32_t)p[i] << (i % 2 * 16);
-          else v[i] = __float_as_uint(p[i]);
-        }
+    for (int i = 0; i < PER_LANE; ++i) {
+      if (k + i >= K) continue;
+      if constexpr (sizeof(T) == 2) v[i / 2] |= (uint32_t)row[k + i] << (i % 2 * 16);
+      else v[i] = __float_as_uint(row[k + i]);
+    }
+  }
+  // behind ask, ahead of the first use
+  template <bool WHOLE>
+  __device__ __forceinline__ void settle(int k, int K) {
+    const int over = k + PER_LANE - K;                    // numbers at the front that are another lane's
+    if (WHOLE || K < PER_LANE || over <= 0 || over >= PER_LANE) return;
+    const int words = over * (int)sizeof(T) / 4;
+#pragma unroll
+    for (int step = 1; step < WORDS; step *= 2)
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const uint32_t up = i + step < WORDS ? v[i + step] : 0u;
+        v[i] = words & step ? up : v[i];
       }
+    if (sizeof(T) == 2 && over % 2 != 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) v[i] = v[i] >> 16 | (i + 1 < WORDS ? v[i + 1] << 16 : 0u);
     }
   }
   // What was made of the words so far is forgotten: they alone stay in registers.

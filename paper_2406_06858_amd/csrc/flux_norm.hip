@@ -104,25 +104,34 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(con
   const TS* const r = static_cast<const TS*>(a.r) + row * a.lds;
   TS* const s = static_cast<TS*>(a.s) + row * a.lds;
   const auto left = [&](int k) { return WHOLE ? (k < a.K ? PER_LANE : 0) : a.K - k; };
-  float v[VECS][PER_LANE], w[VECS][PER_LANE];
+  Raw8<TX> raw_x[VECS];
+  Raw8<TS> raw_r[VECS];
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
     const int k = (i * LANES + lane) * PER_LANE;
-    load8<WHOLE>(x + k, left(k), v[i]);
+    raw_x[i].template ask<WHOLE>(x, k, a.K);
+    if constexpr (RESIDUAL) raw_r[i].template ask<WHOLE>(r, k, a.K);
   }
-  if constexpr (RESIDUAL) {
-    float u[VECS][PER_LANE];
+  Raw8<float> raw_w[VECS];
+  Raw8<uint16_t> raw_w16[VECS];
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) {
-      const int k = (i * LANES + lane) * PER_LANE;
-      load8<WHOLE>(r + k, left(k), u[i]);
-    }
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+    if (a.w_f32) raw_w[i].template ask<WHOLE>(static_cast<const float*>(a.w), k, a.K);
+    else raw_w16[i].template ask<WHOLE>(static_cast<const uint16_t*>(a.w), k, a.K);
+  }
+  float v[VECS][PER_LANE];
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) {
-      const int k = (i * LANES + lane) * PER_LANE;
+  for (int i = 0; i < VECS; ++i) {
+    const int k = (i * LANES + lane) * PER_LANE;
+    raw_x[i].template settle<WHOLE>(k, a.K);
+#pragma unroll
+    for (int e = 0; e < PER_LANE; ++e) v[i][e] = raw_x[i].at(e);
+    if constexpr (RESIDUAL) {
+      raw_r[i].template settle<WHOLE>(k, a.K);
       TS t[PER_LANE];
 #pragma unroll
-      for (int e = 0; e < PER_LANE; ++e) v[i][e] += u[i][e];
+      for (int e = 0; e < PER_LANE; ++e) v[i][e] += raw_r[i].at(e);
       round8(v[i], t);
 #pragma unroll
       for (int e = 0; e < PER_LANE; ++e) {
@@ -130,12 +139,6 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(con
       }
       store8<sizeof(TS) == 2, WHOLE>(s + k, left(k), t);
     }
-  }
-#pragma unroll
-  for (int i = 0; i < VECS; ++i) {
-    const int k = (i * LANES + lane) * PER_LANE;
-    if (a.w_f32) load8<WHOLE>(static_cast<const float*>(a.w) + k, left(k), w[i]);
-    else load8<WHOLE>(static_cast<const uint16_t*>(a.w) + k, left(k), w[i]);
   }
   float sum = 0.f;
 #pragma unroll
@@ -147,8 +150,18 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(con
 #pragma unroll
   for (int i = 0; i < VECS; ++i) {
     const int k = (i * LANES + lane) * PER_LANE;
+    float w[PER_LANE];
+    if (a.w_f32) {
+      raw_w[i].template settle<WHOLE>(k, a.K);
 #pragma unroll
-    for (int e = 0; e < PER_LANE; ++e) v[i][e] = v[i][e] * rstd * w[i][e];
+      for (int e = 0; e < PER_LANE; ++e) w[e] = raw_w[i].at(e);
+    } else {
+      raw_w16[i].template settle<WHOLE>(k, a.K);
+#pragma unroll
+      for (int e = 0; e < PER_LANE; ++e) w[e] = raw_w16[i].at(e);
+    }
+#pragma unroll
+    for (int e = 0; e < PER_LANE; ++e) v[i][e] = v[i][e] * rstd * w[e];
     write_y<true, WHOLE>(a, row, k, left(k), v[i]);
   }
 }
@@ -215,9 +228,9 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
       const int k = (i * LANES + lane) * PER_LANE;
-      x.g[i].template load<WHOLE>(static_cast<const TY*>(a.dy) + row * a.ldy + k, left(k));
-      x.h[i].template load<WHOLE>(static_cast<const TS*>(a.s) + row * a.lds + k, left(k));
-      if (a.ds != nullptr) x.d[i].template load<WHOLE>(static_cast<const TS*>(a.ds) + row * a.lds + k, left(k));
+      x.g[i].template ask<WHOLE>(static_cast<const TY*>(a.dy) + row * a.ldy, k, a.K);
+      x.h[i].template ask<WHOLE>(static_cast<const TS*>(a.s) + row * a.lds, k, a.K);
+      if (a.ds != nullptr) x.d[i].template ask<WHOLE>(static_cast<const TS*>(a.ds) + row * a.lds, k, a.K);
     }
   };
   long long row = (long long)blockIdx.x * ROWS + slot;
@@ -240,6 +253,13 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
       ask(next, row + step);
     } else {
       ask(x, row);
+    }
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const int k = (i * LANES + lane) * PER_LANE;
+      x.g[i].template settle<WHOLE>(k, a.K);
+      x.h[i].template settle<WHOLE>(k, a.K);
+      if (a.ds != nullptr) x.d[i].template settle<WHOLE>(k, a.K);
     }
     const float r = x.rstd;
     float sum = 0.f;
@@ -416,7 +436,13 @@ static hipError_t go(const NormArgs& a, hipStream_t s) {
   if (K <= 8192) return go_row<TX, TS, RESIDUAL, 1024, 1>(a, s);
   if (K <= 12288) return go_row<TX, TS, RESIDUAL, 768, 2>(a, s);
   if (K <= 16384) return go_row<TX, TS, RESIDUAL, 1024, 2>(a, s);
-  if (K <= 32768) return go_row<TX, TS, RESIDUAL, 1024, 4>(a, s);
+  // (registers: a row in 32 bits whose end needs putting in place has no room for four pieces)
+  constexpr bool WIDE = RESIDUAL && sizeof(TX) + sizeof(TS) == 8;
+  if constexpr (WIDE) {
+    if (K <= 32768 && a.K % PER_LANE == 0) return start_with(norm_row_kernel<TX, TS, RESIDUAL, 1024, 4, true>, dim3(a.M), 1024, s, a);
+  } else {
+    if (K <= 32768) return go_row<TX, TS, RESIDUAL, 1024, 4>(a, s);
+  }
   return start(norm_kernel<TX, TS, RESIDUAL>, dim3(a.M), s, a);
 }
 static hipError_t launch_norm(const flux_norm_t* p, const NormArgs& a, bool residual, hipStream_t s) {
@@ -431,7 +457,7 @@ struct GradPlan { int lanes, vecs, groups; };
 static GradPlan grad_plan(const flux_norm_t* p) {
   static constexpr GradPlan plans[] = {{16, 1, 512}, {64, 1, 512}, {64, 2, 512}, {256, 1, 768}, {512, 1, 512}, {768, 1, 256}, {1024, 1, 256}, {768, 2, 256}, {1024, 2, 256}};
   for (GradPlan g : plans)
-    if (p->K <= g.lanes * g.vecs * PER_LANE) {
+    if (p->K <= g.lanes * g.vecs * PER_LANE && (g.lanes * g.vecs <= 1536 || p->K % PER_LANE == 0)) {
       g.groups = std::min(g.groups, ceil_div(p->M, std::max(1, 256 / g.lanes)));
       return g;
     }
@@ -441,19 +467,19 @@ static long long partial_pitch(const flux_norm_t* p) { return (p->K + 31ll) / 32
 
 template <class TY, class TS>
 static hipError_t go_grad(const GradPlan& g, const NormGradArgs& a, hipStream_t s) {
-#define GO(LANES, VECS, AHEAD) \
+#define GO(LANES, VECS, AHEAD, AHEAD_ODD) \
   if (g.lanes == LANES && g.vecs == VECS) \
-    return start_with(a.K % PER_LANE == 0 ? norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD, true> : norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD, false>, \
+    return start_with(a.K % PER_LANE == 0 ? norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD, true> : norm_grad_row_kernel<TY, TS, LANES, VECS, AHEAD_ODD, false>, \
                       dim3(g.groups), LANES < 256 ? 256 : LANES, s, a)
-  GO(16, 1, true);
-  GO(64, 1, true);
-  GO(64, 2, true);
-  GO(256, 1, true);
-  GO(512, 1, true);
-  GO(1024, 1, true);
-  GO(768, 1, true);
-  GO(768, 2, sizeof(TS) == 2);
-  GO(1024, 2, false);
+  GO(16, 1, true, true);
+  GO(64, 1, true, true);
+  GO(64, 2, true, true);
+  GO(256, 1, true, true);
+  GO(512, 1, true, true);
+  GO(768, 1, true, true);
+  GO(1024, 1, true, true);
+  GO(768, 2, sizeof(TS) == 2, sizeof(TS) == 2 && sizeof(TY) == 2);          // (with 32 bits there are no registers for the next row)
+  if (g.lanes == 1024 && g.vecs == 2) return start_with(norm_grad_row_kernel<TY, TS, 1024, 2, false, true>, dim3(g.groups), 1024, s, a);
 #undef GO
   if (a.partial != nullptr) {
     // (ahead of dR, which may take dS's place)
