@@ -60,8 +60,9 @@ int flux_loss(const flux_loss_t* p, const void* X, const void* W, const void* ta
 int flux_loss_join(const flux_loss_t* p, int32_t R, const float* const* lses, const float* const* logits, const void* target,
                    float* lse, float* logit, float* loss, void* stream);
 
-/* Gradients of sum over rows of dloss * loss.  lse is that of the whole vocabulary.  dZ is taken in fp32 and rounded to bf16 once, as operand
- * of the two products, which accumulate in fp32 and are rounded once at the end.
+/* Gradients of sum over rows of dloss * loss.  lse is that of the whole vocabulary.  dZ / D, D the largest |dloss| of the rows that count, is taken in fp32 and
+ * rounded to bf16 once, as operand of the two products, which accumulate in fp32, take the factor D, and are rounded once at the end.  (Rows whose |dloss|
+ * is below 2^-100 of the largest lose digits.)
  *   dloss             fp32, [M] or one number
  *   dX [M,K]          dx_dtype: this rank's part of the sum over ranks.  May be NULL
  *   dW [V,K]          dw_dtype.  May be NULL

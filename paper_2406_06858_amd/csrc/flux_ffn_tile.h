@@ -61,6 +61,7 @@ struct TileArgs {
   void* out[2];                  // dW: by weight; else [0]
   __bf16 *g, *u;                 // gated: kept for the backward pass, or null
   const float* addend;           // dX: added to the sums, pitch `ld`; or null
+  const float* factor;           // dX, dW: the sums' factor; or null
   float* partial;                // [cut_tiles][parts][BM * BN]
   uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
@@ -492,7 +493,16 @@ __device__ __forceinline__ void gate(int which, float (&v)[N], const float (&u)[
 
 // 16 rows of the wave's part of the tile, out of its accumulators
 template <class C>
-__device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, const f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+__device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
+  if constexpr (C::KIND == DX_NK || C::KIND == DX_KN || C::KIND == DW) {
+    if (t.factor != nullptr) {
+      const float by = *t.factor;
+#pragma unroll
+      for (int n = 0; n < C::NI; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] *= by;
+    }
+  }
   const int g = lane >> 4, row = row0 + (lane & 15), in_bf16 = (g & 1) * 32 + (g >> 1) * 16;
   const auto bf16 = [&](void* out, int col, const u32x4 (&p)[C::NIH / 2]) {
     if constexpr (C::NIH == 2) {
@@ -761,7 +771,7 @@ struct Results {
   const TileArgs& t;
   __device__ __forceinline__ void ask(const TileArgs&, int) {}
   __device__ __forceinline__ void keep(unsigned char*) {}
-  __device__ __forceinline__ void operator()(int job, const f32x4 (&x)[C::NI], int row0, int col0, int lane) const { finish_rows16<C>(t, job, x, row0, col0, lane); }
+  __device__ __forceinline__ void operator()(int job, f32x4 (&x)[C::NI], int row0, int col0, int lane) const { finish_rows16<C>(t, job, x, row0, col0, lane); }
 };
 
 template <class C>

@@ -53,6 +53,26 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
 }
 
+// D, the largest |dloss| of the rows that count, where a tile has not all rows.  One workgroup.
+__global__ void __launch_bounds__(1024) most_kernel(const LossArgs l, int rows, float* most) {
+  __shared__ float part[16];
+  float m = 0.f;
+#pragma unroll 4
+  for (int row = threadIdx.x; row < rows; row += 1024) {
+    bool counts;
+    (void)target_column(l, row, 0, counts);
+    const float d = __builtin_fabsf(l.dloss[row]);
+    if (counts) m = fmaxf(m, d);
+  }
+  m = wave_max(m);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = m;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+  *most = sane_most(m);
+}
+
 // X in rows of whole lines, for products that read it many times.  A workgroup takes rows in steps of all workgroups.
 __global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int rows, int row_vecs) {
   for (int row = blockIdx.x; row < rows; row += gridDim.x)
@@ -134,14 +154,15 @@ static size_t x_bytes(int op, const flux_loss_t* p, const Plan& z) { return lays
 // 70 / 73; 200x4000x8192 107 / 90 (its registers leave room for two workgroups a unit then), 100x1000x1000 25.4 / 21.7 (two launches).
 static bool outer(const flux_loss_t* p) { return p->M <= 128 && (long long)p->V * p->K >= 1 << 23; }
 
-// The backward pass's workspace: the header, X in whole lines, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
+// The backward pass's workspace: the header, D, X in whole lines, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
+constexpr size_t MOST_BYTES = 256;
 struct Layout { size_t dz, sums, partial, all; bool lays_out; };
 static Layout layout(const flux_loss_t* p) {
   const int piece = piece_of(p), last = p->V - (p->V - 1) / piece * piece;
   Layout y;
   const size_t x = x_bytes(FLUX_LOSS_BACKWARD, p, plan_z(p, std::min(piece, p->V)));
   y.lays_out = x != 0;
-  y.dz = WS_HEADER + x;
+  y.dz = WS_HEADER + MOST_BYTES + x;
   y.sums = y.dz + up256(2ull * p->M * piece);
   y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
   size_t most = outer(p) ? 2ull * outer_terms(p->M) * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
@@ -303,8 +324,16 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
   const long long lw = pitch_w(p);
   const int piece = piece_of(p);
   if (y.lays_out) {
-    st = lay_out_x(p, X, lx, ws + WS_HEADER, s);
+    st = lay_out_x(p, X, lx, ws + WS_HEADER + MOST_BYTES, s);
     if (st != FLUX_OK) return st;
+  }
+  float* const most = reinterpret_cast<float*>(ws + WS_HEADER);
+  const float* const factor = p->dloss_one ? dloss : most;
+  const auto finds = [&](const Plan& pl) { return !p->dloss_one && (pl.few || pl.tiles_m == 1); };
+  if (!p->dloss_one && !finds(plan_z(p, std::min(piece, p->V)))) {
+    LossArgs l = loss_args(p, target);
+    l.dloss = dloss;
+    FFN_HIP(start_with(most_kernel, dim3(1), 1024, s, l, (int)p->M, most));
   }
   for (int v = 0; v < p->V; v += piece) {
     const int cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
@@ -318,6 +347,8 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       l.v0 += v;
       l.lse = lse;
       l.dloss = dloss;
+      l.most = most;
+      l.finds_most = finds(pl);
       l.dz = dz;
       st = launch_logits(true, pl, t, l, ws, y.partial, s);
       if (st != FLUX_OK) return st;
@@ -340,6 +371,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.out[0] = f32 || last ? dX : sums;
       t.accumulate = !first && (f32 || !last);
       t.addend = !first && !f32 && last ? sums : nullptr;
+      t.factor = factor;
       const Plan pl = plan_dx(p, cols);
       if (pl.tiles_m == 1 && pl.shape >= 4 && t.bytes_b >= 96u << 20 && lw % 64 == 0) {
         set_tiles(t, pl, ws, y.partial);
@@ -362,6 +394,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.depth = p->M;
       t.out_f32 = p->dw_dtype == FLUX_F32;
       t.accumulate = p->dw_accumulate;
+      t.factor = factor;
       t.ld = lw;
       t.out[0] = static_cast<char*>(dW) + v * lw * (t.out_f32 ? 4 : 2);
       if (outer(p)) {

@@ -10,6 +10,19 @@ __global__ void __launch_bounds__(C::NT) few_logits_kernel(const FewArgs t, cons
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
   const int run = by_die((int)blockIdx.x, (int)gridDim.x), n0 = run * C::COLS;
   const float* const red = few_body<C>(t, pool, n0);
+  float most = 1.f;
+  if (GRADIENT && !l.dloss_one) {
+    // (a lane a row)
+    const int row = threadIdx.x & 63;
+    float d = 0.f;
+    if (row < t.rows) {
+      bool counts;
+      (void)target_column(l, row, t.cols, counts);
+      d = row_dloss(l, row, counts);
+    }
+    most = sane_most(wave_max(__builtin_fabsf(d)));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *l.most = most;
+  }
   // COLS neighbouring lanes a row
   for (int e = threadIdx.x; e < C::MB * 16 * C::COLS; e += C::NT) {
     const int c = e % C::COLS, row = e / C::COLS, col = n0 + c;
@@ -18,7 +31,7 @@ __global__ void __launch_bounds__(C::NT) few_logits_kernel(const FewArgs t, cons
     bool counts;
     const int target = target_column(l, row, t.cols, counts);
     if constexpr (GRADIENT) {
-      const float d = counts ? l.dloss[l.dloss_one ? 0 : row] : 0.f;
+      const float d = row_factor(l, row_dloss(l, row, counts), most);
       const float dz = d * (exp_of(z - l.lse[row]) - (col == target ? 1.f : 0.f));
       if (col < (t.cols + 7) / 8 * 8) l.dz[row * t.ld + col] = (__bf16)(d == 0.f || col >= t.cols ? 0.f : dz);
     } else {

@@ -236,6 +236,25 @@ def test_one_number_for_every_row_and_gradients_added_up(M):
         assert_within(dW, dw64 + before, off + (np.abs(dw64 + before) + off) * (HALF[dw] + U), dw)
 
 
+@pytest.mark.parametrize("M", [6, 70, 300])
+def test_dloss_of_every_size(M):
+    """From 2^-60 to 2^60 side by side, zeros, all zeros, one infinity."""
+    c = Case(M, 333, 64, 16)
+    lse = torch.from_numpy(c.lse).float().to(DEV)
+    c.dloss *= 2.0 ** torch.randint(-60, 61, (M,), generator=torch.Generator().manual_seed(M))
+    c.dloss[1] = 0
+    c.check_backward(c.backward(c.dloss, lse, dx_dtype="f32", dw_dtype="f32"), lse, c.dloss, "f32", "f32")
+    for one in (0, 1):
+        dX, dW = c.backward(torch.zeros(1 if one else M), lse, dloss_one=one)
+        assert not dX.any() and not dW.any()
+    c.dloss[0] = float("inf")
+    dX, _ = c.backward(c.dloss, lse, dx_dtype="f32")
+    assert not bool(dX[0].isfinite().any())
+    # (the other rows have no factor then: their dZ is rounded with dloss in it, within the same bound)
+    dx64, off, _, _ = c.gradients(lse, torch.where(c.dloss == float("inf"), 0.0, c.dloss))
+    assert_within(dX[1:], dx64[1:], off[1:] + np.abs(dx64[1:]) * 2 * U, "other rows")
+
+
 def test_rows_that_do_not_count_hide_what_they_hold():
     """A row without a target and with dloss or lse that are no numbers adds nothing; a row of NaN logits keeps to itself in the forward pass."""
     c = Case(70, 200, 64, 4)
