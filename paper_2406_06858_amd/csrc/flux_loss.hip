@@ -53,16 +53,23 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
 }
 
-// D, the largest |dloss| of the rows that count, where a tile has not all rows.  One workgroup.
+// D, the largest |dloss| of the rows that count, where a tile has not all rows.  One workgroup; eight rows a lane are asked for together.
+template <class T>
 __global__ void __launch_bounds__(1024) most_kernel(const LossArgs l, int rows, float* most) {
   __shared__ float part[16];
+  const T* const target = static_cast<const T*>(l.target);
   float m = 0.f;
-#pragma unroll 4
-  for (int row = threadIdx.x; row < rows; row += 1024) {
-    bool counts;
-    (void)target_column(l, row, 0, counts);
-    const float d = __builtin_fabsf(l.dloss[row]);
-    if (counts) m = fmaxf(m, d);
+  for (int from = threadIdx.x; from < rows; from += 8 * 1024) {
+    T t[8];
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = min(from + i * 1024, rows - 1);          // (past the end: the last again)
+      t[i] = target[row];
+      d[i] = l.dloss[row];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, t[i] >= 0 && (long long)t[i] < l.vocab ? __builtin_fabsf(d[i]) : 0.f);
   }
   m = wave_max(m);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = m;
@@ -333,7 +340,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
   if (!p->dloss_one && !finds(plan_z(p, std::min(piece, p->V)))) {
     LossArgs l = loss_args(p, target);
     l.dloss = dloss;
-    FFN_HIP(start_with(most_kernel, dim3(1), 1024, s, l, (int)p->M, most));
+    FFN_HIP(start_with(l.target_i64 ? most_kernel<long long> : most_kernel<int32_t>, dim3(1), 1024, s, l, (int)p->M, most));
   }
   for (int v = 0; v < p->V; v += piece) {
     const int cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
