@@ -66,11 +66,12 @@ struct TileArgs {
   uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
 
-template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_, bool B_ONCE_ = false>
+template <int KIND_, int BM_, int BN_, int NA_, int NB_, int OCC_, bool EDGE_, bool B_ONCE_ = false, bool PHASED_ = false>
 struct Cfg {
   static constexpr int KIND = KIND_, BM = BM_, BN = BN_, NA = NA_, NB = NB_, OCC = OCC_;
   static constexpr bool EDGE = EDGE_;                                        // the tile does not divide the product
   static constexpr bool B_ONCE = B_ONCE_;                                    // one row of tiles: B's lines are read once, past the caches
+  static constexpr bool PHASED = PHASED_;                                    // rows along the contraction may begin anywhere in a line (see Phase)
   static constexpr bool MX = KIND == MX_GEMM || KIND == MX_GLU, A_T = KIND == DW;
   static constexpr bool B_NK = MX || KIND == GLU_NK || KIND == DX_NK;
   static constexpr int HALVES = KIND == GLU_NK || KIND == GLU_KN || KIND == MX_GLU ? 2 : 1;
@@ -97,6 +98,24 @@ template <bool MX>
 __device__ __forceinline__ int swizzle(int row) {
   return MX ? (row & 4) | ((row & 1) << 1) | ((row >> 1) & 1) : row & 7;
 }
+
+// Rows that are no whole lines.  Row r begins 16 (at + r step) bytes into a line (mod 128).  An instruction's lanes are answered four at a time, 64 bytes of a line at
+// once: a row's eight pieces of a slab take two such answers if it begins with a line, and mostly four if it does not.  So the pieces are dealt to
+// the row's lanes by where they lie in their line: piece q goes to slot (q + at + r step) mod 8, and a row takes three answers at most.  With an odd step that alone
+// spreads sixteen rows over the banks as the swizzle does; with an even one the swizzle comes on top (the lowest bit of the slot tells rows of different
+// parity apart then, and each further bit what it leaves).  Whole lines lie as the swizzle alone puts them.  us of logits' statistics, pieces in their order /
+// dealt so: 2328x4096x7640 175 / 157, 1496x4000x5112 82.6 / 77.6, 1496x50257x5112 729 / 711 (in whole lines 589: a line that two slabs share is fetched for
+// either).
+struct Phase {
+  int at = 0, step = 0;
+  __device__ __forceinline__ void of(const void* p, uint32_t pitch) {
+    at = (int)(reinterpret_cast<uintptr_t>(p) >> 4) & 7;
+    step = (int)(pitch >> 4) & 7;
+  }
+  __device__ __forceinline__ int mask(int row) const { return step & 1 ? 0 : row & 7; }
+  __device__ __forceinline__ int slot(int piece, int row) const { return ((piece + at + row * step) & 7) ^ mask(row); }
+  __device__ __forceinline__ int piece(int slot, int row) const { return ((slot ^ mask(row)) - at - row * step) & 7; }
+};
 
 // The scaled MFMA, accumulator in place; BYTE: which byte of the scale registers counts.
 template <int BYTE>
@@ -126,14 +145,14 @@ struct OperandLoader {
 
   uint32_t voff, pitch, lds_wave;
   int k_vec;                       // along: the lane's place in the contraction
-  __device__ __forceinline__ void init(uint32_t pitch_, int rows, int r0, int wave, int lane) {
+  __device__ __forceinline__ void init(uint32_t pitch_, int rows, int r0, int wave, int lane, const Phase* phase = nullptr) {
     pitch = pitch_;
     lds_wave = (uint32_t)(wave_row(wave) * (1024 / RPI));
     if constexpr (T) {
       const int k = wave_row(wave) + lane / SLOTS, s = lane % SLOTS ^ flux::swz_b<SLOTS>(wave_row(wave) + lane / SLOTS);
       voff = EDGE && r0 + s * 8 >= rows ? OUTSIDE : (uint32_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
     } else {
-      const int row = 8 * wave + lane / 8, s = lane % 8 ^ swizzle<MX>(row);
+      const int row = 8 * wave + lane / 8, s = phase ? phase->piece(lane % 8, row) : lane % 8 ^ swizzle<MX>(row);
       voff = (uint32_t)(r0 + row) * pitch + (uint32_t)s * 16u;
       k_vec = s * 8;
     }
@@ -207,16 +226,23 @@ struct Pipe {
     const int k = 8 * g + (i >> 2), n = r + 4 * (i & 3);
     return base + k * (R * 2) + (((n >> 3) ^ flux::swz_b<R / 8>(k)) << 4) + ((n >> 2) & 1) * 8;
   }
-  static __device__ __forceinline__ uint32_t along(uint32_t base, int row, int ks, int g) {
+  static __device__ __forceinline__ uint32_t along(uint32_t base, int row, int ks, int g, const Phase& phase) {
     const int q = C::MX ? 2 * g + ks : ks * 4 + g;
-    return base + row * 128 + ((q ^ swizzle<C::MX>(row)) << 4);
+    return base + row * 128 + ((C::PHASED ? phase.slot(q, row) : q ^ swizzle<C::MX>(row)) << 4);
   }
 
   __device__ __forceinline__ void init(const TileArgs& t, unsigned char* pool_, int m0, int n0, int wave_, int lane) {
     pool = pool_;
     wave = wave_;
-    la.init(t.pitch_a, t.rows, m0, wave, lane);
-    lb.init(t.pitch_b, t.cols, n0, wave, lane);
+    // (tiles begin at multiples of 8 rows, which leave a phase as it is, and so do the 16 and 32 rows from fragment to fragment and load to load)
+    static_assert(!C::PHASED || (!C::A_T && C::B_NK && C::HALVES == 1 && !C::MX), "one matrix each, along the contraction");
+    Phase pa, pb;
+    if constexpr (C::PHASED) {
+      pa.of(t.a[0], t.pitch_a);
+      pb.of(t.b[0], t.pitch_b);
+    }
+    la.init(t.pitch_a, t.rows, m0, wave, lane, C::PHASED ? &pa : nullptr);
+    lb.init(t.pitch_b, t.cols, n0, wave, lane, C::PHASED ? &pb : nullptr);
     const uint32_t base_a = flux::lds_address(pool), base_b = base_a + NA * C::A_BYTES;
     const int g = lane >> 4, i = lane & 15, wm = wave >> 1, wn = wave & 1, rb = wn * (C::SUBN / 2);
 #pragma unroll
@@ -224,13 +250,13 @@ struct Pipe {
 #pragma unroll
       for (int v = 0; v < NAV; ++v) {
         if constexpr (C::A_T) a[h][v] = across<C::BM>(base_a + h * 65536u, wm * C::WTM + v * 16, i, g);
-        else a[h][v] = along(base_a + h * 65536u, wm * C::WTM + i, v, g);
+        else a[h][v] = along(base_a + h * 65536u, wm * C::WTM + i, v, g, pa);
       }
 #pragma unroll
     for (int h = 0; h < B_HI; ++h)
 #pragma unroll
       for (int v = 0; v < NBV; ++v) {
-        if constexpr (C::B_NK) b[h][v] = along(base_b + h * 65536u, rb + i, v, g);
+        if constexpr (C::B_NK) b[h][v] = along(base_b + h * 65536u, rb + i, v, g, pb);
         else b[h][v] = across<C::SUBN>(base_b + h * 65536u, rb + v * 16, i, g);
       }
     if constexpr (C::MX) {

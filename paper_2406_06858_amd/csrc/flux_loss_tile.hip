@@ -13,9 +13,9 @@ static hipError_t go(const TileArgs& a, const LossArgs& l, bool edge, int grid, 
   constexpr bool G = FLUX_LOSS_GRADIENT;
   if constexpr (BM == 64) {
     if (streams_weights(a))
-      return start(edge ? logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, true, true>, G> : logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, false, true>, G>, dim3(grid), s, a, l);
+      return start(edge ? logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, true, true, true>, G> : logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, false, true, true>, G>, dim3(grid), s, a, l);
   }
-  return start(edge ? logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, true>, G> : logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, false>, G>, dim3(grid), s, a, l);
+  return start(edge ? logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, true, false, true>, G> : logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, false, false, true>, G>, dim3(grid), s, a, l);
 }
 
 #if FLUX_LOSS_GRADIENT
