@@ -163,18 +163,33 @@ static bool outer(const flux_loss_t* p) { return p->M <= 128 && (long long)p->V 
 
 // The backward pass's workspace: the header, D, X in whole lines, dZ of a piece, dX in fp32 where its pieces are summed for a result in bf16, the cut tiles' sums.
 constexpr size_t MOST_BYTES = 256;
-struct Layout { size_t dz, sums, partial, all; bool lays_out; };
+struct Layout {
+  size_t dz, sums, partial, all;
+  bool lays_out;
+  Plan z[2], dx[2], dw[2];           // of the pieces before the last one, and of the last
+};
 static Layout layout(const flux_loss_t* p) {
   const int piece = piece_of(p), last = p->V - (p->V - 1) / piece * piece;
   Layout y;
-  const size_t x = x_bytes(FLUX_LOSS_BACKWARD, p, plan_z(p, std::min(piece, p->V)));
+  size_t most = outer(p) ? 2ull * outer_terms(p->M) * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
+  for (int i = 0; i < 2; ++i) {
+    const int cols = i ? last : std::min(piece, p->V);
+    if (i && cols == std::min(piece, p->V)) {
+      y.z[1] = y.z[0];
+      y.dx[1] = y.dx[0];
+      y.dw[1] = y.dw[0];
+      break;
+    }
+    y.z[i] = plan_z(p, cols);
+    y.dx[i] = plan_dx(p, cols);
+    if (!outer(p)) y.dw[i] = plan_dw(p, cols);
+    for (const Plan* pl : {&y.z[i], &y.dx[i], &y.dw[i]}) most = std::max(most, pl->partial_bytes);
+  }
+  const size_t x = x_bytes(FLUX_LOSS_BACKWARD, p, y.z[0]);
   y.lays_out = x != 0;
   y.dz = WS_HEADER + MOST_BYTES + x;
   y.sums = y.dz + up256(2ull * p->M * piece);
   y.partial = y.sums + (p->V > piece && p->dx_dtype == FLUX_BF16 ? up256(4ull * ((p->M - 1ull) * pitch_x(p) + p->K)) : 0);
-  size_t most = outer(p) ? 2ull * outer_terms(p->M) * (piece + (size_t)p->K) : 0;          // (dW of few rows: dZ and X transposed)
-  for (int cols : {std::min(piece, p->V), last})
-    for (const Plan& pl : {plan_z(p, cols), plan_dx(p, cols), plan_dw(p, cols)}) most = std::max(most, pl.partial_bytes);
   y.all = y.partial + most;
   return y;
 }
@@ -337,17 +352,17 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
   float* const most = reinterpret_cast<float*>(ws + WS_HEADER);
   const float* const factor = p->dloss_one ? dloss : most;
   const auto finds = [&](const Plan& pl) { return !p->dloss_one && (pl.few || pl.tiles_m == 1); };
-  if (!p->dloss_one && !finds(plan_z(p, std::min(piece, p->V)))) {
+  if (!p->dloss_one && !finds(y.z[0])) {
     LossArgs l = loss_args(p, target);
     l.dloss = dloss;
     FFN_HIP(start_with(l.target_i64 ? most_kernel<long long> : most_kernel<int32_t>, dim3(1), 1024, s, l, (int)p->M, most));
   }
   for (int v = 0; v < p->V; v += piece) {
-    const int cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
+    const int of = p->V - v <= piece, cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;
     const long long ldz = whole_lines(cols);
     const uint32_t bytes_z = extent(p->M, ldz * 2, held * 2ll);
     {
-      const Plan pl = plan_z(p, cols);
+      const Plan& pl = y.z[of];
       TileArgs t = logits_args(p, X, lx, W, v, cols);
       t.ld = ldz;
       LossArgs l = loss_args(p, target);
@@ -379,7 +394,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.accumulate = !first && (f32 || !last);
       t.addend = !first && !f32 && last ? sums : nullptr;
       t.factor = factor;
-      const Plan pl = plan_dx(p, cols);
+      const Plan& pl = y.dx[of];
       if (pl.tiles_m == 1 && pl.shape >= 4 && t.bytes_b >= 96u << 20 && lw % 64 == 0) {
         set_tiles(t, pl, ws, y.partial);
         FFN_HIP(launch_dx_few(pl.shape, t, pl.full + pl.cut * pl.parts, s));
@@ -408,7 +423,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
         t.stream = lw * (t.out_f32 ? 4 : 2) % 128 == 0 && aligned(t.out[0], 128);          // (parts of lines stay in the caches: us, so / past them, 31x35072x840 19 / 33, 7x2665x11624 17 / 31)
         FFN_HIP(launch_dw_few(t, dz, ldz, X, lx, ws + y.partial, p->M, s));
       } else {
-        st = launch(DW, plan_dw(p, cols), t, ws, y.partial, s);
+        st = launch(DW, y.dw[of], t, ws, y.partial, s);
       }
       if (st != FLUX_OK) return st;
     }

@@ -28,6 +28,8 @@ struct NormGradArgs {
   const float* rstd;
   void *dr, *dx;
   float* partial;                // [groups of rows], pitch `pitch`; or null
+  void* dw;                      // where one group has all rows: dW itself; or null
+  int32_t dw_f32, dw_accumulate;
   long long ldx, lds, ldy, pitch;
   int32_t M, K;
   int32_t w_f32, x_f32;
@@ -210,6 +212,16 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormArgs a) {
   }
 }
 
+__device__ __forceinline__ void write_dw(void* dw, int k, float v, int f32, int accumulate) {
+  if (f32) {
+    float* const p = static_cast<float*>(dw) + k;
+    *p = accumulate ? *p + v : v;
+  } else {
+    __bf16* const p = static_cast<__bf16*>(dw) + k;
+    *p = (__bf16)(accumulate ? (float)*p + v : v);
+  }
+}
+
 // The row in registers, as norm_row_kernel has it; a workgroup takes rows from its first one on in steps of all workgroups' rows, keeps its lanes' part of dW
 // beside them, and leaves it as one row of `partial`.  AHEAD: the next row's numbers are asked for ahead of this one's sum.
 template <class TY, class TS, int LANES, int VECS, bool AHEAD, bool WHOLE>
@@ -296,7 +308,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
       }
     }
   }
-  if (a.partial == nullptr) return;
+  if (a.partial == nullptr && a.dw == nullptr) return;
   // the slots' sums, in their order
   if constexpr (ROWS > 1) {
     __shared__ float part[ROWS][LANES * VECS * PER_LANE];
@@ -309,13 +321,20 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_grad_row_kerne
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < ROWS; ++j) sum += part[j][k];
-      a.partial[blockIdx.x * a.pitch + k] = sum;
+      if (a.dw != nullptr) write_dw(a.dw, k, sum, a.dw_f32, a.dw_accumulate);
+      else a.partial[blockIdx.x * a.pitch + k] = sum;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
       const int k = (i * LANES + lane) * PER_LANE;
-      store8<false, WHOLE>(a.partial + blockIdx.x * a.pitch + k, left(k), dw[i]);
+      if (VECS == 1 && a.dw != nullptr) {          // (with two pieces a lane there are no registers for it)
+#pragma unroll
+        for (int e = 0; e < PER_LANE; ++e)
+          if (k + e < a.K) write_dw(a.dw, k + e, dw[i][e], a.dw_f32, a.dw_accumulate);
+      } else {
+        store8<false, WHOLE>(a.partial + blockIdx.x * a.pitch + k, left(k), dw[i]);
+      }
     }
   }
 }
@@ -388,13 +407,7 @@ __global__ void __launch_bounds__(256) norm_dw_join_kernel(const float* partial,
   float v = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) v += part[i][threadIdx.x];
-  if (f32) {
-    float* const p = static_cast<float*>(dw) + k;
-    *p = accumulate ? *p + v : v;
-  } else {
-    __bf16* const p = static_cast<__bf16*>(dw) + k;
-    *p = (__bf16)(accumulate ? (float)*p + v : v);
-  }
+  write_dw(dw, k, v, f32, accumulate);
 }
 
 // ---- checks ---------------------------------------------------------------------------------------------------
@@ -458,7 +471,9 @@ static GradPlan grad_plan(const flux_norm_t* p) {
   static constexpr GradPlan plans[] = {{16, 1, 512}, {64, 1, 512}, {64, 2, 512}, {256, 1, 768}, {512, 1, 512}, {768, 1, 256}, {1024, 1, 256}, {768, 2, 256}, {1024, 2, 256}};
   for (GradPlan g : plans)
     if (p->K <= g.lanes * g.vecs * PER_LANE && (g.lanes * g.vecs <= 1536 || p->K % PER_LANE == 0)) {
-      g.groups = std::min(g.groups, ceil_div(p->M, std::max(1, 256 / g.lanes)));
+      const int slots = std::max(1, 256 / g.lanes);
+      // (up to four turns of one workgroup are over before a second launch would be: us of 1x8192 4.9 and not 8.5)
+      g.groups = p->M <= 4 * slots && (g.vecs == 1 || g.lanes == 64) ? 1 : std::min(g.groups, ceil_div(p->M, slots));
       return g;
     }
   return GradPlan{0, 0, std::min(p->M, 64)};
@@ -545,7 +560,12 @@ int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, cons
   a.rstd = rstd;
   a.dr = dR;
   a.dx = dX;
-  a.partial = dW != nullptr ? reinterpret_cast<float*>(static_cast<char*>(workspace) + WS_HEADER) : nullptr;
+  const GradPlan g = grad_plan(p);
+  const bool direct = g.groups == 1 && (g.vecs == 1 || g.lanes == 64);
+  a.dw = direct ? dW : nullptr;
+  a.dw_f32 = p->dw_dtype == FLUX_F32;
+  a.dw_accumulate = p->dw_accumulate;
+  a.partial = dW != nullptr && !direct ? reinterpret_cast<float*>(static_cast<char*>(workspace) + WS_HEADER) : nullptr;
   a.pitch = partial_pitch(p);
   a.ldx = pitch(p->ldx, p->K);
   a.lds = pitch(p->lds, p->K);
@@ -556,9 +576,8 @@ int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, cons
   a.x_f32 = p->x_dtype == FLUX_F32;
   if (dR == nullptr && dX == nullptr && dW == nullptr) return FLUX_OK;
   const bool yf = p->out == FLUX_NORM_F32, sf = p->s_dtype == FLUX_F32;
-  const GradPlan g = grad_plan(p);
   FFN_HIP(yf ? (sf ? go_grad<float, float>(g, a, s) : go_grad<float, uint16_t>(g, a, s)) : (sf ? go_grad<uint16_t, float>(g, a, s) : go_grad<uint16_t, uint16_t>(g, a, s)));
-  if (dW != nullptr)
+  if (a.partial != nullptr)
     FFN_HIP(start(norm_dw_join_kernel, dim3(ceil_div(p->K, 32)), s, (const float*)a.partial, a.pitch, g.groups, (int)p->K, dW, (int)(p->dw_dtype == FLUX_F32), (int)p->dw_accumulate));
   return FLUX_OK;
 }

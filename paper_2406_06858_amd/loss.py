@@ -11,7 +11,7 @@ import torch
 from . import ffn
 from .binding import _ptr_list
 from .ffn import _check, _stream
-from .norm import _DT, _TYPES, _buf, _device, _space
+from .norm import _DT, _F32, _TYPES, _buf, _device, _fit, _space
 
 FLUX_LOSS_FORWARD, FLUX_LOSS_BACKWARD = 0, 1
 FLUX_TARGET_I32, FLUX_TARGET_I64 = 0, 1
@@ -48,6 +48,7 @@ def lib():
 
 _TARGET = {"i32": FLUX_TARGET_I32, "i64": FLUX_TARGET_I64, torch.int32: FLUX_TARGET_I32, torch.int64: FLUX_TARGET_I64}
 _TARGETS = (torch.int32, torch.int64)
+_BF16 = torch.bfloat16
 
 
 def loss_problem(M, V, K, v0=0, vocab=0, target_dtype="i64", dloss_one=0, dx_dtype="bf16", dw_dtype="bf16", dw_accumulate=0, ldx=0, ldw=0,
@@ -61,9 +62,15 @@ def flux_loss_workspace_bytes(op: int, p: flux_loss_t) -> int:
 
 
 def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=None):
-    d, f = _device(), torch.float32
-    _check(lib().flux_loss(p, _buf(X, torch.bfloat16, d, "X"), _buf(W, torch.bfloat16, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
-                           _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), *_space(workspace, d), _stream(stream)), "flux_loss")
+    d, t = _device(), _TARGETS[p.target_dtype & 1]
+    if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and logit.dtype is _F32
+            and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == logit.get_device()
+            and (loss is None or (loss.dtype is _F32 and loss.get_device() == d))):
+        _fit(d, X=(X, _BF16), W=(W, _BF16), target=(target, t), lse=(lse, _F32), logit=(logit, _F32), loss=(loss, _F32))
+    status = lib().flux_loss(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), logit.data_ptr(), 0 if loss is None else loss.data_ptr(),
+                             *_space(workspace, d), _stream(stream))
+    if status:
+        _check(status, "flux_loss")
 
 
 def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, stream=None):
@@ -77,7 +84,12 @@ def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, str
 
 
 def flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace, stream=None):
-    d, b, f = _device(), torch.bfloat16, torch.float32
-    _check(lib().flux_loss_backward(p, _buf(X, b, d, "X"), _buf(W, b, d, "W"), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
-                                    _buf(lse, f, d, "lse"), _buf(dloss, f, d, "dloss"), _buf(dX, _TYPES[p.dx_dtype & 1], d, "dX"),
-                                    _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_loss_backward")
+    d, t, x, w = _device(), _TARGETS[p.target_dtype & 1], _TYPES[p.dx_dtype & 1], _TYPES[p.dw_dtype & 1]
+    if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and dloss.dtype is _F32
+            and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == dloss.get_device()
+            and (dX is None or (dX.dtype is x and dX.get_device() == d)) and (dW is None or (dW.dtype is w and dW.get_device() == d))):
+        _fit(d, X=(X, _BF16), W=(W, _BF16), target=(target, t), lse=(lse, _F32), dloss=(dloss, _F32), dX=(dX, x), dW=(dW, w))
+    status = lib().flux_loss_backward(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), 0 if dX is None else dX.data_ptr(),
+                                      0 if dW is None else dW.data_ptr(), *_space(workspace, d), _stream(stream))
+    if status:
+        _check(status, "flux_loss_backward")

@@ -48,6 +48,7 @@ def lib():
 _DT = {"bf16": FLUX_BF16, "f32": FLUX_F32, torch.bfloat16: FLUX_BF16, torch.float32: FLUX_F32}
 _OUT = {"bf16": FLUX_NORM_BF16, "f32": FLUX_NORM_F32, "mx4": FLUX_NORM_MX4, "mx8": FLUX_NORM_MX8, torch.bfloat16: FLUX_NORM_BF16, torch.float32: FLUX_NORM_F32}
 _TYPES = (torch.bfloat16, torch.float32, torch.uint8, torch.uint8)          # by flux_dtype_t and flux_norm_out_t
+_U8, _F32 = torch.uint8, torch.float32
 _device = torch._C._cuda_getDevice
 
 
@@ -75,18 +76,35 @@ def flux_norm_workspace_bytes(p: flux_norm_t) -> int:
     return int(lib().flux_norm_workspace_bytes(C.byref(p)))
 
 
+def _fit(device, **tensors):
+    """Raises for the first (tensor or None, dtype) that does not fit.  (The calls look at all tensors at once and come here if one is not as it should be: as long as a launch
+    is a microsecond or two, so is a function call a tensor.)"""
+    for what, (t, dtype) in tensors.items():
+        _buf(t, dtype, device, what)
+
+
 def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
-    d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
-    _check(lib().flux_norm(p, _buf(X, x, d, "X"), _buf(R, s, d, "R"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"), _buf(S, s, d, "S"),
-                           _buf(Y, _TYPES[p.out & 3], d, "Y"), _buf(scales, torch.uint8, d, "scales"), _buf(rstd, torch.float32, d, "rstd"),
-                           _stream(stream)), "flux_norm")
+    d, x, s, w, y = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1], _TYPES[p.w_dtype & 1], _TYPES[p.out & 3]
+    if not (X.dtype is x and W.dtype is w and Y.dtype is y and d == X.get_device() == W.get_device() == Y.get_device()
+            and (R is None or (R.dtype is s and R.get_device() == d)) and (S is None or (S.dtype is s and S.get_device() == d))
+            and (scales is None or (scales.dtype is _U8 and scales.get_device() == d)) and (rstd is None or (rstd.dtype is _F32 and rstd.get_device() == d))):
+        _fit(d, X=(X, x), R=(R, s), W=(W, w), S=(S, s), Y=(Y, y), scales=(scales, _U8), rstd=(rstd, _F32))
+    status = lib().flux_norm(p, X.data_ptr(), 0 if R is None else R.data_ptr(), W.data_ptr(), 0 if S is None else S.data_ptr(), Y.data_ptr(),
+                             0 if scales is None else scales.data_ptr(), 0 if rstd is None else rstd.data_ptr(), _stream(stream))
+    if status:
+        _check(status, "flux_norm")
 
 
 def flux_norm_backward(p, dY, S, W, rstd, dS=None, dR=None, dX=None, dW=None, workspace=None, stream=None):
-    d, x, s = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1]
-    _check(lib().flux_norm_backward(p, _buf(dY, _TYPES[p.out & 1], d, "dY"), _buf(S, s, d, "S"), _buf(W, _TYPES[p.w_dtype & 1], d, "W"),
-                                    _buf(rstd, torch.float32, d, "rstd"), _buf(dS, s, d, "dS"), _buf(dR, s, d, "dR"), _buf(dX, x, d, "dX"),
-                                    _buf(dW, _TYPES[p.dw_dtype & 1], d, "dW"), *_space(workspace, d), _stream(stream)), "flux_norm_backward")
+    d, x, s, w, y, dw = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1], _TYPES[p.w_dtype & 1], _TYPES[p.out & 1], _TYPES[p.dw_dtype & 1]
+    if not (dY.dtype is y and S.dtype is s and W.dtype is w and rstd.dtype is _F32 and d == dY.get_device() == S.get_device() == W.get_device() == rstd.get_device()
+            and (dS is None or (dS.dtype is s and dS.get_device() == d)) and (dR is None or (dR.dtype is s and dR.get_device() == d))
+            and (dX is None or (dX.dtype is x and dX.get_device() == d)) and (dW is None or (dW.dtype is dw and dW.get_device() == d))):
+        _fit(d, dY=(dY, y), S=(S, s), W=(W, w), rstd=(rstd, _F32), dS=(dS, s), dR=(dR, s), dX=(dX, x), dW=(dW, dw))
+    status = lib().flux_norm_backward(p, dY.data_ptr(), S.data_ptr(), W.data_ptr(), rstd.data_ptr(), 0 if dS is None else dS.data_ptr(), 0 if dR is None else dR.data_ptr(),
+                                      0 if dX is None else dX.data_ptr(), 0 if dW is None else dW.data_ptr(), *_space(workspace, d), _stream(stream))
+    if status:
+        _check(status, "flux_norm_backward")
 
 
 def flux_mx8_row_bytes(K: int) -> int:
