@@ -395,7 +395,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.addend = !first && !f32 && last ? sums : nullptr;
       t.factor = factor;
       const Plan& pl = y.dx[of];
-      if (pl.tiles_m == 1 && pl.shape >= 4 && t.bytes_b >= 96u << 20 && lw % 64 == 0) {
+      if (pl.tiles_m == 1 && pl.shape >= 2 && t.bytes_b >= 192u << 20 && lw % 64 == 0) {
         set_tiles(t, pl, ws, y.partial);
         FFN_HIP(launch_dx_few(pl.shape, t, pl.full + pl.cut * pl.parts, s));
       } else {

@@ -15,6 +15,8 @@ __global__ void __launch_bounds__(C::NT, C::OCC) streamed_kernel(const TileArgs 
 }
 
 hipError_t launch_dx_few(int shape, const TileArgs& a, int grid, hipStream_t s) {
+  if (shape == 2) return start(streamed_kernel<Cfg<DX_KN, 128, 128, 2, 2, 2, true, true>>, dim3(grid), s, a);
+  if (shape == 3) return start(streamed_kernel<Cfg<DX_KN, 128, 128, 4, 4, 1, true, true>>, dim3(grid), s, a);
   if (shape == 4) return start(streamed_kernel<Cfg<DX_KN, 64, 128, 3, 3, 2, true, true>>, dim3(grid), s, a);
   return start(streamed_kernel<Cfg<DX_KN, 64, 128, 6, 6, 1, true, true>>, dim3(grid), s, a);
 }
@@ -92,7 +94,7 @@ hipError_t launch_dw_few(const TileArgs& t, const void* dz, long long ldz, const
   TransposeArgs a = {{static_cast<const __bf16*>(dz), static_cast<const __bf16*>(X)}, {zt, zt + t.rows * (long long)held}, {ldz, ldx}, M, held, {t.rows, t.cols}, ceil_div(t.rows, 256)};
   const hipError_t e = start(transpose_kernel, dim3(a.groups + ceil_div(t.cols, 256), held / 8), s, a);
   if (e != hipSuccess) return e;
-  const int strips = ceil_div(t.cols, 256), groups = std::max(1, std::min(ceil_div(t.rows, 16), ceil_div(1024, strips)));
+  const int strips = ceil_div(t.cols, 256), groups = std::max(1, std::min(ceil_div(t.rows, 16), (held == 128 ? 768 : 1024) / strips));          // (as many workgroups as run at once)
   o.rows_each = ceil_div(ceil_div(t.rows, groups), 16) * 16;
   return start(held == 32 ? outer_kernel<1> : held == 64 ? outer_kernel<2> : outer_kernel<4>, dim3(strips, ceil_div(t.rows, o.rows_each)), s, o);
 }

@@ -6,12 +6,13 @@ namespace flux_ffn {
 
 // One row of tiles reads the weights once: past the caches, unless they may be there from the call before, or lines are read in two pieces.
 // us, through the caches / past them: 64x128256x4096 222 / 189, 16x128256x4096 178 / 160, 64x32000x2048 44.5 / 41.3; 16x4000x8192 (66 MB) 18.4 / 20.2.
-static bool streams_weights(const TileArgs& a) { return a.tiles_m == 1 && a.bytes_b >= 96u << 20 && a.pitch_b % 128 == 0 && aligned(a.b[0], 128); }
+// (The backward pass reads them twice, and the Infinity Cache keeps what is below its 256 MiB: 128x50257x1024, 103 MB, 115 / 124 for the whole pass.)
+static bool streams_weights(const TileArgs& a) { return a.tiles_m == 1 && a.bytes_b >= (FLUX_LOSS_GRADIENT ? 192u : 96u) << 20 && a.pitch_b % 128 == 0 && aligned(a.b[0], 128); }
 
 template <int BM, int BN, int NA, int NB, int OCC>
 static hipError_t go(const TileArgs& a, const LossArgs& l, bool edge, int grid, hipStream_t s) {
   constexpr bool G = FLUX_LOSS_GRADIENT;
-  if constexpr (BM == 64) {
+  if constexpr (BM <= 128) {
     if (streams_weights(a))
       return start(edge ? logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, true, true, true>, G> : logits_kernel<Cfg<DX_NK, BM, BN, NA, NB, OCC, false, true, true>, G>, dim3(grid), s, a, l);
   }

@@ -348,10 +348,10 @@ def test_rows_that_are_no_whole_lines():
             assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("M", [1, 40])
-def test_weights_that_are_read_past_the_caches(M):
+@pytest.mark.parametrize("M,config", [(1, 6), (40, 5), (64, 6), (65, 3), (100, 4)])
+def test_weights_that_are_read_past_the_caches(M, config):
     """Large matrices in whole lines are, others are not: the same bits."""
-    V, K = 13001, 4096
+    V, K = 25001, 4096
     gen = torch.Generator(device=DEV).manual_seed(M)
     X = torch.randn(M, K, generator=gen, device=DEV).to(torch.bfloat16)
     W = (0.02 * torch.randn(V, K, generator=gen, device=DEV)).to(torch.bfloat16)
@@ -360,7 +360,7 @@ def test_weights_that_are_read_past_the_caches(M):
     for pitch in (K, K + 8):
         w, _ = padded(V, K, pitch, torch.bfloat16)
         w.copy_(W)
-        p = loss.loss_problem(M, V, K, ldw=pitch, tile_config=6)
+        p = loss.loss_problem(M, V, K, ldw=pitch, tile_config=config)
         out = [torch.empty(M, device=DEV) for _ in range(3)]
         loss.flux_loss(p, X, w, target, *out, workspace(loss.FLUX_LOSS_FORWARD, p))
         dX, (dW, buf) = torch.empty_like(X), padded(V, K, pitch, torch.bfloat16)

@@ -24,5 +24,5 @@ def test_nothing_between_the_written_out_instructions(tmp_path):
             bad, n = _check_stores([line for line in lines if line and not line.endswith(":")])
             assert bad is None, f"{name}: {bad}"
             stores += n
-    # statistics and dZ, masked and not, those of the two tiles of 64 rows with streamed weights too; and dX of these two
-    assert kernels == 2 * 2 * (TILES + 2) + 2 and stores > 0
+    # statistics and dZ, masked and not, those of the four tiles of up to 128 rows with streamed weights too; and dX of these four
+    assert kernels == 2 * 2 * (TILES + 4) + 4 and stores > 0
