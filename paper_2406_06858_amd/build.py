@@ -37,6 +37,7 @@ def ffn_units():
     """(source, object, further flags) of the second library."""
     units = [(os.path.join(CSRC, "flux_ffn_tile.hip"), os.path.join(OBJ, f"flux_ffn_tile{k}.o"), [f"-DFLUX_FFN_KIND={k}"])
              for k in range(FFN_KINDS)]
+    units += [(os.path.join(CSRC, "flux_ffn_tile.hip"), os.path.join(OBJ, f"flux_ffn_scaled{k}.o"), [f"-DFLUX_FFN_KIND={k}", "-DFLUX_FFN_SCALED"]) for k in (3, 4)]
     units += [(os.path.join(CSRC, "flux_loss_tile.hip"), os.path.join(OBJ, f"flux_loss_tile{g}.o"), [f"-DFLUX_LOSS_GRADIENT={g}"]) for g in (0, 1)]
     return units + [(os.path.join(CSRC, f"{name}.hip"), os.path.join(OBJ, f"{name}.o"), [])
                     for name in ("flux_ffn_few", "flux_ffn_api", "flux_mx4", "flux_norm", "flux_loss", "flux_loss_few_grad")]

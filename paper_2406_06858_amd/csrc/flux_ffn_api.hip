@@ -204,7 +204,7 @@ int launch(int kind, const Plan& pl, TileArgs& t, void* ws, size_t partial_at, h
   const int size = t.out_f32 ? 4 : 2;
   t.stream = t.ld * size % 128 == 0 && aligned(t.out[0], 128) && aligned(t.out[1], 128) && aligned(t.g, 128) && aligned(t.u, 128) &&
              (halves_of(kind) == 2 || t.slabs >= 20);
-  FFN_HIP(launchers[kind](pl.shape, t, pl.edge, pl.full + pl.cut * pl.parts, s));
+  FFN_HIP((t.factor == nullptr ? launchers[kind] : kind == DW ? launch_scaled4 : launch_scaled3)(pl.shape, t, pl.edge, pl.full + pl.cut * pl.parts, s));
   return FLUX_OK;
 }
 

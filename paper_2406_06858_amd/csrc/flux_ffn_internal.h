@@ -20,14 +20,16 @@ constexpr Shape SHAPES[] = {
     {64, 128, 2, {{0.63, 0.28, 3.1, 2.1, 9.0}, {0.83, 0.40, 3.9, 2.3, 6.4}}},  {64, 128, 1, {{0.34, 0.30, 3.2, 2.5, 4.8}, {0.41, 0.40, 4.5, 3.0, 2.6}}}};
 constexpr int N_SHAPES = 6;
 
-#define FFN_DECLARE(KIND) hipError_t launch_tile##KIND(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s);
-FFN_DECLARE(0)
-FFN_DECLARE(1)
-FFN_DECLARE(2)
-FFN_DECLARE(3)
-FFN_DECLARE(4)
-FFN_DECLARE(5)
-FFN_DECLARE(6)
+#define FFN_DECLARE(NAME) hipError_t launch_##NAME(int shape, const TileArgs& a, bool edge, int grid, hipStream_t s);
+FFN_DECLARE(tile0)
+FFN_DECLARE(tile1)
+FFN_DECLARE(tile2)
+FFN_DECLARE(tile3)
+FFN_DECLARE(tile4)
+FFN_DECLARE(tile5)
+FFN_DECLARE(tile6)
+FFN_DECLARE(scaled3)
+FFN_DECLARE(scaled4)
 #undef FFN_DECLARE
 
 // How a product is run.

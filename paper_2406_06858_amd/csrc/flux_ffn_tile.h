@@ -60,8 +60,9 @@ struct TileArgs {
   int64_t ld;                    // pitch of the results, elements
   void* out[2];                  // dW: by weight; else [0]
   __bf16 *g, *u;                 // gated: kept for the backward pass, or null
-  const float* addend;           // dX: added to the sums, pitch `ld`; or null
-  const float* factor;           // dX, dW: the sums' factor; or null
+  // SCALED kernels of dX and dW
+  const float* factor;           // the sums' factor
+  const float* addend;           // dX: added to the product, pitch `ld`, in the place of `accumulate`; or null
   float* partial;                // [cut_tiles][parts][BM * BN]
   uint32_t* counters;            // a word a cut tile, COUNTER_STRIDE apart, 0 between calls
 };
@@ -73,6 +74,7 @@ struct Cfg {
   static constexpr bool B_ONCE = B_ONCE_;                                    // one row of tiles: B's lines are read once, past the caches
   static constexpr bool PHASED = PHASED_;                                    // rows along the contraction may begin anywhere in a line (see Phase)
   static constexpr bool MX = KIND == MX_GEMM || KIND == MX_GLU, A_T = KIND == DW;
+  static constexpr bool TIGHT = (KIND == DX_NK || KIND == DX_KN) && BM == 256 && BN == 256;
   static constexpr bool B_NK = MX || KIND == GLU_NK || KIND == DX_NK;
   static constexpr int HALVES = KIND == GLU_NK || KIND == GLU_KN || KIND == MX_GLU ? 2 : 1;
   static constexpr int NT = 256, BK = 64;
@@ -131,7 +133,7 @@ __device__ __forceinline__ void mfma_scaled(f32x4& acc, const u32x4& a, const u3
 //   along   rows of 128 bytes, one instruction 8 rows;
 //   across  (T) one row per step of the contraction, R values each, one instruction 512 / R of those.
 // (The same patterns as DmaLoader's.)  A lane outside the matrix loads from outside the buffer's records: zeros.
-template <int R, bool T, bool EDGE, bool MX, bool ONCE = false>
+template <int R, bool T, bool EDGE, bool MX, bool ONCE, bool TIGHT>
 struct OperandLoader {
   static constexpr int RPI = T ? 512 / R : 8;
   static constexpr int INSTR = (T ? 64 : R) / RPI / 4;         // per wave
@@ -143,7 +145,8 @@ struct OperandLoader {
   static constexpr __device__ int instr_row(int p) { return RPI == 8 ? p * 32 : RPI == 4 ? 16 * p : 4 * (p & 1) + 16 * (p >> 1); }
   static_assert(RPI == 2 || RPI == 4 || RPI == 8, "the swizzle must not depend on the instruction");
 
-  uint32_t voff, pitch, lds_wave;
+  uint32_t voff, pitch;
+  mutable uint32_t lds_wave;
   int k_vec;                       // along: the lane's place in the contraction
   __device__ __forceinline__ void init(uint32_t pitch_, int rows, int r0, int wave, int lane, const Phase* phase = nullptr) {
     pitch = pitch_;
@@ -161,7 +164,11 @@ struct OperandLoader {
   // where the whole offset is the lane's (a sum that stays at the largest number instead of wrapping): what is left to ask is whether a slab's last
   // pieces are in the row (once a slab), and whether rows of a contraction that lies across begin at all (uniform).  With a mask for every load the
   // 256x256 tile ran out of scalar registers: logits of 8192x4000x8192 409 us, 366 for 4096 columns without masks.
+  // TIGHT: the place in LDS is added up at each load.  Left to itself the compiler keeps all forty places of the large tile in scalar registers; beside the
+  // segments of dX and logits there is no room for these, and they came back from vector lanes one by one.  us without / with: gradients of the loss
+  // 8192x32000x8192 8518 / 8470, statistics of 8192x4000x8192 359 / 356, dX of 8192x8192 over two times 3584 633 / 625; dW, whose registers suffice, 617 / 624.
   __device__ __forceinline__ void load(int d, const __amdgpu_buffer_rsrc_t& rsrc, int k, int depth, unsigned char* tile) const {
+    if constexpr (TIGHT) asm volatile("" : "+s"(lds_wave));
     uint32_t at = voff, from = T ? (uint32_t)(k + instr_row(d)) * pitch : (uint32_t)k * 2u + (uint32_t)instr_row(d) * pitch;
     if constexpr (EDGE) {
       if constexpr (T) from = k + instr_row(d) < depth ? from : OUTSIDE;
@@ -181,8 +188,8 @@ struct Slab {
 
 template <class C>
 struct Pipe {
-  typedef OperandLoader<C::BM, C::A_T, C::EDGE, C::MX> LdA;
-  typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX, C::B_ONCE> LdB;
+  typedef OperandLoader<C::BM, C::A_T, C::EDGE, C::MX, false, C::TIGHT> LdA;
+  typedef OperandLoader<C::SUBN, !C::B_NK, C::EDGE, C::MX, C::B_ONCE, C::TIGHT> LdB;
   static constexpr int NA = C::NA, NB = C::NB;
   static constexpr bool A_LEADS = NA > NB;                               // by one slab
   static constexpr int U = NA != NB ? NA * NB : NB;      // slabs after which the rings are where they were
@@ -517,17 +524,18 @@ __device__ __forceinline__ void gate(int which, float (&v)[N], const float (&u)[
   }
 }
 
-// 16 rows of the wave's part of the tile, out of its accumulators
-template <class C>
+// 16 rows of the wave's part of the tile, out of its accumulators.  SCALED: the results are the sums times a factor, and dX may have an addend elsewhere than in its
+// place.  (A kernel of its own: in the gated block's the branches alone cost dX of 8192x8192 over two times 3584 662 us to 673.)
+template <class C, bool SCALED>
 __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 (&acc)[C::NI], int row0, int col0, int lane) {
-  if constexpr (C::KIND == DX_NK || C::KIND == DX_KN || C::KIND == DW) {
-    if (t.factor != nullptr) {
-      const float by = *t.factor;
+  static_assert(!SCALED || C::KIND == DX_KN || C::KIND == DW, "");
+  constexpr bool ADDEND = SCALED && C::KIND == DX_KN;
+  if constexpr (SCALED) {
+    const float by = *t.factor;
 #pragma unroll
-      for (int n = 0; n < C::NI; ++n)
+    for (int n = 0; n < C::NI; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[n][e] *= by;
-    }
+      for (int e = 0; e < 4; ++e) acc[n][e] *= by;
   }
   const int g = lane >> 4, row = row0 + (lane & 15), in_bf16 = (g & 1) * 32 + (g >> 1) * 16;
   const auto bf16 = [&](void* out, int col, const u32x4 (&p)[C::NIH / 2]) {
@@ -556,16 +564,16 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 
   // What is added to, asked for before the first of it is used (it may lie where the results go, so no load would pass a store).
   f32x4 old[C::HALVES == 2 ? 1 : C::NI];
   if constexpr (C::HALVES == 1) {
-    const bool sums = (C::KIND == DX_NK || C::KIND == DX_KN) && t.addend != nullptr;
-    if (sums || (t.accumulate && t.out_f32)) {
+    const bool in_f32 = ADDEND ? t.addend != nullptr : t.accumulate && t.out_f32;
+    if (in_f32) {
       // four columns a block
-      const float* const from = (sums ? t.addend : static_cast<const float*>(t.out[job])) + row * t.ld;
+      const float* const from = (ADDEND ? t.addend : static_cast<const float*>(t.out[job])) + row * t.ld;
 #pragma unroll
       for (int n = 0; n < C::NI; ++n) {
         const int col = col0 + n * 16 + 4 * g;
         if (!C::EDGE || (row < t.rows && col < t.cols)) old[n] = *reinterpret_cast<const f32x4*>(from + col);
       }
-    } else if (t.accumulate) {
+    } else if (!ADDEND && t.accumulate) {
       // eight columns of two blocks, in bf16
 #pragma unroll
       for (int n = 0; n < C::NI; n += 2) {
@@ -575,7 +583,7 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (sums || (t.accumulate && t.out_f32)) {
+    if (in_f32) {
 #pragma unroll
       for (int n = 0; n < C::NI; ++n)
 #pragma unroll
@@ -592,11 +600,11 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 
         eight_columns(acc[n], acc[n + 1], v);
         eight_columns(acc[C::NIH + n], acc[C::NIH + n + 1], u);
         gate<false>(t.act, v, u);
-      } else if ((C::KIND == DX_NK || C::KIND == DX_KN) && t.addend != nullptr) {
+      } else if (ADDEND && t.addend != nullptr) {
         eight_columns(old[n], old[n + 1], v);
       } else {
         eight_columns(acc[n], acc[n + 1], v);
-        if (t.accumulate) {
+        if (!ADDEND && t.accumulate) {
           const bf16x8 o = __builtin_bit_cast(bf16x8, old[n]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += (float)o[e];
@@ -616,7 +624,7 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 
           const f32x4& y = acc[C::NIH + n + h];
           const float u[4] = {y[0], y[1], y[2], y[3]};
           gate<true>(t.act, v, u);
-        } else if (t.accumulate) {
+        } else if (ADDEND ? t.addend != nullptr : t.accumulate != 0) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = old[n + h][e];
         }
@@ -792,18 +800,25 @@ __device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool
   }
 }
 
-template <class C>
+template <class C, bool SCALED>
 struct Results {
   const TileArgs& t;
   __device__ __forceinline__ void ask(const TileArgs&, int) {}
   __device__ __forceinline__ void keep(unsigned char*) {}
-  __device__ __forceinline__ void operator()(int job, f32x4 (&x)[C::NI], int row0, int col0, int lane) const { finish_rows16<C>(t, job, x, row0, col0, lane); }
+  __device__ __forceinline__ void operator()(int job, f32x4 (&x)[C::NI], int row0, int col0, int lane) const { finish_rows16<C, SCALED>(t, job, x, row0, col0, lane); }
 };
 
 template <class C>
 __global__ void __launch_bounds__(C::NT, C::OCC) tile_kernel(const TileArgs t) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
-  Results<C> results{t};
+  Results<C, false> results{t};
+  tile_body<C>(t, pool, results);
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::NT, C::OCC) scaled_kernel(const TileArgs t) {
+  __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
+  Results<C, true> results{t};
   tile_body<C>(t, pool, results);
 }
 

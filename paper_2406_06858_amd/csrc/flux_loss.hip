@@ -391,8 +391,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       // sums of pieces stay in fp32: in dX, or in the workspace until the last piece rounds them
       t.out_f32 = f32 || !last;
       t.out[0] = f32 || last ? dX : sums;
-      t.accumulate = !first && (f32 || !last);
-      t.addend = !first && !f32 && last ? sums : nullptr;
+      t.addend = first ? nullptr : f32 ? static_cast<const float*>(dX) : sums;
       t.factor = factor;
       const Plan& pl = y.dx[of];
       if (pl.tiles_m == 1 && pl.shape >= 2 && t.bytes_b >= 192u << 20 && lw % 64 == 0) {

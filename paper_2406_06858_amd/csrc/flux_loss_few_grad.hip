@@ -10,7 +10,7 @@ namespace flux_ffn {
 template <class C>
 __global__ void __launch_bounds__(C::NT, C::OCC) streamed_kernel(const TileArgs t) {
   __shared__ __attribute__((aligned(1024))) unsigned char pool[C::POOL_BYTES];
-  Results<C> results{t};
+  Results<C, true> results{t};
   tile_body<C>(t, pool, results);
 }
 
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(256) outer_kernel(const OuterArgs o) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[k][n], a[k], acc[n], 0, 0, 0);
     }
-    finish_rows16<C>(o.t, 0, acc, row, col0, lane);
+    finish_rows16<C, true>(o.t, 0, acc, row, col0, lane);
   };
   ask(z[0], first);
   for (int row = first; row < last; row += 32) {
