@@ -14,8 +14,9 @@ int outer_terms(int M);
 hipError_t launch_dw_few(const TileArgs& t, const void* dz, long long ldz, const void* X, long long ldx, void* scratch, int M, hipStream_t s);
 
 // ---- joins ----------------------------------------------------------------------------------------------------
-// lse = m + log(s) over all runs of columns of a row; then the loss.  A workgroup takes ROWS rows, whose statistics lie side by side, and
-// shares out the runs among 256 / ROWS lanes a row; these meet in LDS, in ascending order.
+// lse = m + log(s) over all runs of columns of a row; then the loss.  A workgroup takes ROWS rows, whose statistics lie side by side, and shares out the runs among
+// 256 / ROWS lanes a row; these meet in LDS, in ascending order.  (Of few rows with many runs a workgroup takes few: 1496 rows of 394 runs 6.3 us with four, 12.4
+// with sixteen.)
 struct StatsArgs {
   const float2* stats;           // [runs][rows]
   int32_t runs, rows, cols;
@@ -53,18 +54,18 @@ __global__ void __launch_bounds__(256) stats_kernel(const StatsArgs a) {
   if (a.value != nullptr) a.value[row] = counts ? lse - z : 0.f;
 }
 
-// D, the largest |dloss| of the rows that count, where a tile has not all rows.  One workgroup; eight rows a lane are asked for together.
-template <class T>
-__global__ void __launch_bounds__(1024) most_kernel(const LossArgs l, int rows, float* most) {
-  __shared__ float part[16];
+// D, the largest |dloss| of the rows that count, where a tile has not all rows.  One workgroup of NT lanes; eight rows a lane are asked for together.
+template <class T, int NT>
+__device__ __forceinline__ void find_most(const LossArgs& l, int rows, float* most) {
+  __shared__ float part[NT / 64];
   const T* const target = static_cast<const T*>(l.target);
   float m = 0.f;
-  for (int from = threadIdx.x; from < rows; from += 8 * 1024) {
+  for (int from = threadIdx.x; from < rows; from += 8 * NT) {
     T t[8];
     float d[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = min(from + i * 1024, rows - 1);          // (past the end: the last again)
+      const int row = min(from + i * NT, rows - 1);          // (past the end: the last again)
       t[i] = target[row];
       d[i] = l.dloss[row];
     }
@@ -76,13 +77,25 @@ __global__ void __launch_bounds__(1024) most_kernel(const LossArgs l, int rows, 
   __syncthreads();
   if (threadIdx.x != 0) return;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+  for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, part[i]);
   *most = sane_most(m);
 }
+template <int NT>
+__device__ __forceinline__ void find_most_of(const LossArgs& l, int rows, float* most) {
+  if (l.target_i64) find_most<long long, NT>(l, rows, most);
+  else find_most<int32_t, NT>(l, rows, most);
+}
+__global__ void __launch_bounds__(1024) most_kernel(const LossArgs l, int rows, float* most) { find_most_of<1024>(l, rows, most); }
 
-// X in rows of whole lines, for products that read it many times.  A workgroup takes rows in steps of all workgroups.
-__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int rows, int row_vecs) {
-  for (int row = blockIdx.x; row < rows; row += gridDim.x)
+// X in rows of whole lines, for products that read it many times.  A workgroup takes rows in steps of all workgroups.  Where `most` is asked for, one workgroup more
+// finds it: a launch of its own takes 5 us.
+__global__ void __launch_bounds__(256) whole_rows_kernel(const uint4* from, uint4* to, long long pitch, long long to_pitch, int rows, int row_vecs, const LossArgs l, float* most) {
+  const int step = gridDim.x - (most != nullptr);
+  if ((int)blockIdx.x == step) {
+    find_most_of<256>(l, rows, most);
+    return;
+  }
+  for (int row = blockIdx.x; row < rows; row += step)
     for (int i = threadIdx.x; i < row_vecs; i += 256) to[row * to_pitch + i] = from[row * pitch + i];
 }
 
@@ -134,7 +147,8 @@ static Plan plan_z(const flux_loss_t* p, int cols) { return plan_tiles(LOGITS, p
 static Plan plan_dx(const flux_loss_t* p, int cols) { return plan_tiles(DX_KN, p->M, p->K, (cols + 7) / 8 * 8, 0, 0); }
 static Plan plan_dw(const flux_loss_t* p, int cols) { return plan_tiles(DW, cols, p->K, p->M, 0, 0); }
 
-// Columns of the backward pass's pieces, the last one's apart.
+// Columns of the backward pass's pieces, the last one's apart.  dZ of a piece takes 256 MiB, what the Infinity Cache holds: in smaller ones dX is added to the more
+// often, larger ones take memory and give nothing.  us of 8192x32000x8192 by columns a piece: 2048 10650, 4096 9530, 8192 9050, 16384 8960, 32768 8990.
 static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
 static int piece_of(const flux_loss_t* p) {
   const long long all = whole_lines(p->V);
@@ -224,9 +238,9 @@ static TileArgs logits_args(const flux_loss_t* p, const void* X, long long lx, c
 }
 
 // From here on X and its pitch are those of the copy.
-static int lay_out_x(const flux_loss_t* p, const void*& X, long long& lx, char* to, hipStream_t s) {
+static int lay_out_x(const flux_loss_t* p, const void*& X, long long& lx, char* to, const LossArgs& l, float* most, hipStream_t s) {
   const long long pitch = whole_lines(p->K);
-  FFN_HIP(start(whole_rows_kernel, dim3(std::min(p->M, 1 << 16)), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, (int)p->M, p->K / 8));
+  FFN_HIP(start(whole_rows_kernel, dim3(std::min(p->M, 1 << 16) + (most != nullptr)), s, static_cast<const uint4*>(X), reinterpret_cast<uint4*>(to), lx / 8, pitch / 8, (int)p->M, p->K / 8, l, most));
   X = to;
   lx = pitch;
   return FLUX_OK;
@@ -284,7 +298,7 @@ int flux_loss(const flux_loss_t* p, const void* X, const void* W, const void* ta
   a.loss.logit = logit;
   long long lx = pitch_x(p);
   if (stats_at != WS_HEADER) {
-    st = lay_out_x(p, X, lx, static_cast<char*>(workspace) + WS_HEADER, s);
+    st = lay_out_x(p, X, lx, static_cast<char*>(workspace) + WS_HEADER, a.loss, nullptr, s);
     if (st != FLUX_OK) return st;
   }
   TileArgs t = logits_args(p, X, lx, W, 0, p->V);
@@ -345,17 +359,17 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
   long long lx = pitch_x(p);
   const long long lw = pitch_w(p);
   const int piece = piece_of(p);
-  if (y.lays_out) {
-    st = lay_out_x(p, X, lx, ws + WS_HEADER + MOST_BYTES, s);
-    if (st != FLUX_OK) return st;
-  }
   float* const most = reinterpret_cast<float*>(ws + WS_HEADER);
   const float* const factor = p->dloss_one ? dloss : most;
   const auto finds = [&](const Plan& pl) { return !p->dloss_one && (pl.few || pl.tiles_m == 1); };
-  if (!p->dloss_one && !finds(y.z[0])) {
-    LossArgs l = loss_args(p, target);
-    l.dloss = dloss;
-    FFN_HIP(start_with(l.target_i64 ? most_kernel<long long> : most_kernel<int32_t>, dim3(1), 1024, s, l, (int)p->M, most));
+  const bool wants_most = !p->dloss_one && !finds(y.z[0]);
+  LossArgs of_rows = loss_args(p, target);
+  of_rows.dloss = dloss;
+  if (y.lays_out) {
+    st = lay_out_x(p, X, lx, ws + WS_HEADER + MOST_BYTES, of_rows, wants_most ? most : nullptr, s);
+    if (st != FLUX_OK) return st;
+  } else if (wants_most) {
+    FFN_HIP(start_with(most_kernel, dim3(1), 1024, s, of_rows, (int)p->M, most));
   }
   for (int v = 0; v < p->V; v += piece) {
     const int of = p->V - v <= piece, cols = std::min(piece, p->V - v), held = (cols + 7) / 8 * 8;

@@ -40,11 +40,13 @@ __device__ __forceinline__ float wave_max(float m) {
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(LOG2E * x); }
 
 // The row's target as a column of this product, -1 where it is none; counts: whether the row counts at all.
-__device__ __forceinline__ int target_column(const LossArgs& l, int row, int cols, bool& counts) {
-  const long long t = l.target_i64 ? static_cast<const long long*>(l.target)[row] : static_cast<const int32_t*>(l.target)[row];
-  counts = t >= 0 && t < l.vocab;
-  const long long c = t - l.v0;
+__device__ __forceinline__ int column_of(const LossArgs& l, long long target, int cols, bool& counts) {
+  counts = target >= 0 && target < l.vocab;
+  const long long c = target - l.v0;
   return counts && c >= 0 && c < cols ? (int)c : -1;
+}
+__device__ __forceinline__ int target_column(const LossArgs& l, int row, int cols, bool& counts) {
+  return column_of(l, l.target_i64 ? static_cast<const long long*>(l.target)[row] : static_cast<const int32_t*>(l.target)[row], cols, counts);
 }
 
 // (m, s) and (m2, s2) of two sets of logits as of one.  An infinite m leaves exp its argument as it is: no infinity is taken from another.
@@ -147,31 +149,36 @@ __device__ __forceinline__ void finish_dz16(const TileArgs& t, const LossArgs& l
 }
 
 // What the rows of a tile need beside their sums: a lane asks for one row's ahead of the main loop, all lanes read them out of LDS behind it.  (Asked for 16 rows at a time where
-// they are used, every 16 rows wait for memory: 7490x44009x64 214 us.)
+// they are used, every 16 rows wait for memory: 7490x44009x64 214 us.)  As they come, and a target in two halves: anything that was done with them
+// at once would wait for them before the first slab is asked for (2328x4096x1024 33.3 us, so 32.6).
 template <class C, bool GRADIENT>
 struct Logits {
   const TileArgs& t;
   const LossArgs& l;
-  int m0, target;
+  int m0;
+  uint32_t low, high;
   float lse, d;
   struct Row { int target; float lse, d; };
   const Row* rows;
   __device__ __forceinline__ void ask(const TileArgs&, int m0_) {
     m0 = m0_;
-    const int row = m0 + (int)threadIdx.x;
-    target = -1;
-    lse = d = 0.f;
-    if ((int)threadIdx.x >= C::BM || row >= t.rows) return;
-    bool counts;
-    target = target_column(l, row, t.cols, counts);
+    const int row = min(m0 + (int)threadIdx.x, t.rows - 1);
+    const uint32_t* const from = static_cast<const uint32_t*>(l.target) + ((long long)row << l.target_i64);
+    low = from[0];
+    high = from[l.target_i64];
     if constexpr (GRADIENT) {
       lse = l.lse[row];
-      d = row_dloss(l, row, counts);
+      d = l.dloss[l.dloss_one ? 0 : row];
     }
   }
   __device__ __forceinline__ void keep(unsigned char* pool) {
     static_assert(C::POOL_BYTES >= 1024 + C::BM * (int)sizeof(Row) && C::BM <= C::NT, "rows of a tile");
     Row* const to = reinterpret_cast<Row*>(pool + 1024);          // (the first word is finish_cut's)
+    const long long is = l.target_i64 ? (long long)((uint64_t)high << 32 | low) : (int32_t)low;
+    bool counts = false;
+    int target = -1;
+    if ((int)threadIdx.x < C::BM && m0 + (int)threadIdx.x < t.rows) target = column_of(l, is, t.cols, counts);
+    if constexpr (GRADIENT) d = counts ? d : 0.f;
     __syncthreads();                                              // all waves are done with the ring
     if constexpr (GRADIENT) {
       float most = 1.f;
