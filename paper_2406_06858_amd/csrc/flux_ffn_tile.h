@@ -532,10 +532,18 @@ __device__ __forceinline__ void finish_rows16(const TileArgs& t, int job, f32x4 
   constexpr bool ADDEND = SCALED && C::KIND == DX_KN;
   if constexpr (SCALED) {
     const float by = *t.factor;
+    // (no number, as the mean over no row has it: what no row added to stays 0)
+    if (__builtin_fabsf(by) < __builtin_inff()) {
 #pragma unroll
-    for (int n = 0; n < C::NI; ++n)
+      for (int n = 0; n < C::NI; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[n][e] *= by;
+        for (int e = 0; e < 4; ++e) acc[n][e] *= by;
+    } else {
+#pragma unroll
+      for (int n = 0; n < C::NI; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] = acc[n][e] == 0.f ? 0.f : acc[n][e] * by;
+    }
   }
   const int g = lane >> 4, row = row0 + (lane & 15), in_bf16 = (g & 1) * 32 + (g >> 1) * 16;
   const auto bf16 = [&](void* out, int col, const u32x4 (&p)[C::NIH / 2]) {

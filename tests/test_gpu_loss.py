@@ -274,6 +274,19 @@ def test_rows_that_do_not_count_hide_what_they_hold():
         assert torch.equal(a[rows], b[rows])
 
 
+@pytest.mark.parametrize("M,V,K", [(5, 77, 136), (70, 300, 264), (300, 520, 512), (31, 4100, 2056)])
+@pytest.mark.parametrize("dloss", [float("inf"), float("nan")])
+def test_a_mean_over_no_row_has_no_gradient(M, V, K, dloss):
+    c = Case(M, V, K, 41)
+    target = torch.full((M,), -100, device=DEV)
+    for accumulate in (0, 1):
+        p = c.problem(dloss_one=1, dw_dtype="f32", dw_accumulate=accumulate)
+        dX, dW = torch.full_like(c.X, 5.0), torch.full((V, K), 3.0, device=DEV)
+        loss.flux_loss_backward(p, c.X, c.W, target, torch.full((M,), float("nan"), device=DEV), torch.tensor([dloss], device=DEV), dX, dW,
+                                workspace(loss.FLUX_LOSS_BACKWARD, p))
+        assert (dX == 0).all() and (dW == 3.0 * accumulate).all()
+
+
 @pytest.mark.parametrize("M", [5, 70])
 def test_logits_beyond_all_measure(M):
     """Rows of equal logits of 2^100: what is left of the difference to the largest is nothing, not its rounding."""
