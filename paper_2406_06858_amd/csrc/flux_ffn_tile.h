@@ -153,7 +153,9 @@ struct OperandLoader {
     lds_wave = (uint32_t)(wave_row(wave) * (1024 / RPI));
     if constexpr (T) {
       const int k = wave_row(wave) + lane / SLOTS, s = lane % SLOTS ^ flux::swz_b<SLOTS>(wave_row(wave) + lane / SLOTS);
-      voff = EDGE && r0 + s * 8 >= rows ? OUTSIDE : (uint32_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
+      // (of fewer rows than the tile takes, with gaps of 100 MB and more, a row past the last one may be past 32 bits too)
+      const uint64_t at = (uint64_t)k * pitch + (uint32_t)(r0 + s * 8) * 2u;
+      voff = EDGE && (r0 + s * 8 >= rows || at > OUTSIDE) ? OUTSIDE : (uint32_t)at;
     } else {
       const int row = 8 * wave + lane / 8, s = phase ? phase->piece(lane % 8, row) : lane % 8 ^ swizzle<MX>(row);
       voff = (uint32_t)(r0 + row) * pitch + (uint32_t)s * 16u;

@@ -361,6 +361,36 @@ def test_rows_that_are_no_whole_lines():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("M,V,ldx,ldw", [(40, 8, 0, 150_000_000), (14, 96, 150_000_000, 0), (40, 31, 0, 71_000_000), (31, 30, 71_000_000, 71_000_000), (3, 3, 0, 1_000_000_000)])
+def test_pitches_whose_offsets_take_all_32_bits(M, V, ldx, ldw):
+    """The bits of rows side by side; what lies between the rows is no number."""
+    K = 136
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    X, W = (torch.randn(n, K, generator=gen, device=DEV).to(torch.bfloat16) for n in (M, V))
+    target, dloss = torch.arange(M, device=DEV) % (V + 1), torch.randn(M, generator=gen, device=DEV)
+    got = []
+    for lx, lw in ((0, 0), (ldx, ldw)):
+        views = []
+        for t, ld in ((X, lx), (W, lw), (X, lx), (W, lw)):
+            n = t.shape[0]
+            buf = torch.full(((n - 1) * (ld or K) + K,), float("nan"), dtype=torch.bfloat16, device=DEV)
+            views.append(buf.as_strided((n, K), (ld or K, 1)))
+        x, w, dX, dW = views
+        x.copy_(X)
+        w.copy_(W)
+        p = loss.loss_problem(M, V, K, ldx=lx, ldw=lw)
+        out = [torch.empty(M, device=DEV) for _ in range(3)]
+        loss.flux_loss(p, x, w, target, *out, workspace(loss.FLUX_LOSS_FORWARD, p))
+        loss.flux_loss_backward(p, x, w, target, out[0], dloss, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+        torch.cuda.synchronize()
+        got.append([*out, dX.contiguous(), dW.contiguous()])
+        del x, w, dX, dW, views, buf
+        torch.cuda.empty_cache()
+    assert torch.isfinite(got[0][4]).all()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("M,config", [(1, 6), (40, 5), (64, 6), (65, 3), (100, 4)])
 def test_weights_that_are_read_past_the_caches(M, config):
     """Large matrices in whole lines are, others are not: the same bits."""

@@ -291,6 +291,31 @@ def test_backward_without_a_stream_and_added_up(M, K, dw):
     assert_within(dW, want, dw_off + (np.abs(want) + dw_off) * (half(dw) + U))
 
 
+@pytest.mark.parametrize("M,K,ld", [(15, 1029, 150_000_001), (3, 40000, 1_073_000_000)])
+def test_pitches_whose_offsets_pass_32_bits(M, K, ld):
+    """The bits of rows side by side."""
+    X, S, W = case(M, K, 5, s="f32")
+    dY = torch.randn(M, K, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    got = []
+    for pitch in (K, ld):
+        views = []
+        for t in (X, S, dY, S, X, X, S):                                          # X, R, dY; S, Y, dX, dR
+            buf = torch.full(((M - 1) * pitch + K,), float("nan"), dtype=t.dtype, device=DEV)
+            views.append(buf.as_strided((M, K), (pitch, 1)))
+            views[-1].copy_(t)
+        p = norm.norm_problem(M, K, s_dtype="f32", ldx=pitch, lds=pitch, ldy=pitch)
+        rstd, dW = torch.empty(M, device=DEV), torch.empty(K, device=DEV)
+        norm.flux_norm(p, views[0], views[1], W, views[3], views[4], None, rstd)
+        ws = torch.zeros(norm.flux_norm_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+        norm.flux_norm_backward(p, views[2], views[3], W, rstd, None, views[6], views[5], dW, ws)
+        torch.cuda.synchronize()
+        got.append([rstd, dW] + [v.contiguous() for v in views[3:]])
+        del views, buf
+        torch.cuda.empty_cache()
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 @pytest.mark.parametrize("K", [1, 3])
 def test_more_rows_than_a_grid_is_wide(K):
     M = (1 << 27) + 33 if K == 1 else (1 << 24) + 5
