@@ -144,7 +144,9 @@ static int validate(int op, const flux_loss_t* p) {
 
 // ---- plans -----------------------------------------------------------------------------------------------------
 static Plan plan_z(const flux_loss_t* p, int cols) { return plan_tiles(LOGITS, p->M, cols, p->K, p->tile_config, p->split_k); }
-static Plan plan_dx(const flux_loss_t* p, int cols) { return plan_tiles(DX_KN, p->M, p->K, (cols + 7) / 8 * 8, 0, 0); }
+// (dX runs over the weights' rows, cols of them, though dZ is in whole vectors of 8: of 57 to 63 the masked kernel has to be the one, since the other would read up to seven
+// rows more than there are, for dZ's zeros)
+static Plan plan_dx(const flux_loss_t* p, int cols) { return plan_tiles(DX_KN, p->M, p->K, cols, 0, 0); }
 static Plan plan_dw(const flux_loss_t* p, int cols) { return plan_tiles(DW, cols, p->K, p->M, 0, 0); }
 
 // Columns of the backward pass's pieces, the last one's apart.  dZ of a piece takes 256 MiB, what the Infinity Cache holds: in smaller ones dX is added to the more
@@ -400,7 +402,7 @@ int flux_loss_backward(const flux_loss_t* p, const void* X, const void* W, const
       t.bytes_b = extent(cols, lw * 2, p->K * 2ll);
       t.rows = p->M;
       t.cols = p->K;
-      t.depth = held;
+      t.depth = cols;
       t.ld = pitch_x(p);
       // sums of pieces stay in fp32: in dX, or in the workspace until the last piece rounds them
       t.out_f32 = f32 || !last;
