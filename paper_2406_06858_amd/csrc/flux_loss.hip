@@ -165,9 +165,9 @@ static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // Whether X is laid out anew: a slab's loads, 128 bytes a row, are two lines each where rows are no whole lines, and every column tile reads X.  us, X as it is / laid
 // out anew by the caller: statistics of 1496x50257x5112 (256x256 tiles) 729 / 678, 8192x4000x5112 252 / 244, 2328x4096x7640 (256x128) 175 / 135, 512x8000x5112
 // (128x128) 58.6 / 49.2; gradients of 1496x6283x5112 279 / 262: 5 to 7 % of the products that read X on the largest tiles, 12 to 23 % on the others, which read X
-// for fewer columns each.  Against that, a launch and a pass of 4.5 TB/s.
+// for fewer columns each.  Against that, a launch and a pass of 4.5 TB/s.  The copy's rows are longer than X's: it is a matrix below 2^31 elements too, or is not made.
 static bool lays_out_x(int op, const flux_loss_t* p, const Plan& z) {
-  if (pitch_x(p) % 64 == 0 || z.few) return false;
+  if (pitch_x(p) % 64 == 0 || z.few || !below_limit(p->M, whole_lines(p->K), p->K)) return false;
   const double gflop = 2e-9 * p->M * p->V * p->K, gain_us = z.shape == 0 ? 0.046 * gflop : 0.15 * gflop;
   return gain_us * (op == FLUX_LOSS_BACKWARD ? 2 : 1) > 2.0 + 4.0 * p->M * p->K / 4.5e6;
 }

@@ -51,3 +51,45 @@ def test_what_lies_behind_the_matrices(M, V, K, piece, dx):
     z = X.double() @ W.double().t()
     dz = (torch.exp(z - lse.double()[:, None]) - torch.nn.functional.one_hot(target, V)) * dloss.double()[:, None]
     assert ((got[1][0].double() - dz @ W.double()).abs() <= 2.5 * 2.0 ** -8 * (dz.abs() @ W.double().abs())).all()
+
+
+def test_rows_that_are_no_whole_lines_of_a_matrix_near_the_limit():
+    """X below 2^31 elements as it is, above with its rows rounded up to whole lines.  Rows from the front, the middle and the end, against 64 bits; all others do not
+    count, and their gradient is zeros."""
+    M, V, K, U = 2_120_000, 16384, 1000, 2.0 ** -24
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    X = torch.empty(M, K, dtype=torch.bfloat16, device=DEV)
+    for part in X.split(1 << 18):
+        part.copy_(torch.randn(part.shape, generator=gen, device=DEV))
+    W = (torch.randn(V, K, generator=gen, device=DEV) * 2 / K ** 0.5).to(torch.bfloat16)
+    rows = torch.cat([torch.arange(at, at + 100, device=DEV) for at in (0, 1 << 20, 2_097_100, M - 100)])          # (2_097_152: where a copy's offsets would wrap)
+    target = torch.full((M,), -100, device=DEV)
+    target[rows] = torch.randint(0, V, (len(rows),), generator=gen, device=DEV)
+    dloss = torch.randn(M, generator=gen, device=DEV)
+    p = loss.loss_problem(M, V, K)
+    lse, logit, value = (torch.empty(M, device=DEV) for _ in range(3))
+    ws = workspace(loss.FLUX_LOSS_FORWARD, p)
+    loss.flux_loss(p, X, W, target, lse, logit, value, ws)
+    torch.cuda.synchronize()
+    x, w, t = X[rows].double(), W.double(), target[rows]
+    z = x @ w.t()
+    want = torch.logsumexp(z, 1)
+    # (as in test_gpu_loss: what a logit is off by, the sums, exp's argument, the logarithm)
+    z_off = (x.abs() @ w.abs().t()).amax(1) * (K / 16 + 16) * 2 * U
+    off = z_off + ((torch.exp(z - want[:, None]) * (z.amax(1, keepdim=True) - z + 2)).sum(1) * 2 + V / 256 + 64 + (want.abs() + 8) * 4) * U
+    z_t = z.gather(1, t[:, None])[:, 0]
+    assert ((lse[rows].double() - want).abs() <= off).all()
+    assert ((logit[rows].double() - z_t).abs() <= z_off).all()
+    assert ((value[rows].double() - (want - z_t)).abs() <= off + z_off + (want - z_t).abs() * U).all()
+    others = torch.ones(M, dtype=torch.bool, device=DEV)
+    others[rows] = False
+    assert not value[others].any() and bool(lse.isfinite().all())
+    del ws
+    dX, dW = torch.full_like(X, 7.0), torch.empty_like(W)
+    loss.flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+    torch.cuda.synchronize()
+    dz = (torch.exp(z - lse[rows].double()[:, None]) - torch.nn.functional.one_hot(t, V)) * dloss[rows].double()[:, None]
+    # (dZ's and the results' roundings, 2^-8 each; zeros add nothing to a sum's error)
+    assert ((dX[rows].double() - dz @ w).abs() <= 2.5 * 2.0 ** -8 * (dz.abs() @ w.abs())).all()
+    assert ((dW.double() - dz.t() @ x).abs() <= 2.5 * 2.0 ** -8 * (dz.abs().t() @ x.abs())).all()
+    assert not (dX.view(torch.int16) != 0)[others].any()

@@ -3,6 +3,8 @@ tiles reads are worked out from the arguments, in whole numbers of any size."""
 import pytest
 from launch_recorder import record
 
+from paper_2406_06858_amd import loss
+
 ALONG, DX, DW = 2, 3, 4                        # kinds of tile kernels: both operands along the contraction; the second across; both across
 BACKWARD = range(7)                            # X, W, target, lse, dloss, dX, dW
 
@@ -36,3 +38,42 @@ def test_gradients_read_no_row_past_the_weights(tmp_path, M, K):
         assert dx
         masks.update(t["masked"] for t in dx)
     assert masks == {0, 1}
+
+
+def _whole_vectors(n):
+    return (n + 7) // 8 * 8
+
+
+def _extents(t):
+    """Bytes that A and B span, as the buffers' records have to say it (whole numbers of any size)."""
+    across = lambda n, pitch: (t["depth"] - 1) * pitch + n * 2         # noqa: E731
+    along = lambda n, pitch, row: (n - 1) * pitch + row * 2            # noqa: E731
+    rows, cols, depth = t["rows"], t["cols"], t["depth"]
+    if t["kind"] == DW:
+        return across(_whole_vectors(rows), t["pitch_a"]), across(cols, t["pitch_b"])
+    row = depth if t["kind"] == ALONG else _whole_vectors(depth)
+    return along(rows, t["pitch_a"], row), along(cols, t["pitch_b"], depth) if t["kind"] == ALONG else across(cols, t["pitch_b"])
+
+
+# X below 2^31 elements as it is, and not with its rows rounded up to whole lines; on either side of the border; with a pitch of its own; far from it
+WIDE = [dict(M=420000, V=50257, K=5112), dict(M=2120000, V=32000, K=1000), dict(M=419430, V=50257, K=5112), dict(M=419431, V=50257, K=5112),
+        dict(M=420000, V=50257, K=5040, ldx=5112), dict(M=8192, V=50257, K=5112)]
+
+
+@pytest.mark.parametrize("function,pointers", [("flux_loss", range(6)), ("flux_loss_backward", BACKWARD)])
+def test_buffers_span_what_their_32_bits_say(tmp_path, function, pointers):
+    calls = record(tmp_path, [(function, p, pointers) for p in WIDE])
+    for call, p in zip(calls, WIDE):
+        tiles = _check(call, p)
+        assert tiles
+        for t in tiles:
+            assert (t["bytes_a"], t["bytes_b"]) == _extents(t) and max(_extents(t)) < 1 << 32, (p, t["name"], t["bytes_a"], t["bytes_b"], _extents(t))
+
+
+def test_a_copy_is_made_where_its_offsets_fit():
+    """The forward pass's workspace has room for X in whole lines, or has not.  (Everything else in it is smaller.)"""
+    fit = [(p["M"] - 1) * ((p["K"] + 63) // 64 * 64) + p["K"] < 1 << 31 for p in WIDE]
+    assert fit == [False, False, True, False, True, True]
+    for p, fits in zip(WIDE, fit):
+        need = loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_FORWARD, loss.loss_problem(**p))
+        assert (need >= 2 * p["M"] * ((p["K"] + 63) // 64 * 64)) == fits, p
