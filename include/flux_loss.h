@@ -23,7 +23,7 @@ extern "C" {
 typedef enum { FLUX_LOSS_FORWARD = 0, FLUX_LOSS_BACKWARD = 1 } flux_loss_op_t;
 typedef enum { FLUX_TARGET_I32 = 0, FLUX_TARGET_I64 = 1 } flux_target_t;
 
-/* M, V >= 1; M <= 2^27, M V <= 2^36; K % 8 == 0; pitches multiples of 8, at least a row long; X, W, dX and dW 16-byte aligned; every matrix below 2^31
+/* M, V >= 1; M <= 2^27, M V <= 2^36; K % 8 == 0, K <= 2^28 for gradients; pitches multiples of 8, at least a row long; X, W, dX and dW 16-byte aligned; every matrix below 2^31
  * elements.
  * A row whose target is not in [0, vocab) does not count: its loss is 0 and it adds nothing to a gradient, whatever its lse and dloss are (but X has to be finite: dW is a
  * sum over all rows, and 0 times infinity is none).  So is a row whose dloss is 0.  A target of another rank's columns gives a logit of 0 here. */

@@ -128,6 +128,7 @@ static long long pitch_w(const flux_loss_t* p) { return p->ldw ? p->ldw : p->K; 
 static long long vocab_of(const flux_loss_t* p) { return p->vocab ? p->vocab : p->v0 + p->V; }
 constexpr long long MAX_VOCAB = 1ll << 62, MAX_LOGITS = 1ll << 36;          // (at most 2^23 workgroups of the smallest tile)
 constexpr int MAX_ROWS = 1 << 27;
+constexpr int MAX_WIDTH = 1 << 28;          // of gradients: a result's place in its row is counted in bytes, in 32 bits (store_pair)
 
 static int validate(int op, const flux_loss_t* p) {
   if (p == nullptr || (op != FLUX_LOSS_FORWARD && op != FLUX_LOSS_BACKWARD)) return FLUX_ERR_INVALID_ARG;
@@ -137,6 +138,7 @@ static int validate(int op, const flux_loss_t* p) {
   if (p->M < 1 || p->V < 1 || p->K < 1 || p->K % 8 != 0 || p->piece % 64 != 0) return FLUX_ERR_SHAPE;
   if (p->v0 > MAX_VOCAB || p->vocab > MAX_VOCAB || vocab_of(p) < p->v0 + p->V) return FLUX_ERR_SHAPE;
   if (!pitch_ok(pitch_x(p), p->M, p->K) || !pitch_ok(pitch_w(p), p->V, p->K)) return FLUX_ERR_SHAPE;
+  if (op == FLUX_LOSS_BACKWARD && p->K > MAX_WIDTH) return FLUX_ERR_SHAPE;
   if (p->M > MAX_ROWS || (long long)p->M * p->V > MAX_LOGITS) return FLUX_ERR_SHAPE;
   if (p->tile_config == FEW_CONFIG && !few_fits(LOGITS, p->M, p->V)) return FLUX_ERR_UNSUPPORTED;
   return FLUX_OK;

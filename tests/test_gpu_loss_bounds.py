@@ -93,3 +93,37 @@ def test_rows_that_are_no_whole_lines_of_a_matrix_near_the_limit():
     assert ((dX[rows].double() - dz @ w).abs() <= 2.5 * 2.0 ** -8 * (dz.abs() @ w.abs())).all()
     assert ((dW.double() - dz.t() @ x).abs() <= 2.5 * 2.0 ** -8 * (dz.abs().t() @ x.abs())).all()
     assert not (dX.view(torch.int16) != 0)[others].any()
+
+
+@pytest.mark.parametrize("M,V,dtype", [(1, 2, "f32"), (3, 3, "bf16")])
+def test_the_widest_rows(M, V, dtype):
+    """2^28 numbers; X is zeros but for a thousand columns, the first and the last among them, so that the logits are sums of few numbers."""
+    K, U = 1 << 28, 2.0 ** -24
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    at = torch.randint(0, K, (1000,), generator=gen, device=DEV).unique()
+    at[0], at[-1] = 0, K - 1
+    X = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    X[:, at] = torch.randn(M, len(at), generator=gen, device=DEV).to(torch.bfloat16)
+    W = torch.empty(V, K, dtype=torch.bfloat16, device=DEV)
+    for row in W:
+        row.copy_(torch.randn(K, generator=gen, device=DEV) * 0.03)
+    target, dloss = torch.arange(M, device=DEV) % V, torch.randn(M, generator=gen, device=DEV)
+    p = loss.loss_problem(M, V, K, dx_dtype=dtype, dw_dtype=dtype)
+    lse, logit, value = (torch.empty(M, device=DEV) for _ in range(3))
+    loss.flux_loss(p, X, W, target, lse, logit, value, workspace(loss.FLUX_LOSS_FORWARD, p))
+    x, w = X[:, at].double(), W[:, at].double()
+    z = x @ w.t()
+    z_off = (x.abs() @ w.abs().t()).amax(1) * (len(at) + 16) * 2 * U          # (each of them in a sum of its own, at worst)
+    want = torch.logsumexp(z, 1)
+    assert ((lse.double() - want).abs() <= z_off + 100 * U).all() and ((logit.double() - z.gather(1, target[:, None])[:, 0]).abs() <= z_off).all()
+    t = (torch.bfloat16, torch.float32)[p.dx_dtype]
+    dX, dW = torch.full((M, K), 7.0, dtype=t, device=DEV), torch.full((V, K), 7.0, dtype=t, device=DEV)
+    loss.flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace(loss.FLUX_LOSS_BACKWARD, p))
+    torch.cuda.synchronize()
+    dz = (torch.exp(z - lse.double()[:, None]) - torch.nn.functional.one_hot(target, V)) * dloss.double()[:, None]
+    # (dZ's rounding to bf16 and the result's, 2^-8 each of the sum of magnitudes; piece by piece, for memory)
+    for a in range(0, K, 1 << 25):
+        part = W[:, a:a + (1 << 25)].double()
+        assert ((dX[:, a:a + (1 << 25)].double() - dz @ part).abs() <= 2.5 * 2.0 ** -8 * (dz.abs() @ part.abs())).all()
+        part = X[:, a:a + (1 << 25)].double()
+        assert ((dW[:, a:a + (1 << 25)].double() - dz.t() @ part).abs() <= 2.5 * 2.0 ** -8 * (dz.abs().t() @ part.abs())).all()

@@ -3,6 +3,7 @@ tiles reads are worked out from the arguments, in whole numbers of any size."""
 import pytest
 from launch_recorder import record
 
+from paper_2406_06858_amd import binding as fb
 from paper_2406_06858_amd import loss
 
 ALONG, DX, DW = 2, 3, 4                        # kinds of tile kernels: both operands along the contraction; the second across; both across
@@ -77,3 +78,17 @@ def test_a_copy_is_made_where_its_offsets_fit():
     for p, fits in zip(WIDE, fit):
         need = loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_FORWARD, loss.loss_problem(**p))
         assert (need >= 2 * p["M"] * ((p["K"] + 63) // 64 * 64)) == fits, p
+
+
+def test_results_have_their_places_in_32_bits(tmp_path):
+    """A result's place in its row is counted in bytes, a tile's past the last column too.  Wider rows are refused."""
+    problems = [dict(M=M, V=V, K=K, dx_dtype=dtype, dw_dtype=dtype) for K in (1 << 28, (1 << 28) + 8, 1 << 29, (1 << 29) + 4096, 3 << 28, 1 << 30, (1 << 31) - 8)
+                for M, V in ((1, 1), (3, 7), (2, 2)) if max(M, V) * K < 1 << 31 for dtype in ("bf16", "f32")]
+    calls = record(tmp_path, [("flux_loss_backward", p, BACKWARD) for p in problems])
+    for call, p in zip(calls, problems):
+        if p["K"] > 1 << 28:
+            assert call["status"] == fb.FLUX_ERR_SHAPE and not call["launches"], p
+            assert loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_BACKWARD, loss.loss_problem(**p)) == 0
+            continue
+        for t in _check(call, p):
+            assert t["tiles_n"] * t["bn"] * 4 < 1 << 31, (p, t["name"])
