@@ -1,6 +1,6 @@
 """ctypes binding of include/flux_loss.h (in libflux_ffn_mi355.so): the softmax cross entropy of a vocabulary projection, its join over ranks and its
-backward pass.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, or of another device than the current
-one, raises ValueError.
+backward pass.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, of another device than the current
+one, or whose numbers do not lie where the problem says, raises ValueError.
 """
 from __future__ import annotations
 
@@ -9,9 +9,9 @@ import ctypes as C
 import torch
 
 from . import ffn
-from .binding import _ptr_list
+from .binding import _ptr, _ptr_list
 from .ffn import _check, _stream
-from .norm import _DT, _F32, _TYPES, _buf, _device, _fit, _space
+from .norm import _DT, _F32, _TYPES, _device, _fit, _space
 
 FLUX_LOSS_FORWARD, FLUX_LOSS_BACKWARD = 0, 1
 FLUX_TARGET_I32, FLUX_TARGET_I64 = 0, 1
@@ -62,11 +62,13 @@ def flux_loss_workspace_bytes(op: int, p: flux_loss_t) -> int:
 
 
 def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=None):
-    d, t = _device(), _TARGETS[p.target_dtype & 1]
+    d, t, M, K = _device(), _TARGETS[p.target_dtype & 1], p.M, p.K
     if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and logit.dtype is _F32
             and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == logit.get_device()
-            and (loss is None or (loss.dtype is _F32 and loss.get_device() == d))):
-        _fit(d, X=(X, _BF16), W=(W, _BF16), target=(target, t), lse=(lse, _F32), logit=(logit, _F32), loss=(loss, _F32))
+            and X.numel() == M * K and W.numel() == p.V * K and target.numel() >= M and lse.numel() >= M and logit.numel() >= M and not (p.ldx or p.ldw)
+            and X.is_contiguous() and W.is_contiguous() and target.is_contiguous() and lse.is_contiguous() and logit.is_contiguous()
+            and (loss is None or (loss.dtype is _F32 and loss.get_device() == d and loss.numel() >= M and loss.is_contiguous()))):
+        _fit(d, X=(X, _BF16, M, K, p.ldx), W=(W, _BF16, p.V, K, p.ldw), target=(target, t, M), lse=(lse, _F32, M), logit=(logit, _F32, M), loss=(loss, _F32, M))
     status = lib().flux_loss(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), logit.data_ptr(), 0 if loss is None else loss.data_ptr(),
                              *_space(workspace, d), _stream(stream))
     if status:
@@ -74,21 +76,26 @@ def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=Non
 
 
 def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, stream=None):
-    d, f = _device(), torch.float32
+    d, M = _device(), p.M
     if len(lses) != len(logits):
         raise ValueError("as many lses as logits")
-    for t in (*lses, *logits):
-        _buf(t, f, d, "lses and logits")
-    _check(lib().flux_loss_join(p, len(lses), _ptr_list(lses), _ptr_list(logits), _buf(target, _TARGETS[p.target_dtype & 1], d, "target"),
-                                _buf(lse, f, d, "lse"), _buf(logit, f, d, "logit"), _buf(loss, f, d, "loss"), _stream(stream)), "flux_loss_join")
+    for r, (a, b) in enumerate(zip(lses, logits)):
+        _fit(d, **{f"lses[{r}]": (a, _F32, M), f"logits[{r}]": (b, _F32, M)})
+    _fit(d, target=(target, _TARGETS[p.target_dtype & 1], M), lse=(lse, _F32, M), logit=(logit, _F32, M), loss=(loss, _F32, M))
+    _check(lib().flux_loss_join(p, len(lses), _ptr_list(lses), _ptr_list(logits), *map(_ptr, (target, lse, logit, loss)), _stream(stream)), "flux_loss_join")
 
 
 def flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace, stream=None):
-    d, t, x, w = _device(), _TARGETS[p.target_dtype & 1], _TYPES[p.dx_dtype & 1], _TYPES[p.dw_dtype & 1]
+    d, t, x, w, M, K = _device(), _TARGETS[p.target_dtype & 1], _TYPES[p.dx_dtype & 1], _TYPES[p.dw_dtype & 1], p.M, p.K
+    n, m, rows = M * K, p.V * K, 1 if p.dloss_one else M
     if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and dloss.dtype is _F32
             and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == dloss.get_device()
-            and (dX is None or (dX.dtype is x and dX.get_device() == d)) and (dW is None or (dW.dtype is w and dW.get_device() == d))):
-        _fit(d, X=(X, _BF16), W=(W, _BF16), target=(target, t), lse=(lse, _F32), dloss=(dloss, _F32), dX=(dX, x), dW=(dW, w))
+            and X.numel() == n and W.numel() == m and target.numel() >= M and lse.numel() >= M and dloss.numel() >= rows and not (p.ldx or p.ldw)
+            and X.is_contiguous() and W.is_contiguous() and target.is_contiguous() and lse.is_contiguous() and dloss.is_contiguous()
+            and (dX is None or (dX.dtype is x and dX.get_device() == d and dX.numel() == n and dX.is_contiguous()))
+            and (dW is None or (dW.dtype is w and dW.get_device() == d and dW.numel() == m and dW.is_contiguous()))):
+        _fit(d, X=(X, _BF16, M, K, p.ldx), W=(W, _BF16, p.V, K, p.ldw), target=(target, t, M), lse=(lse, _F32, M), dloss=(dloss, _F32, rows),
+             dX=(dX, x, M, K, p.ldx), dW=(dW, w, p.V, K, p.ldw))
     status = lib().flux_loss_backward(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), 0 if dX is None else dX.data_ptr(),
                                       0 if dW is None else dW.data_ptr(), *_space(workspace, d), _stream(stream))
     if status:

@@ -1,6 +1,6 @@
 """ctypes binding of include/flux_norm.h (in libflux_ffn_mi355.so): the root-mean-square norm with the residual's addition, its backward pass,
-and 8-bit blocks read back.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, or of another device than the
-current one, raises ValueError.
+and 8-bit blocks read back.  Argument marshalling only, as in `ffn`; a tensor of another type than the problem's, of another device than the
+current one, or whose numbers do not lie where the problem says, raises ValueError.
 """
 from __future__ import annotations
 
@@ -61,9 +61,29 @@ def _buf(t, dtype, device, what):
     return t.data_ptr()
 
 
+def _lies(t, what, rows, cols=None, pitch=0):
+    """Raises if t has not `rows` numbers side by side; with `cols`, rows of so many, `pitch` apart (0: side by side).  A matrix may be of any shape if it is side by side as
+    a whole; rows behind the last one are nobody's business."""
+    if cols is None:
+        ok, wanted = t.is_contiguous() and t.numel() >= rows, f"{rows} numbers side by side"
+    else:
+        pitch = pitch or cols
+        if t.dim() != 2 and t.is_contiguous():
+            t = t.view(-1, t.shape[-1]) if t.dim() > 2 else t.view(-1)
+        if t.dim() == 1:
+            ok = t.numel() >= (rows - 1) * pitch + cols
+        else:
+            ok = t.dim() == 2 and t.shape[0] >= rows and t.shape[1] >= cols and (cols == 1 or t.stride(1) == 1) and (rows == 1 or t.stride(0) == pitch)
+        wanted = f"{rows} rows of {cols} numbers, {pitch} apart"
+    if not ok:
+        raise ValueError(f"{what} has to be {wanted}, not {tuple(t.shape)} with strides {t.stride()}")
+
+
 def _space(workspace, device):
-    if workspace is not None and workspace.get_device() != device:
-        raise ValueError(f"the workspace has to be on device {device}, not on {workspace.device}")
+    if workspace is None:
+        return 0, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"the workspace has to be in one piece on device {device}, not {tuple(workspace.shape)} with strides {workspace.stride()} on {workspace.device}")
     return _ws(workspace)
 
 
@@ -76,19 +96,35 @@ def flux_norm_workspace_bytes(p: flux_norm_t) -> int:
     return int(lib().flux_norm_workspace_bytes(C.byref(p)))
 
 
+def _in_blocks(M, K, out):
+    """Bytes of M rows of K numbers in blocks, and of their scales."""
+    blocks = (K + 31) // 32
+    return M * blocks * (16 if out == FLUX_NORM_MX4 else 32), M * ((blocks + 15) // 16 * 16)
+
+
 def _fit(device, **tensors):
-    """Raises for the first (tensor or None, dtype) that does not fit.  (The calls look at all tensors at once and come here if one is not as it should be: as long as a launch
-    is a microsecond or two, so is a function call a tensor.)"""
-    for what, (t, dtype) in tensors.items():
+    """Raises for the first (tensor or None, dtype, where its numbers lie: see _lies) that does not fit.  (The calls look at all tensors at once and come here if one is not as
+    it usually is: as long as a launch is a microsecond or two, so is a function call a tensor.)"""
+    for what, (t, dtype, *place) in tensors.items():
         _buf(t, dtype, device, what)
+        if t is not None:
+            _lies(t, what, *place)
 
 
 def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
     d, x, s, w, y = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1], _TYPES[p.w_dtype & 1], _TYPES[p.out & 3]
+    M, K = p.M, p.K
+    held = n = M * K
+    if y is _U8:
+        held, scaled = _in_blocks(M, K, p.out)
     if not (X.dtype is x and W.dtype is w and Y.dtype is y and d == X.get_device() == W.get_device() == Y.get_device()
-            and (R is None or (R.dtype is s and R.get_device() == d)) and (S is None or (S.dtype is s and S.get_device() == d))
-            and (scales is None or (scales.dtype is _U8 and scales.get_device() == d)) and (rstd is None or (rstd.dtype is _F32 and rstd.get_device() == d))):
-        _fit(d, X=(X, x), R=(R, s), W=(W, w), S=(S, s), Y=(Y, y), scales=(scales, _U8), rstd=(rstd, _F32))
+            and X.numel() == n and Y.numel() == held and W.numel() == K and X.is_contiguous() and Y.is_contiguous() and W.is_contiguous() and not (p.ldx or p.lds or p.ldy)
+            and (R is None or (R.dtype is s and R.get_device() == d and R.numel() == n and R.is_contiguous()))
+            and (S is None or (S.dtype is s and S.get_device() == d and S.numel() == n and S.is_contiguous()))
+            and (scales is None or (y is _U8 and scales.dtype is _U8 and scales.get_device() == d and scales.numel() == scaled and scales.is_contiguous()))
+            and (rstd is None or (rstd.dtype is _F32 and rstd.get_device() == d and rstd.numel() >= M and rstd.is_contiguous()))):
+        _fit(d, X=(X, x, M, K, p.ldx), R=(R, s, M, K, p.lds), W=(W, w, K), S=(S, s, M, K, p.lds), Y=(Y, y, held) if y is _U8 else (Y, y, M, K, p.ldy),
+             scales=(scales, _U8, scaled if y is _U8 else 0), rstd=(rstd, _F32, M))
     status = lib().flux_norm(p, X.data_ptr(), 0 if R is None else R.data_ptr(), W.data_ptr(), 0 if S is None else S.data_ptr(), Y.data_ptr(),
                              0 if scales is None else scales.data_ptr(), 0 if rstd is None else rstd.data_ptr(), _stream(stream))
     if status:
@@ -97,10 +133,17 @@ def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
 
 def flux_norm_backward(p, dY, S, W, rstd, dS=None, dR=None, dX=None, dW=None, workspace=None, stream=None):
     d, x, s, w, y, dw = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1], _TYPES[p.w_dtype & 1], _TYPES[p.out & 1], _TYPES[p.dw_dtype & 1]
+    M, K = p.M, p.K
+    n = M * K
     if not (dY.dtype is y and S.dtype is s and W.dtype is w and rstd.dtype is _F32 and d == dY.get_device() == S.get_device() == W.get_device() == rstd.get_device()
-            and (dS is None or (dS.dtype is s and dS.get_device() == d)) and (dR is None or (dR.dtype is s and dR.get_device() == d))
-            and (dX is None or (dX.dtype is x and dX.get_device() == d)) and (dW is None or (dW.dtype is dw and dW.get_device() == d))):
-        _fit(d, dY=(dY, y), S=(S, s), W=(W, w), rstd=(rstd, _F32), dS=(dS, s), dR=(dR, s), dX=(dX, x), dW=(dW, dw))
+            and dY.numel() == n and S.numel() == n and W.numel() == K and rstd.numel() >= M and not (p.ldx or p.lds or p.ldy)
+            and dY.is_contiguous() and S.is_contiguous() and W.is_contiguous() and rstd.is_contiguous()
+            and (dS is None or (dS.dtype is s and dS.get_device() == d and dS.numel() == n and dS.is_contiguous()))
+            and (dR is None or (dR.dtype is s and dR.get_device() == d and dR.numel() == n and dR.is_contiguous()))
+            and (dX is None or (dX.dtype is x and dX.get_device() == d and dX.numel() == n and dX.is_contiguous()))
+            and (dW is None or (dW.dtype is dw and dW.get_device() == d and dW.numel() == K and dW.is_contiguous()))):
+        _fit(d, dY=(dY, y, M, K, p.ldy), S=(S, s, M, K, p.lds), W=(W, w, K), rstd=(rstd, _F32, M), dS=(dS, s, M, K, p.lds), dR=(dR, s, M, K, p.lds),
+             dX=(dX, x, M, K, p.ldx), dW=(dW, dw, K))
     status = lib().flux_norm_backward(p, dY.data_ptr(), S.data_ptr(), W.data_ptr(), rstd.data_ptr(), 0 if dS is None else dS.data_ptr(), 0 if dR is None else dR.data_ptr(),
                                       0 if dX is None else dX.data_ptr(), 0 if dW is None else dW.data_ptr(), *_space(workspace, d), _stream(stream))
     if status:
