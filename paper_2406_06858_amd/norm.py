@@ -49,7 +49,7 @@ _DT = {"bf16": FLUX_BF16, "f32": FLUX_F32, torch.bfloat16: FLUX_BF16, torch.floa
 _OUT = {"bf16": FLUX_NORM_BF16, "f32": FLUX_NORM_F32, "mx4": FLUX_NORM_MX4, "mx8": FLUX_NORM_MX8, torch.bfloat16: FLUX_NORM_BF16, torch.float32: FLUX_NORM_F32}
 _TYPES = (torch.bfloat16, torch.float32, torch.uint8, torch.uint8)          # by flux_dtype_t and flux_norm_out_t
 _U8, _F32 = torch.uint8, torch.float32
-_device = torch._C._cuda_getDevice
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)          # (a torch without GPU has no such function, and an error for every call)
 
 
 def _buf(t, dtype, device, what):

@@ -1,10 +1,15 @@
 """CPU-only: tensors whose numbers do not lie where the problem says are refused before anything is enqueued, and every view that does lie so is taken.  The
 library's entry points are replaced by ones that note what would have been called."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
 from paper_2406_06858_amd import loss, norm
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 M, K, V = 6, 64, 40
 BF16, F32 = torch.bfloat16, torch.float32
 
@@ -150,3 +155,11 @@ def test_one_dloss_for_all_rows(calls):
     with pytest.raises(ValueError):
         _call("loss_bwd", dloss=one)
     assert len(calls) == 2
+
+
+@pytest.mark.parametrize("module", ["norm", "loss", "ffn"])
+def test_a_torch_without_gpu_can_import(module):
+    """As `ffn`: what only a build of torch for GPUs has is looked for when a call is made."""
+    code = f"import torch; del torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream; import paper_2406_06858_amd.{module} as m; assert m.lib"
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-500:]
