@@ -90,6 +90,11 @@ __device__ __forceinline__ void decode8(const CastArgs& c, int row, int k, const
   store8<true>(p, c.K - k, v);
 }
 
+// The byte that number k of a row is in.
+template <int BITS>
+constexpr __device__ int byte_of(int k) { return k / (8 / BITS); }
+static_assert(byte_of<8>((1 << 30) - 8) == (1 << 30) - 8 && byte_of<4>((1 << 30) - 8) == (1 << 29) - 4, "rows of 2^30 numbers, in 32 bits");
+
 // A wave takes SEGS neighbouring pieces of a row: their loads are out together.  us by SEGS, 1 / 2 / 4, to bf16: 64x8192 2.9 / 3.3 / 4.0,
 // 1024x8192 6.1 / 5.7 / 5.9, 8192x8192 31.2 / 26.5 / 26.9, 8192x3413 16.3 / 14.7 / 16.1; to fp32: 64x8192 3.1 / 3.5 / 4.1, 8192x8192 105 / 102 / 115.
 constexpr int SEGS = 4;
@@ -105,7 +110,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const CastArgs c) {
 #pragma unroll
   for (int s = 0; s < SEGS; ++s) {
     const int k = min((seg + s) * PER_WAVE + lane * PER_LANE, (c.K - 1) / PER_LANE * PER_LANE);      // (past the end: the last again)
-    codes[s] = *reinterpret_cast<const V*>(c.q + (long long)row * c.row_bytes + k * BITS / 8);
+    codes[s] = *reinterpret_cast<const V*>(c.q + (long long)row * c.row_bytes + byte_of<BITS>(k));
     e[s] = c.scales[(long long)row * c.scale_row_bytes + k / 32];
   }
 #pragma unroll
