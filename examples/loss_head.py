@@ -30,6 +30,8 @@ class LossHead:
     """Plans, workspace and buffers of the ranks, made once and used by every step."""
 
     def __init__(self, M, D, V, R, eps=1e-5, device="cuda:0"):
+        if M < R or M % R:
+            raise ValueError(f"{M} tokens cannot be shared out over {R} ranks")
         self.M, self.D, self.V, self.R, self.chunk = M, D, V, R, M // R
         self.norm = norm.norm_problem(self.chunk, D, eps=eps, dw_accumulate=1)
         self.shards = [loss.loss_problem(M, V, D, v0=r * V, vocab=R * V) for r in range(R)]
