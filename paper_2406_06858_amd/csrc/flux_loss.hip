@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(256) ranks_kernel(const RanksArgs a) {
 static long long pitch_x(const flux_loss_t* p) { return p->ldx ? p->ldx : p->K; }
 static long long pitch_w(const flux_loss_t* p) { return p->ldw ? p->ldw : p->K; }
 static long long vocab_of(const flux_loss_t* p) { return p->vocab ? p->vocab : p->v0 + p->V; }
-constexpr long long MAX_VOCAB = 1ll << 62, MAX_LOGITS = 1ll << 36;          // (at most 2^23 workgroups of the smallest tile)
+constexpr long long MAX_VOCAB = 1ll << 62, MAX_LOGITS = 1ll << 36;          // (with V <= 2^28 below 2^24 workgroups of the smallest tile, both sides rounded up: 2^32 threads)
 constexpr int MAX_ROWS = 1 << 27;
 constexpr int MAX_WIDTH = 1 << 28;          // of gradients: a result's place in its row is counted in bytes, in 32 bits (store_pair)
 

@@ -31,11 +31,19 @@ class TileArgs(C.Structure):
     _fields_ += [(n, C.c_uint32) for n in ("pitch_a", "pitch_b", "bytes_a", "bytes_b", "pitch_s")]
     _fields_ += [(n, C.c_int32) for n in ("rows", "cols", "depth", "seg_slabs", "slabs", "full_tiles", "cut_tiles", "parts", "part_slabs", "tiles_m", "tiles_n", "band",
                                           "act", "out_f32", "accumulate", "stream")]
-    _fields_ += [("ld", C.c_int64), ("out", C.c_uint64 * 2)]
+    _fields_ += [("ld", C.c_int64), ("out", C.c_uint64 * 2)] + [(n, C.c_uint64) for n in ("g", "u", "factor", "addend", "partial", "counters")]
+
+
+class OuterArgs(C.Structure):
+    """csrc/flux_loss_few_grad.hip"""
+    _fields_ = [("t", TileArgs), ("zt", C.c_uint64), ("xt", C.c_uint64), ("rows_each", C.c_int32)]
+
+
+WORKSPACE = 99 << 40
 
 
 def _child():
-    """stdin: [shim, [[function, problem's fields, number of pointers behind it, the workspace's bytes]]]; stdout: a list of launches a call."""
+    """stdin: [shim, [[function, problem's fields, which of its pointers are not null, the workspace's bytes]]]; stdout: status and launches of every call."""
     shim, calls = json.load(sys.stdin)
     shim = C.CDLL(shim, mode=C.RTLD_GLOBAL)                    # (ahead of the runtime: its hipLaunchKernel is the one that is found)
     sys.path.insert(0, ROOT)
@@ -47,6 +55,10 @@ def _child():
         name = name.decode()
         seen = {"name": name, "grid": grid[:3], "block": block[:3]}
         cfg = re.search(r"3CfgILi(\d+)ELi(\d+)ELi(\d+)ELi\d+ELi\d+ELi\d+ELb([01])E", name)
+        outer = re.search(r"12outer_kernelILi(\d)E", name)
+        if outer:
+            o = C.cast(args[0], C.POINTER(OuterArgs)).contents
+            seen.update(terms=32 * int(outer.group(1)), rows=o.t.rows, cols=o.t.cols, zt=o.zt, xt=o.xt, rows_each=o.rows_each)
         if cfg:
             seen["kind"], seen["bm"], seen["bn"], seen["masked"] = (int(v) for v in cfg.groups())
             t = C.cast(args[0], C.POINTER(TileArgs)).contents
@@ -59,13 +71,14 @@ def _child():
         launches.clear()
         p = loss.loss_problem(**fields)
         # (a terabyte apart)
-        status = getattr(lib, function)(C.byref(p), *[(i + 1) << 40 if i in pointers else 0 for i in range(max(pointers) + 1)], 99 << 40, ws, None)
+        status = getattr(lib, function)(C.byref(p), *[(i + 1) << 40 if i in pointers else 0 for i in range(max(pointers) + 1)], WORKSPACE, ws, None)
         out.append({"status": status, "launches": list(launches)})
     json.dump(out, sys.stdout)
 
 
 def record(tmp_path, calls):
-    """[(function, problem's fields, which of its pointers are not null)] -> [{status, launches}]; the workspace is as large as any has to be."""
+    """[(function, problem's fields, which of its pointers are not null)] -> [{status, launches}].  Pointer i is (i + 1) << 40, the workspace lies at WORKSPACE and is as large as
+    any has to be."""
     src, so = tmp_path / "shim.c", tmp_path / "shim.so"
     src.write_text(SHIM)
     subprocess.run(["gcc", "-shared", "-fPIC", "-o", str(so), str(src), "-ldl"], check=True)

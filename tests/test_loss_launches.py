@@ -1,7 +1,9 @@
 """CPU-only: what the loss launches reads nothing past the end of its matrices.  The launches are noted by tests/launch_recorder.py, and the places that a grid of
 tiles reads are worked out from the arguments, in whole numbers of any size."""
+import random
+
 import pytest
-from launch_recorder import record
+from launch_recorder import WORKSPACE, record
 
 from paper_2406_06858_amd import binding as fb
 from paper_2406_06858_amd import loss
@@ -92,3 +94,68 @@ def test_results_have_their_places_in_32_bits(tmp_path):
             continue
         for t in _check(call, p):
             assert t["tiles_n"] * t["bn"] * 4 < 1 << 31, (p, t["name"])
+
+
+def _some_problem(rng):
+    """Sizes over their logarithm, in turn whole tiles, multiples of 8 and 64 and odd; pitches, pieces, tiles and cuts of the caller's own."""
+    size = lambda most, step: max(step, int(most ** rng.random()) // step * step)      # noqa: E731
+    while True:
+        step = rng.choice([1, 1, 8, 64, 256])
+        p = dict(M=size(rng.choice([128, 20000, 1 << 22]), step), V=size(rng.choice([5000, 60000, 1 << 20]), step), K=size(rng.choice([2048, 16384]), rng.choice([8, 8, 64, 256])))
+        if rng.random() < 0.2:
+            p["ldx"], p["ldw"] = p["K"] + 8 * rng.randrange(0, 20), p["K"] + 8 * rng.randrange(0, 20)
+        if rng.random() < 0.3:
+            p["piece"] = 64 * rng.randrange(1, 200)
+        if rng.random() < 0.3:
+            p["tile_config"], p["split_k"] = rng.randrange(0, 7), rng.randrange(0, 9)
+        p.update(dx_dtype=rng.choice(["bf16", "f32"]), dw_dtype=rng.choice(["bf16", "f32"]), dloss_one=rng.randrange(2))
+        if loss.flux_loss_workspace_bytes(loss.FLUX_LOSS_BACKWARD, loss.loss_problem(**p)) > 0:
+            return p
+
+
+@pytest.mark.parametrize("function,pointers,op", [("flux_loss", range(6), loss.FLUX_LOSS_FORWARD), ("flux_loss_backward", BACKWARD, loss.FLUX_LOSS_BACKWARD)])
+def test_any_problem_stays_in_its_buffers(tmp_path, function, pointers, op):
+    rng = random.Random(function)
+    problems = [_some_problem(rng) for _ in range(600)]
+    calls = record(tmp_path, [(function, p, pointers) for p in problems])
+    kinds = set()
+    for call, p in zip(calls, problems):
+        end = WORKSPACE + loss.flux_loss_workspace_bytes(op, loss.loss_problem(**p))
+        for t in call["launches"]:
+            assert all(g * b < 1 << 32 for g, b in zip(t["grid"], t["block"])), (p, t["name"])
+            if "terms" in t:
+                assert t["xt"] - t["zt"] == t["rows"] * t["terms"] * 2 and t["xt"] + t["cols"] * t["terms"] * 2 <= end and t["grid"][1] * t["rows_each"] >= t["rows"], p
+                kinds.add("outer")
+        for t in _check(call, p):
+            bytes_a, bytes_b = _extents(t)
+            assert (t["bytes_a"], t["bytes_b"]) == (bytes_a, bytes_b), (p, t["name"])
+            held = [(t["a"][0], bytes_a), (t["b"][0], bytes_b)]
+            if t["kind"] != ALONG:
+                held.append((t["out"][0], ((t["rows"] - 1) * t["ld"] + t["cols"]) * (4 if t["out_f32"] else 2)))
+            if t["kind"] == DX and t["addend"]:
+                held.append((t["addend"], ((t["rows"] - 1) * t["ld"] + t["cols"]) * 4))
+            if t["cut_tiles"]:
+                held.append((t["partial"], t["cut_tiles"] * t["parts"] * t["bm"] * t["bn"] * 4))
+                assert t["counters"] == WORKSPACE and t["cut_tiles"] <= 512 and (t["parts"] - 1) * t["part_slabs"] < t["slabs"] <= t["parts"] * t["part_slabs"], p
+            lx, lw = p.get("ldx", p["K"]), p.get("ldw", p["K"])
+            x, w = (p["M"] - 1) * lx + p["K"], (p["V"] - 1) * lw + p["K"]
+            ends = {0: x * 2, 1: w * 2, 5: x * (2, 4)[p["dx_dtype"] == "f32"], 6: w * (2, 4)[p["dw_dtype"] == "f32"], (WORKSPACE >> 40) - 1: end - WORKSPACE}
+            for at, size in held:
+                assert at % (1 << 40) + size <= ends[(at >> 40) - 1], (p, t["name"], at, size)
+            assert t["full_tiles"] + t["cut_tiles"] == t["tiles_m"] * t["tiles_n"] and t["grid"][0] == t["full_tiles"] + t["cut_tiles"] * t["parts"], p
+            kinds.add((t["kind"], t["masked"], bool(t["cut_tiles"])))
+    assert {(ALONG, m, c) for m in (0, 1) for c in (False, True)} <= kinds
+    if op == loss.FLUX_LOSS_BACKWARD:
+        assert {(k, 1, c) for k in (DX, DW) for c in (False, True)} | {(DX, 0, False), (DW, 0, False), "outer"} <= kinds
+
+
+def test_grids_are_below_2_32_threads(tmp_path):
+    """The most tiles that the limits on M, V and K allow, both sides rounded up."""
+    problems = [dict(M=133956083, V=513, K=8), dict(M=1 << 27, V=512, K=8), dict(M=(1 << 27) - 64 + 1, V=449, K=8), dict(M=1, V=(1 << 28) - 8, K=8), dict(M=257, V=(1 << 27) - 1, K=8),
+                dict(M=(1 << 25) - 1, V=2047, K=8), dict(M=512, V=1 << 27, K=8)]
+    problems = [dict(p, tile_config=config) for p in problems for config in range(7)]
+    tiles = 0
+    for call, p in zip(record(tmp_path, [("flux_loss", p, range(6)) for p in problems]), problems):
+        assert call["status"] == 0 and all(g * b < 1 << 32 for t in call["launches"] for g, b in zip(t["grid"], t["block"])), p
+        tiles = max([tiles] + [t["grid"][0] for t in call["launches"] if "kind" in t])
+    assert 1 << 23 < tiles < 1 << 24
