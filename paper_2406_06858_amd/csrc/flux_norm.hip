@@ -399,14 +399,16 @@ __global__ void __launch_bounds__(256) norm_dw_kernel(const NormGradArgs a, int 
 __global__ void __launch_bounds__(256) norm_dw_join_kernel(const float* partial, long long pitch, int groups, int K, void* dw, int f32, int accumulate) {
   __shared__ float part[32][33];
   const int c = threadIdx.x % 8 * 4, run = threadIdx.x / 8, each = (groups + 31) / 32, first = run * each, last = min(first + each, groups);
+  const long long k0 = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 32;
+  if (k0 >= K) return;                           // (the whole workgroup)
   flux::f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  const float* const from = partial + blockIdx.x * 32ll + c;
+  const float* const from = partial + k0 + c;
 #pragma unroll 8
   for (int g = first; g < last; ++g) sum += *reinterpret_cast<const flux::f32x4*>(from + g * pitch);
 #pragma unroll
   for (int e = 0; e < 4; ++e) part[run][c + e] = sum[e];
   __syncthreads();
-  const int k = blockIdx.x * 32 + threadIdx.x;
+  const int k = (int)k0 + threadIdx.x;
   if (threadIdx.x >= 32 || k >= K) return;
   float v = 0.f;
 #pragma unroll
@@ -586,7 +588,7 @@ int flux_norm_backward(const flux_norm_t* p, const void* dY, const void* S, cons
   const bool yf = p->out == FLUX_NORM_F32, sf = p->s_dtype == FLUX_F32;
   FFN_HIP(yf ? (sf ? go_grad<float, float>(g, a, s) : go_grad<float, uint16_t>(g, a, s)) : (sf ? go_grad<uint16_t, float>(g, a, s) : go_grad<uint16_t, uint16_t>(g, a, s)));
   if (a.partial != nullptr)
-    FFN_HIP(start(norm_dw_join_kernel, dim3(ceil_div(p->K, 32)), s, (const float*)a.partial, a.pitch, g.groups, (int)p->K, dW, (int)(p->dw_dtype == FLUX_F32), (int)p->dw_accumulate));
+    FFN_HIP(start(norm_dw_join_kernel, grid_of(ceil_div(p->K, 32)), s, (const float*)a.partial, a.pitch, g.groups, (int)p->K, dW, (int)(p->dw_dtype == FLUX_F32), (int)p->dw_accumulate));
   return FLUX_OK;
 }
 

@@ -47,7 +47,7 @@ def _child():
     shim, calls = json.load(sys.stdin)
     shim = C.CDLL(shim, mode=C.RTLD_GLOBAL)                    # (ahead of the runtime: its hipLaunchKernel is the one that is found)
     sys.path.insert(0, ROOT)
-    from paper_2406_06858_amd import loss
+    from paper_2406_06858_amd import loss, norm
     launches = []
 
     @C.CFUNCTYPE(None, C.c_char_p, C.POINTER(C.c_uint32), C.POINTER(C.c_uint32), C.POINTER(C.c_void_p))
@@ -66,12 +66,14 @@ def _child():
         launches.append(seen)
 
     shim.recorder_note(note)
-    lib, out = loss.lib(), []
+    libs, out = {"loss": loss.lib(), "norm": norm.lib()}, []
     for function, fields, pointers, ws in calls:
         launches.clear()
-        p = loss.loss_problem(**fields)
+        which = "norm" if "norm" in function else "loss"
+        p = (norm.norm_problem if which == "norm" else loss.loss_problem)(**fields)
         # (a terabyte apart)
-        status = getattr(lib, function)(C.byref(p), *[(i + 1) << 40 if i in pointers else 0 for i in range(max(pointers) + 1)], WORKSPACE, ws, None)
+        args = [(i + 1) << 40 if i in pointers else 0 for i in range(max(pointers) + 1)] + ([] if function == "flux_norm" else [WORKSPACE, ws])
+        status = getattr(libs[which], function)(C.byref(p), *args, None)
         out.append({"status": status, "launches": list(launches)})
     json.dump(out, sys.stdout)
 
