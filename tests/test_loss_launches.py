@@ -22,6 +22,7 @@ def _reads(t):
 
 def _check(call, problem):
     assert call["status"] == 0, problem
+    assert all(g * b < 1 << 32 for t in call["launches"] for g, b in zip(t["grid"], t["block"])), problem
     tiles = [t for t in call["launches"] if "kind" in t]
     for t in tiles:
         if not t["masked"]:
@@ -122,7 +123,6 @@ def test_any_problem_stays_in_its_buffers(tmp_path, function, pointers, op):
     for call, p in zip(calls, problems):
         end = WORKSPACE + loss.flux_loss_workspace_bytes(op, loss.loss_problem(**p))
         for t in call["launches"]:
-            assert all(g * b < 1 << 32 for g, b in zip(t["grid"], t["block"])), (p, t["name"])
             if "terms" in t:
                 assert t["xt"] - t["zt"] == t["rows"] * t["terms"] * 2 and t["xt"] + t["cols"] * t["terms"] * 2 <= end and t["grid"][1] * t["rows_each"] >= t["rows"], p
                 kinds.add("outer")
@@ -147,6 +147,14 @@ def test_any_problem_stays_in_its_buffers(tmp_path, function, pointers, op):
     assert {(ALONG, m, c) for m in (0, 1) for c in (False, True)} <= kinds
     if op == loss.FLUX_LOSS_BACKWARD:
         assert {(k, 1, c) for k in (DX, DW) for c in (False, True)} | {(DX, 0, False), (DW, 0, False), "outer"} <= kinds
+
+
+def test_grids_of_gradients_at_their_limits(tmp_path):
+    problems = [dict(M=1, V=(1 << 28) - 1, K=8), dict(M=64, V=(1 << 28) - 1, K=8), dict(M=100, V=(1 << 28) - 64, K=8), dict(M=(1 << 25) - 1, V=64, K=56), dict(M=(1 << 25) - 1, V=2047, K=8, piece=64),
+                dict(M=1, V=7, K=1 << 28), dict(M=7, V=7, K=1 << 28), dict(M=129, V=1, K=(1 << 24) - (1 << 18)), dict(M=3, V=(1 << 21) + 1, K=1016)]
+    problems = [dict(p, dx_dtype=dtype, dw_dtype=dtype) for p in problems for dtype in ("bf16", "f32")]
+    for call, p in zip(record(tmp_path, [("flux_loss_backward", p, BACKWARD) for p in problems]), problems):
+        assert _check(call, p)
 
 
 def test_grids_are_below_2_32_threads(tmp_path):
