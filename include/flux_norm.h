@@ -22,7 +22,7 @@ extern "C" {
 
 /* What Y is: numbers, or blocks of 32 along a row (OCP Microscaling Formats 1.0, "MXFP4" and "MXFP8") laid out as flux_mx4_quantize lays them out.
  * 8 bits (E4M3): the largest magnitude's exponent less 8 is the block's, numbers are held at 448, and a row of numbers takes 32 bytes per
- * block: flux_mx8_row_bytes.  Scales as with 4 bits (flux_mx4_scale_row_bytes). */
+ * block: flux_mx8_row_bytes.  Scales as with 4 bits (flux_mx4_scale_row_bytes).  (8 bits are for a caller who moves Y: the products of flux_ffn.h read 4 bits.) */
 typedef enum { FLUX_NORM_BF16 = 0, FLUX_NORM_F32 = 1, FLUX_NORM_MX4 = 2, FLUX_NORM_MX8 = 3 } flux_norm_out_t;
 
 /* M >= 1; 1 <= K <= 2^30; pitches at least a row long; every matrix below 2^31 elements. */
@@ -51,7 +51,7 @@ int flux_norm(const flux_norm_t* p, const void* X, const void* R, const void* W,
 /* Bytes of workspace of the backward pass (0 for a problem that is refused).  It may be shared with the operators of flux_ffn.h, as they share theirs. */
 size_t flux_norm_workspace_bytes(const flux_norm_t* p);
 
-/* Gradients of flux_norm, whose S (X where there was no R) and rstd are read.
+/* Gradients of flux_norm, whose S and rstd are read.  (Where there was no R, S is X, and s_dtype and lds have to be X's.)
  *   dY [M,K]          gradient of Y, bf16 or fp32 as `out` says; FLUX_ERR_UNSUPPORTED where Y is in blocks
  *   dS [M,K]          s_dtype: the gradient of S from what else reads it, or NULL for none
  *   dR [M,K]          s_dtype: the gradient of R, and of X; may be dS itself.  May be NULL

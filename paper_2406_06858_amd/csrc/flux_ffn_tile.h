@@ -132,7 +132,8 @@ __device__ __forceinline__ void mfma_scaled(f32x4& acc, const u32x4& a, const u3
 // One operand tile of R rows (or columns) of the result by 128 bytes of contraction, in LDS in one of two ways:
 //   along   rows of 128 bytes, one instruction 8 rows;
 //   across  (T) one row per step of the contraction, R values each, one instruction 512 / R of those.
-// (The same patterns as DmaLoader's.)  A lane outside the matrix loads from outside the buffer's records: zeros.
+// (The same patterns as DmaLoader's.)  Where the contraction ends, and past the last column of a matrix that lies across, a lane loads from outside the buffer's records:
+// zeros.  What it loads for a row of the result past the last one of a matrix that lies along is its finish's to leave alone (see load).
 template <int R, bool T, bool EDGE, bool MX, bool ONCE, bool TIGHT>
 struct OperandLoader {
   static constexpr int RPI = T ? 512 / R : 8;
@@ -162,10 +163,12 @@ struct OperandLoader {
       k_vec = s * 8;
     }
   }
-  // The d-th of the wave's loads of the slab that starts at k (`depth` in all) into `tile`.  Rows past the last one end up past the buffer's records by themselves
-  // where the whole offset is the lane's (a sum that stays at the largest number instead of wrapping): what is left to ask is whether a slab's last
-  // pieces are in the row (once a slab), and whether rows of a contraction that lies across begin at all (uniform).  With a mask for every load the
-  // 256x256 tile ran out of scalar registers: logits of 8192x4000x8192 409 us, 366 for 4096 columns without masks.
+  // The d-th of the wave's loads of the slab that starts at k (`depth` in all) into `tile`.  Rows of the contraction past the last one end up past the buffer's records by
+  // themselves where the whole offset is the lane's (a sum that stays at the largest number instead of wrapping; a scalar offset takes no part in the range check): what is
+  // left to ask is whether a slab's last pieces are in the row (once a slab), and whether rows of a contraction that lies across begin at all (uniform).  With a mask
+  // for every load the 256x256 tile ran out of scalar registers: logits of 8192x4000x8192 409 us, 366 for 4096 columns without masks.
+  // Along: a row of the result past the last one is mostly past the records too, but with 100 MB and more from row to row its offset may wrap to a place between the
+  // caller's rows.  Whatever lies there, NaN too, comes into that row's (column's) sums and no others, and a finish neither stores these nor adds anything up over them.
   // TIGHT: the place in LDS is added up at each load.  Left to itself the compiler keeps all forty places of the large tile in scalar registers; beside the
   // segments of dX and logits there is no room for these, and they came back from vector lanes one by one.  us without / with: gradients of the loss
   // 8192x32000x8192 8518 / 8470, statistics of 8192x4000x8192 359 / 356, dX of 8192x8192 over two times 3584 633 / 625; dW, whose registers suffice, 617 / 624.
@@ -747,7 +750,7 @@ __device__ __forceinline__ int by_die(int b, int n) {
 }
 
 // One workgroup's tile or part of one.  finish(job, sums, row, column, lane) takes 16 rows of a wave's part of the result (see finish_rows16);
-// finish.ask(row, cols) asks for what it needs of the tile's rows ahead of the main loop, finish.keep(pool) leaves it in LDS behind it.
+// finish.ask(t, m0) asks for what it needs of the tile's rows ahead of the main loop, finish.keep(pool) leaves it in LDS behind it.
 template <class C, class F>
 __device__ __forceinline__ void tile_body(const TileArgs& t, unsigned char* pool, F& finish) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -152,7 +152,7 @@ static Plan plan_dx(const flux_loss_t* p, int cols) { return plan_tiles(DX_KN, p
 static Plan plan_dw(const flux_loss_t* p, int cols) { return plan_tiles(DW, cols, p->K, p->M, 0, 0); }
 
 // Columns of the backward pass's pieces, the last one's apart.  dZ of a piece takes 256 MiB, what the Infinity Cache holds: in smaller ones dX is added to the more
-// often, larger ones take memory and give nothing.  us of 8192x32000x8192 by columns a piece: 2048 10650, 4096 9530, 8192 9050, 16384 8960, 32768 8990.
+// often, larger ones take memory and give nothing.  (Of few rows it is the whole vocabulary: W is read from memory twice, for Z and for dX.)  us of 8192x32000x8192 by columns a piece: 2048 10650, 4096 9530, 8192 9050, 16384 8960, 32768 8990.
 static long long whole_lines(long long n) { return (n + 63) / 64 * 64; }
 static int piece_of(const flux_loss_t* p) {
   const long long all = whole_lines(p->V);

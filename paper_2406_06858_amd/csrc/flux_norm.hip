@@ -6,8 +6,9 @@
 // Sums are fp32, a lane's own first and then over lanes in a fixed order.  r is taken with the square root and the division that round
 // correctly: one a row.
 //
-// Memory bounds both: each number is read once and each result written once.  us (TB/s): forward in bf16 8192x12288 134 (6.0), 8192x8192 90 (6.0); backward
-// 8192x8192 with dS 100 (5.6, and 4 for the join of dW); a copy by a kernel reaches 6.3.  Up to some hundred rows it is the launch.
+// Memory bounds both: each number is read once and each result written once.  us (TB/s): forward in bf16 8192x12288 135 (6.0), 8192x8192 91 (5.9), into 4 bits 83
+// (5.3); backward with dS 8192x8192 100 (5.6, and 4 for the join of dW), 8192x12288 151 (5.3); a pass that scales 1 GiB reaches 6.25.  Up to some hundred rows it is
+// the launch.
 #include <algorithm>
 #include "flux_ffn_internal.h"
 #include "flux_mx_blocks.h"
@@ -98,7 +99,7 @@ __device__ __forceinline__ void write_y(const NormArgs& a, int row, int k, int l
 // ---- kernels --------------------------------------------------------------------------------------------------
 // The row in registers, so that memory is read once: LANES lanes a row, VECS pieces of 8 numbers a lane, 256 / LANES rows a workgroup where LANES is less.  WHOLE: K
 // is a multiple of 8, a piece is in the row or is not.  All pieces of the row and of W are asked for before the first is used.  Results in bf16 go past the caches
-// (8192x8192 98 us, through them 106); fp32 ones, of which a lane's two stores are half lines, do not (1496x5112 12.2, past them 14.3).
+// (8192x8192 91 us, through them 95); fp32 ones, of which a lane's two stores are half lines, do not (1496x5112 12.2, past them 14.3).
 template <class TX, class TS, bool RESIDUAL, int LANES, int VECS, bool WHOLE>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) norm_row_kernel(const NormArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
@@ -503,7 +504,7 @@ static hipError_t go_grad(const GradPlan& g, const NormGradArgs& a, hipStream_t 
   GO(512, 1, true, true);
   GO(768, 1, true, true);
   GO(1024, 1, true, true);
-  GO(768, 2, sizeof(TS) == 2, sizeof(TS) == 2 && sizeof(TY) == 2);          // (with 32 bits there are no registers for the next row)
+  GO(768, 2, sizeof(TS) == 2, sizeof(TS) == 2 && sizeof(TY) == 2);          // (beside a stream in 32 bits there are no registers for the next row; with a row's odd end beside dY in 32 bits neither)
   if (g.lanes == 1024 && g.vecs == 2) return start_with(norm_grad_row_kernel<TY, TS, 1024, 2, false, true>, dim3(g.groups), 1024, s, a);
 #undef GO
   if (a.partial != nullptr) {
