@@ -65,8 +65,9 @@ def flux_loss(p, X, W, target, lse, logit, loss=None, workspace=None, stream=Non
     d, t, M, K = _device(), _TARGETS[p.target_dtype & 1], p.M, p.K
     if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and logit.dtype is _F32
             and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == logit.get_device()
-            and X.numel() == M * K and W.numel() == p.V * K and target.numel() >= M and lse.numel() >= M and logit.numel() >= M and not (p.ldx or p.ldw)
-            and X.is_contiguous() and W.is_contiguous() and target.is_contiguous() and lse.is_contiguous() and logit.is_contiguous()
+            and (X.numel() == M * K and W.numel() == p.V * K and X.is_contiguous() and W.is_contiguous() if not (p.ldx or p.ldw) else
+                 X.shape == (M, K) and W.shape == (p.V, K) and X.stride() == (p.ldx or K, 1) and W.stride() == (p.ldw or K, 1))
+            and target.numel() >= M and lse.numel() >= M and logit.numel() >= M and target.is_contiguous() and lse.is_contiguous() and logit.is_contiguous()
             and (loss is None or (loss.dtype is _F32 and loss.get_device() == d and loss.numel() >= M and loss.is_contiguous()))):
         _fit(d, X=(X, _BF16, M, K, p.ldx), W=(W, _BF16, p.V, K, p.ldw), target=(target, t, M), lse=(lse, _F32, M), logit=(logit, _F32, M), loss=(loss, _F32, M))
     status = lib().flux_loss(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), logit.data_ptr(), 0 if loss is None else loss.data_ptr(),
@@ -87,13 +88,14 @@ def flux_loss_join(p, lses, logits, target, lse=None, logit=None, loss=None, str
 
 def flux_loss_backward(p, X, W, target, lse, dloss, dX, dW, workspace, stream=None):
     d, t, x, w, M, K = _device(), _TARGETS[p.target_dtype & 1], _TYPES[p.dx_dtype & 1], _TYPES[p.dw_dtype & 1], p.M, p.K
-    n, m, rows = M * K, p.V * K, 1 if p.dloss_one else M
+    n, m, rows, side = M * K, p.V * K, 1 if p.dloss_one else M, not (p.ldx or p.ldw)
     if not (X.dtype is _BF16 and W.dtype is _BF16 and target.dtype is t and lse.dtype is _F32 and dloss.dtype is _F32
             and d == X.get_device() == W.get_device() == target.get_device() == lse.get_device() == dloss.get_device()
-            and X.numel() == n and W.numel() == m and target.numel() >= M and lse.numel() >= M and dloss.numel() >= rows and not (p.ldx or p.ldw)
-            and X.is_contiguous() and W.is_contiguous() and target.is_contiguous() and lse.is_contiguous() and dloss.is_contiguous()
-            and (dX is None or (dX.dtype is x and dX.get_device() == d and dX.numel() == n and dX.is_contiguous()))
-            and (dW is None or (dW.dtype is w and dW.get_device() == d and dW.numel() == m and dW.is_contiguous()))):
+            and (X.numel() == n and W.numel() == m and X.is_contiguous() and W.is_contiguous() if side else
+                 X.shape == (M, K) and W.shape == (p.V, K) and X.stride() == (p.ldx or K, 1) and W.stride() == (p.ldw or K, 1))
+            and target.numel() >= M and lse.numel() >= M and dloss.numel() >= rows and target.is_contiguous() and lse.is_contiguous() and dloss.is_contiguous()
+            and (dX is None or (dX.dtype is x and dX.get_device() == d and (dX.numel() == n and dX.is_contiguous() if side else dX.shape == (M, K) and dX.stride() == (p.ldx or K, 1))))
+            and (dW is None or (dW.dtype is w and dW.get_device() == d and (dW.numel() == m and dW.is_contiguous() if side else dW.shape == (p.V, K) and dW.stride() == (p.ldw or K, 1))))):
         _fit(d, X=(X, _BF16, M, K, p.ldx), W=(W, _BF16, p.V, K, p.ldw), target=(target, t, M), lse=(lse, _F32, M), dloss=(dloss, _F32, rows),
              dX=(dX, x, M, K, p.ldx), dW=(dW, w, p.V, K, p.ldw))
     status = lib().flux_loss_backward(p, X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), 0 if dX is None else dX.data_ptr(),

@@ -117,10 +117,12 @@ def flux_norm(p, X, R, W, S, Y, scales=None, rstd=None, stream=None):
     held = n = M * K
     if y is _U8:
         held, scaled = _in_blocks(M, K, p.out)
-    if not (X.dtype is x and W.dtype is w and Y.dtype is y and d == X.get_device() == W.get_device() == Y.get_device()
-            and X.numel() == n and Y.numel() == held and W.numel() == K and X.is_contiguous() and Y.is_contiguous() and W.is_contiguous() and not (p.ldx or p.lds or p.ldy)
-            and (R is None or (R.dtype is s and R.get_device() == d and R.numel() == n and R.is_contiguous()))
-            and (S is None or (S.dtype is s and S.get_device() == d and S.numel() == n and S.is_contiguous()))
+    side = not (p.ldx or p.lds or p.ldy)                                        # (rows side by side)
+    if not (X.dtype is x and W.dtype is w and Y.dtype is y and d == X.get_device() == W.get_device() == Y.get_device() and W.numel() == K and W.is_contiguous()
+            and (X.numel() == n and X.is_contiguous() if side else X.shape == (M, K) and X.stride() == (p.ldx or K, 1))
+            and (Y.numel() == held and Y.is_contiguous() if side or y is _U8 else Y.shape == (M, K) and Y.stride() == (p.ldy or K, 1))
+            and (R is None or (R.dtype is s and R.get_device() == d and (R.numel() == n and R.is_contiguous() if side else R.shape == (M, K) and R.stride() == (p.lds or K, 1))))
+            and (S is None or (S.dtype is s and S.get_device() == d and (S.numel() == n and S.is_contiguous() if side else S.shape == (M, K) and S.stride() == (p.lds or K, 1))))
             and (scales is None or (y is _U8 and scales.dtype is _U8 and scales.get_device() == d and scales.numel() == scaled and scales.is_contiguous()))
             and (rstd is None or (rstd.dtype is _F32 and rstd.get_device() == d and rstd.numel() >= M and rstd.is_contiguous()))):
         _fit(d, X=(X, x, M, K, p.ldx), R=(R, s, M, K, p.lds), W=(W, w, K), S=(S, s, M, K, p.lds), Y=(Y, y, held) if y is _U8 else (Y, y, M, K, p.ldy),
@@ -135,12 +137,14 @@ def flux_norm_backward(p, dY, S, W, rstd, dS=None, dR=None, dX=None, dW=None, wo
     d, x, s, w, y, dw = _device(), _TYPES[p.x_dtype & 1], _TYPES[p.s_dtype & 1], _TYPES[p.w_dtype & 1], _TYPES[p.out & 1], _TYPES[p.dw_dtype & 1]
     M, K = p.M, p.K
     n = M * K
+    side = not (p.ldx or p.lds or p.ldy)
     if not (dY.dtype is y and S.dtype is s and W.dtype is w and rstd.dtype is _F32 and d == dY.get_device() == S.get_device() == W.get_device() == rstd.get_device()
-            and dY.numel() == n and S.numel() == n and W.numel() == K and rstd.numel() >= M and not (p.ldx or p.lds or p.ldy)
-            and dY.is_contiguous() and S.is_contiguous() and W.is_contiguous() and rstd.is_contiguous()
-            and (dS is None or (dS.dtype is s and dS.get_device() == d and dS.numel() == n and dS.is_contiguous()))
-            and (dR is None or (dR.dtype is s and dR.get_device() == d and dR.numel() == n and dR.is_contiguous()))
-            and (dX is None or (dX.dtype is x and dX.get_device() == d and dX.numel() == n and dX.is_contiguous()))
+            and W.numel() == K and W.is_contiguous() and rstd.numel() >= M and rstd.is_contiguous()
+            and (dY.numel() == n and dY.is_contiguous() if side else dY.shape == (M, K) and dY.stride() == (p.ldy or K, 1))
+            and (S.numel() == n and S.is_contiguous() if side else S.shape == (M, K) and S.stride() == (p.lds or K, 1))
+            and (dS is None or (dS.dtype is s and dS.get_device() == d and (dS.numel() == n and dS.is_contiguous() if side else dS.shape == (M, K) and dS.stride() == (p.lds or K, 1))))
+            and (dR is None or (dR.dtype is s and dR.get_device() == d and (dR.numel() == n and dR.is_contiguous() if side else dR.shape == (M, K) and dR.stride() == (p.lds or K, 1))))
+            and (dX is None or (dX.dtype is x and dX.get_device() == d and (dX.numel() == n and dX.is_contiguous() if side else dX.shape == (M, K) and dX.stride() == (p.ldx or K, 1))))
             and (dW is None or (dW.dtype is dw and dW.get_device() == d and dW.numel() == K and dW.is_contiguous()))):
         _fit(d, dY=(dY, y, M, K, p.ldy), S=(S, s, M, K, p.lds), W=(W, w, K), rstd=(rstd, _F32, M), dS=(dS, s, M, K, p.lds), dR=(dR, s, M, K, p.lds),
              dX=(dX, x, M, K, p.ldx), dW=(dW, dw, K))
