@@ -63,7 +63,7 @@ int flux_loss_join(const flux_loss_t* p, int32_t R, const float* const* lses, co
 /* Gradients of sum over rows of dloss * loss.  lse is that of the whole vocabulary.  dZ / D, D the largest |dloss| of the rows that count, is taken in fp32 and
  * rounded to bf16 once, as operand of the two products, which accumulate in fp32, take the factor D, and are rounded once at the end.  (Rows whose |dloss|
  * is below 2^-100 of the largest lose digits.)  So dX and dW in fp32 hold dZ's rounding, up to half a step of bf16 (2^-8) of every term: fp32 spares them a rounding of their own, and
- * adds up micro-batches without one.  Off by, in parts of their norm: 3e-4 to 8e-4 with one dloss for all rows, 1.7e-3 with one a row; in bf16 1.7e-3 and 2.3e-3.
+ * adds up micro-batches without one.  Off by, in parts of their norm: 2e-4 to 8e-4 with one dloss for all rows, 1.4e-3 to 1.7e-3 with one a row; in bf16 1.7e-3 and 2.3e-3.
  *   dloss             fp32, [M] or one number
  *   dX [M,K]          dx_dtype: this rank's part of the sum over ranks.  May be NULL
  *   dW [V,K]          dw_dtype.  May be NULL

@@ -24,7 +24,7 @@ struct LossArgs {
 // What a row's dZ is multiplied by: dloss / D.  Where every row that counts has the same dloss, as in a mean, that is 1, and the target's number, which
 // outweighs the others, is p - 1: all but free of rounding to bf16 where p is small.  With dloss in dZ it is -dloss in every row, rounded the same way in
 // every row: up to 2^-8 of the gradients.  Error of dX and dW in bf16 of a mean, 37x13183x6144 and the like against 64 bits, in parts of their norm: 1.7e-3, as the
-// rounding of the results alone gives; with dloss in dZ up to 4e-3.  (In fp32 3e-4 to 8e-4; with a dloss of its own in every row 2.3e-3, in fp32 1.7e-3.)
+// rounding of the results alone gives; with dloss in dZ up to 4e-3.  (In fp32 2e-4 to 8e-4; with a dloss of its own in every row 2.3e-3, in fp32 1.7e-3.)
 __device__ __forceinline__ float row_dloss(const LossArgs& l, int row, bool counts) { return counts ? l.dloss[l.dloss_one ? 0 : row] : 0.f; }
 __device__ __forceinline__ float row_factor(const LossArgs& l, float dloss, float most) {
   return l.dloss_one ? (dloss == 0.f ? 0.f : 1.f) : dloss / most;
